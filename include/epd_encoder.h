@@ -402,6 +402,91 @@ int epd_op_merge(int32_t dtype, const void* y, const int32_t* merge_idx, void* o
                  int32_t hidden, void* stream);
 
 /* ------------------------------------------------------------------------------------------
+ * Gated feed-forward block, and gradients (for training an encoder's layers)
+ * ---------------------------------------------------------------------------------------- */
+
+enum { EPD_GATE_SILU = 0, EPD_GATE_GELU_TANH = 1, EPD_GATE_GELU_ERF = 2 };   /* act of the gated product */
+
+/* out[M,N] = act(x[M,K] . w[0:N,K]^T + bias[0:N]) * (x . w[N:2N,K]^T + bias[N:2N]): both projections of a gated
+ * feed-forward block, the activation and the product.  w [2N, K]: gate rows, then up rows; bias [2N] or NULL.  pre
+ * (optional) [M, 2N] receives the two projections in front of the activation, gate | up, which the gradient reads.
+ * x, w, bias, out, pre: element type per dtype; sums are held in float.  Leading dimensions in elements.  Outputs must
+ * not overlap inputs or each other.  In bf16 the tensor-core kernels run when N, K and every leading dimension are
+ * multiples of 8 and every matrix starts on a 16-byte boundary; other shapes run on a plain-FMA kernel.
+ * M == 0 is valid and launches nothing.  Extents up to 2^28; EPD_EINVAL otherwise. */
+int epd_op_gated_linear(int32_t dtype, const void* x, int64_t ldx, const void* w, int64_t ldw, const void* bias, void* out,
+                        int64_t ldo, void* pre, int64_t ldp, int64_t M, int64_t N, int64_t K, int32_t gate,
+                        void* stream);
+
+/* The whole block: hidden[M,N] as epd_op_gated_linear(x, w_in, b_in), then out[M,D] = hidden . w_out[D,N]^T + b_out.
+ * hidden is caller memory (scratch for inference; the gradient reads it), pre as above.  flags: EPD_LINEAR_ACCUMULATE
+ * (out float, += : the residual update) and EPD_LINEAR_OUT_F32 as for epd_op_linear.  One token and a handful of tokens
+ * run on kernels that stream the weights. */
+int epd_op_gated_mlp(int32_t dtype, const void* x, int64_t ldx, const void* w_in, int64_t ldw_in, const void* b_in,
+                     const void* w_out, int64_t ldw_out, const void* b_out, void* hidden, int64_t ldh, void* pre,
+                     int64_t ldp, void* out, int64_t ldo, int64_t M, int64_t N, int64_t K, int64_t D, int32_t gate,
+                     int32_t flags, void* stream);
+
+/* Gradient of epd_op_gated_mlp: from dout[M,D], x, the weights, and hidden and pre as the forward call left them,
+ *   dx[M,K], dw_in[2N,K], db_in[2N], dw_out[D,N], db_out[D]   (any may be NULL: not formed),
+ * each overwritten, element type per dtype.  In bf16 the gradient with respect to pre is rounded to bf16 between the
+ * products.  workspace: device memory, 256-byte aligned, epd_gated_mlp_backward_workspace_bytes() bytes, free again
+ * once the call's work has run; calls that may overlap on the device need one each.  The same inputs give the same bits on
+ * every call (no atomics).  M == 0 zeroes dw_in, db_in, dw_out and db_out. */
+size_t epd_gated_mlp_backward_workspace_bytes(int32_t dtype, int64_t M, int64_t N, int64_t D);
+int epd_op_gated_mlp_backward(int32_t dtype, const void* dout, int64_t lddo, const void* x, int64_t ldx, const void* w_in,
+                              int64_t ldw_in, const void* w_out, int64_t ldw_out, const void* hidden, int64_t ldh,
+                              const void* pre, int64_t ldp, void* dx, int64_t lddx, void* dw_in, int64_t lddw_in,
+                              void* db_in, void* dw_out, int64_t lddw_out, void* db_out, void* workspace,
+                              size_t workspace_bytes, int64_t M, int64_t N, int64_t K, int64_t D, int32_t gate,
+                              void* stream);
+
+/* Gradient of a linear layer out[M,N] = x[M,K] . w[N,K]^T + bias (epd_op_linear without activation):
+ *   dx[M,K] = dout . w,  dw[N,K] = dout^T . x,  db[N] = column sums of dout   (any may be NULL),
+ * overwritten, element type per dtype.  workspace (needed for db only) as above. */
+size_t epd_linear_backward_workspace_bytes(int32_t dtype, int64_t M, int64_t N);
+int epd_op_linear_backward(int32_t dtype, const void* dout, int64_t lddo, const void* x, int64_t ldx, const void* w,
+                           int64_t ldw, void* dx, int64_t lddx, void* dw, int64_t lddw, void* db, void* workspace,
+                           size_t workspace_bytes, int64_t M, int64_t N, int64_t K, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Rotary embedding with several position axes (time, row, column of images and clips)
+ * ---------------------------------------------------------------------------------------- */
+
+/* Which head dimensions pair up, and which axis and frequency turn a pair.  sections (HOST, n_axes entries, 1 to 4
+ * axes): rotation pairs per axis; R = their sum, 2R <= head_dim; dimensions from 2R on are not rotated.
+ *   BLOCKS       axis a owns 2*sections[a] consecutive dimensions; inside them pair f is (f, f + sections[a]) and turns
+ *                by pos[a] * theta^(-f/sections[a]).  Two axes of head_dim/4 pairs each are epd_op_rope_split's form.
+ *   SECTIONS     pair i is (i, i + R) and turns by pos[a(i)] * theta^(-i/R); the first sections[0] pairs belong to
+ *                axis 0, the next sections[1] to axis 1, and so on.
+ *   INTERLEAVED  as SECTIONS, but the axes take the pairs in turns, an axis whose section is used up being passed over.
+ * theta <= 0 turns nothing.  Positions are int32, any value; angles are formed in double precision. */
+enum { EPD_ROPE_BLOCKS = 0, EPD_ROPE_SECTIONS = 1, EPD_ROPE_INTERLEAVED = 2 };
+
+/* Rotates x [T, heads, head_dim] (element (t, h, d) at t*x_token_stride + h*x_head_stride + d) by the tokens'
+ * positions, times `scale` (all dimensions), into out (its own strides; out may be x with the same strides, and must not
+ * overlap it otherwise).  pos device int32, axis a of token t at a*pos_stride + t, pos_stride >= T.  inverse != 0
+ * rotates the other way: the gradient of the call.  Any strides whose rows do not run into one another; heads of a
+ * packed projection row and key / value heads fewer than query heads need no copy.  head_dim <= 128, heads <= 65535. */
+int epd_op_rope_axes(int32_t dtype, const void* x, int64_t x_token_stride, int64_t x_head_stride, const int32_t* pos,
+                     int64_t pos_stride, void* out, int64_t out_token_stride, int64_t out_head_stride, int64_t T,
+                     int32_t heads, int32_t head_dim, const int32_t* sections, int32_t n_axes, int32_t layout,
+                     float theta, float scale, int32_t inverse, void* stream);
+
+/* epd_op_rope_split with several axes: qkv [T, ldqkv >= 3*heads*head_dim] -> q, k, v [heads, T, head_dim_padded],
+ * padding as epd_op_rope_split writes it, ready for epd_op_attention; q additionally multiplied by q_scale. */
+int epd_op_rope_axes_split(int32_t dtype, const void* qkv, int64_t ldqkv, const int32_t* pos, int64_t pos_stride, void* q,
+                           void* k, void* v, int64_t T, int32_t heads, int32_t head_dim, const int32_t* sections,
+                           int32_t n_axes, int32_t layout, float theta, float q_scale, void* stream);
+
+/* Its gradient: dq, dk, dv [heads, T, head_dim_padded] (padding columns are not read) -> dqkv [T, lddqkv], of which
+ * the first 3*heads*head_dim columns are written. */
+int epd_op_rope_axes_split_backward(int32_t dtype, const void* dq, const void* dk, const void* dv, const int32_t* pos,
+                                    int64_t pos_stride, void* dqkv, int64_t lddqkv, int64_t T, int32_t heads,
+                                    int32_t head_dim, const int32_t* sections, int32_t n_axes, int32_t layout,
+                                    float theta, float q_scale, void* stream);
+
+/* ------------------------------------------------------------------------------------------
  * After the stage: feature keys and a feature cache (the encoder's side of the multimodal store of
  * Section 3.2, "Asynchronous Feature Prefetching": features are kept under a hash of the input so
  * that a repeated input is not encoded again and only the key travels with the request)

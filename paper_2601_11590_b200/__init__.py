@@ -7,6 +7,7 @@ an op requires the compiled library and a CUDA device.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Dict, List, Optional, Sequence
@@ -23,6 +24,8 @@ FRAMES_U8, FRAMES_BF16 = 0, 1
 ATTENTION_FORCE_FMA = 1
 ATTENTION_SPLIT_KEYS = 2
 ATTENTION_TWO_QUERY_TILES = 4
+GATE_SILU, GATE_GELU_TANH, GATE_GELU_ERF = 0, 1, 2
+ROPE_BLOCKS, ROPE_SECTIONS, ROPE_INTERLEAVED = 0, 1, 2
 
 EXPORTED_SYMBOLS = [
     "epd_encoder_workspace_bytes", "epd_encoder_create", "epd_encode", "epd_encode_host",
@@ -38,6 +41,9 @@ EXPORTED_SYMBOLS = [
     "epd_feature_cache_lookup", "epd_feature_cache_insert", "epd_feature_cache_stats",
     "epd_encode_frames_cached", "epd_debug_set_wait_limit", "epd_encode_frames_fmt", "epd_op_patchify_fmt",
     "epd_op_quantize_e4m3", "epd_op_linear_e4m3",
+    "epd_op_gated_linear", "epd_op_gated_mlp", "epd_op_gated_mlp_backward", "epd_gated_mlp_backward_workspace_bytes",
+    "epd_op_linear_backward", "epd_linear_backward_workspace_bytes", "epd_op_rope_axes", "epd_op_rope_axes_split",
+    "epd_op_rope_axes_split_backward",
 ]
 
 
@@ -187,6 +193,29 @@ def load_library() -> ctypes.CDLL:
     lib.epd_op_rope_attention_static.argtypes = [i32, vp, vp, vp, vp, i32p, i32, vp, i64, i32, i32, f32, vp]
     lib.epd_static_scratch_bytes.restype = ctypes.c_size_t
     lib.epd_static_scratch_bytes.argtypes = []
+    lib.epd_op_gated_linear.restype = ctypes.c_int
+    lib.epd_op_gated_linear.argtypes = [i32, vp, i64, vp, i64, vp, vp, i64, vp, i64, i64, i64, i64, i32, vp]
+    lib.epd_op_gated_mlp.restype = ctypes.c_int
+    lib.epd_op_gated_mlp.argtypes = [i32, vp, i64, vp, i64, vp, vp, i64, vp, vp, i64, vp, i64, vp, i64, i64, i64, i64, i64,
+                                     i32, i32, vp]
+    lib.epd_gated_mlp_backward_workspace_bytes.restype = ctypes.c_size_t
+    lib.epd_gated_mlp_backward_workspace_bytes.argtypes = [i32, i64, i64, i64]
+    lib.epd_op_gated_mlp_backward.restype = ctypes.c_int
+    lib.epd_op_gated_mlp_backward.argtypes = [i32, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64,
+                                              vp, vp, i64, vp, vp, ctypes.c_size_t, i64, i64, i64, i64, i32, vp]
+    lib.epd_linear_backward_workspace_bytes.restype = ctypes.c_size_t
+    lib.epd_linear_backward_workspace_bytes.argtypes = [i32, i64, i64]
+    lib.epd_op_linear_backward.restype = ctypes.c_int
+    lib.epd_op_linear_backward.argtypes = [i32, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, ctypes.c_size_t, i64,
+                                           i64, i64, vp]
+    lib.epd_op_rope_axes.restype = ctypes.c_int
+    lib.epd_op_rope_axes.argtypes = [i32, vp, i64, i64, vp, i64, vp, i64, i64, i64, i32, i32, i32p, i32, i32, f32, f32,
+                                     i32, vp]
+    lib.epd_op_rope_axes_split.restype = ctypes.c_int
+    lib.epd_op_rope_axes_split.argtypes = [i32, vp, i64, vp, i64, vp, vp, vp, i64, i32, i32, i32p, i32, i32, f32, f32, vp]
+    lib.epd_op_rope_axes_split_backward.restype = ctypes.c_int
+    lib.epd_op_rope_axes_split_backward.argtypes = [i32, vp, vp, vp, vp, i64, vp, i64, i64, i32, i32, i32p, i32, i32, f32,
+                                                    f32, vp]
     _lib = lib
     return lib
 
@@ -594,6 +623,217 @@ def op_qkv_rope(x, w, bias, pos_row, pos_col, heads, head_dim, theta, q_scale, t
                                table_rows, _ptr(q), _ptr(k), _ptr(v), T, heads, head_dim, q_scale, sp),
            "epd_op_qkv_rope")
     return q, k, v
+
+
+# ---- gated feed-forward block, gradients ------------------------------------------------------------
+
+def _op_context(dtype, named, stream):
+    """Checks the tensors of one call (name -> (tensor or None, shape)): on one CUDA device, of the call's element type,
+    rows contiguous.  Returns (torch, element type, device context, stream pointer); the launch belongs on the tensors'
+    device, whichever is current."""
+    import torch
+    if dtype != DTYPE_F32 and dtype != DTYPE_BF16:
+        raise EpdError(EPD_EINVAL, "dtype")
+    want = torch.float32 if dtype == DTYPE_F32 else torch.bfloat16
+    device = None
+    for name, (t, shape) in named.items():
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError(f"{name}: not a CUDA tensor (there is no CPU path)")
+        device = t.device if device is None else device
+        if t.device != device:
+            raise ValueError(f"{name}: on {t.device}, the other tensors on {device}")
+        if t.dtype != want:
+            raise ValueError(f"{name}: {t.dtype}, expected {want}")
+        if tuple(t.shape) != shape:
+            raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {shape}")
+        if t.stride(-1) != 1 and t.shape[-1] > 1:
+            raise ValueError(f"{name}: the last dimension must be contiguous")
+    here = torch.cuda.current_device() == device.index
+    if stream is None:
+        stream = torch.cuda.current_stream(device)
+    elif stream.device != device:
+        raise ValueError(f"stream on {stream.device}, tensors on {device}")
+    return torch, want, (contextlib.nullcontext() if here else torch.cuda.device(device)), stream.cuda_stream
+
+
+def _ld(t, cols) -> int:
+    """Leading dimension of a matrix; one row may have any stride."""
+    return cols if t is None or t.shape[0] <= 1 else t.stride(0)
+
+
+def _out_tensor(name, t, shape, dtype, device):
+    if t.dtype != dtype or tuple(t.shape) != shape or t.device != device or (t.stride(-1) != 1 and shape[-1] > 1):
+        raise ValueError(f"{name}: expected {dtype} {shape} on {device}, rows contiguous")
+    return t
+
+
+def op_gated_linear(dtype, x, w, bias, gate, out=None, pre=None, stream=None):
+    """act(x . w[:N]^T + bias[:N]) * (x . w[N:]^T + bias[N:]) for w [2N, K]; `pre` [M, 2N] receives both projections."""
+    M, K = x.shape
+    N = w.shape[0] // 2
+    torch, want, device, sp = _op_context(dtype, {"x": (x, (M, K)), "w": (w, (2 * N, K)), "bias": (bias, (2 * N,)),
+                                                  "out": (out, (M, N)), "pre": (pre, (M, 2 * N))}, stream)
+    if out is None:
+        out = torch.empty((M, N), dtype=want, device=x.device)
+    with device:
+        _check(load_library().epd_op_gated_linear(dtype, _ptr(x), _ld(x, K), _ptr(w), _ld(w, K), _ptr(bias), _ptr(out),
+                                                  _ld(out, N), _ptr(pre), _ld(pre, 2 * N), M, N, K, gate, sp),
+               "epd_op_gated_linear")
+    return out
+
+
+def op_gated_mlp(dtype, x, w_in, b_in, w_out, b_out, gate, out=None, hidden=None, pre=None, save=False, flags=0,
+                 stream=None):
+    """The gated feed-forward block (epd_op_gated_mlp).  Returns out, or with save=True (out, hidden, pre), which
+    op_gated_mlp_backward takes.  flags: LINEAR_ACCUMULATE adds into a float `out` (which has to be given)."""
+    M, K = x.shape
+    N, D = w_in.shape[0] // 2, w_out.shape[0]
+    torch, want, device, sp = _op_context(
+        dtype, {"x": (x, (M, K)), "w_in": (w_in, (2 * N, K)), "b_in": (b_in, (2 * N,)), "w_out": (w_out, (D, N)),
+                "b_out": (b_out, (D,)), "hidden": (hidden, (M, N)), "pre": (pre, (M, 2 * N))}, stream)
+    out_type = torch.float32 if flags & (LINEAR_ACCUMULATE | LINEAR_OUT_F32) else want
+    if out is None:
+        if flags & LINEAR_ACCUMULATE:
+            raise ValueError("LINEAR_ACCUMULATE adds into `out`: give one")
+        out = torch.empty((M, D), dtype=out_type, device=x.device)
+    else:
+        _out_tensor("out", out, (M, D), out_type, x.device)
+    if hidden is None:
+        hidden = torch.empty((M, N), dtype=want, device=x.device)
+    if pre is None and save:
+        pre = torch.empty((M, 2 * N), dtype=want, device=x.device)
+    with device:
+        _check(load_library().epd_op_gated_mlp(
+            dtype, _ptr(x), _ld(x, K), _ptr(w_in), _ld(w_in, K), _ptr(b_in), _ptr(w_out), _ld(w_out, N), _ptr(b_out),
+            _ptr(hidden), _ld(hidden, N), _ptr(pre), _ld(pre, 2 * N), _ptr(out), _ld(out, D), M, N, K, D, gate, flags, sp),
+            "epd_op_gated_mlp")
+    return (out, hidden, pre) if save else out
+
+
+def op_gated_mlp_backward(dtype, dout, x, w_in, w_out, hidden, pre, gate, bias=True, need_dx=True, need_dw=True,
+                          workspace=None, stream=None) -> Dict:
+    """Gradients of op_gated_mlp: {"dx", "dw_in", "dw_out", "db_in", "db_out"} (those asked for)."""
+    M, K = x.shape
+    N, D = w_in.shape[0] // 2, w_out.shape[0]
+    torch, want, device, sp = _op_context(
+        dtype, {"dout": (dout, (M, D)), "x": (x, (M, K)), "w_in": (w_in, (2 * N, K)), "w_out": (w_out, (D, N)),
+                "hidden": (hidden, (M, N)), "pre": (pre, (M, 2 * N))}, stream)
+    g = {}
+    if need_dx:
+        g["dx"] = torch.empty((M, K), dtype=want, device=x.device)
+    if need_dw:
+        g["dw_in"] = torch.empty((2 * N, K), dtype=want, device=x.device)
+        g["dw_out"] = torch.empty((D, N), dtype=want, device=x.device)
+    if bias:
+        g["db_in"] = torch.empty(2 * N, dtype=want, device=x.device)
+        g["db_out"] = torch.empty(D, dtype=want, device=x.device)
+    lib = load_library()
+    nbytes = lib.epd_gated_mlp_backward_workspace_bytes(dtype, M, N, D)
+    workspace = _workspace(torch, workspace, nbytes, x.device)
+    with device:
+        _check(lib.epd_op_gated_mlp_backward(
+            dtype, _ptr(dout), _ld(dout, D), _ptr(x), _ld(x, K), _ptr(w_in), _ld(w_in, K), _ptr(w_out), _ld(w_out, N),
+            _ptr(hidden), _ld(hidden, N), _ptr(pre), _ld(pre, 2 * N), _ptr(g.get("dx")), K, _ptr(g.get("dw_in")), K,
+            _ptr(g.get("db_in")), _ptr(g.get("dw_out")), N, _ptr(g.get("db_out")), _ptr(workspace),
+            workspace.numel() * workspace.element_size(), M, N, K, D, gate, sp), "epd_op_gated_mlp_backward")
+    return g
+
+
+def _workspace(torch, given, nbytes, device):
+    if given is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    if given.device != device or not given.is_contiguous():
+        raise ValueError(f"workspace: expected contiguous memory on {device}")
+    return given
+
+
+def op_linear_backward(dtype, dout, x, w, bias=True, need_dx=True, need_dw=True, workspace=None, stream=None) -> Dict:
+    """Gradients of a linear layer x . w^T + bias: {"dx", "dw", "db"} (those asked for)."""
+    M, K = x.shape
+    N = w.shape[0]
+    torch, want, device, sp = _op_context(dtype, {"dout": (dout, (M, N)), "x": (x, (M, K)), "w": (w, (N, K))}, stream)
+    g = {}
+    if need_dx:
+        g["dx"] = torch.empty((M, K), dtype=want, device=x.device)
+    if need_dw:
+        g["dw"] = torch.empty((N, K), dtype=want, device=x.device)
+    if bias:
+        g["db"] = torch.empty(N, dtype=want, device=x.device)
+    lib = load_library()
+    workspace = _workspace(torch, workspace, lib.epd_linear_backward_workspace_bytes(dtype, M, N), x.device)
+    with device:
+        _check(lib.epd_op_linear_backward(
+            dtype, _ptr(dout), _ld(dout, N), _ptr(x), _ld(x, K), _ptr(w), _ld(w, K), _ptr(g.get("dx")), K,
+            _ptr(g.get("dw")), K, _ptr(g.get("db")), _ptr(workspace), workspace.numel() * workspace.element_size(), M, N,
+            K, sp), "epd_op_linear_backward")
+    return g
+
+
+# ---- rotary embedding with several axes ---------------------------------------------------------------
+
+def _check_positions(pos, T, n_axes, device) -> int:
+    import torch
+    if pos.dtype != torch.int32 or tuple(pos.shape) != (n_axes, T) or pos.device != device or \
+            (T > 1 and pos.stride(1) != 1):
+        raise ValueError(f"pos: expected int32 {(n_axes, T)} on {device}, each axis contiguous")
+    return max(T, pos.stride(0)) if n_axes > 1 else T
+
+
+def op_rope_axes(dtype, x, pos, sections, layout, theta, scale=1.0, inverse=False, out=None, stream=None):
+    """Rotates x [T, heads, head_dim] (any token and head strides) by int32 positions pos [axes, T]; `out` may be x."""
+    T, heads, dh = x.shape
+    torch, want, device, sp = _op_context(dtype, {"x": (x, (T, heads, dh)), "out": (out, (T, heads, dh))}, stream)
+    n = len(sections)
+    ps = _check_positions(pos, T, n, x.device)
+    if out is None:
+        out = torch.empty((T, heads, dh), dtype=want, device=x.device)
+
+    def strides(t):                     # one token or one head may have any stride
+        head = t.stride(1) if heads > 1 else dh
+        return (t.stride(0) if T > 1 else 0), head
+    (xt, xh), (ot, oh) = strides(x), strides(out)
+    with device:
+        _check(load_library().epd_op_rope_axes(dtype, _ptr(x), xt, xh, _ptr(pos), ps, _ptr(out), ot, oh, T, heads, dh,
+                                               (ctypes.c_int32 * n)(*sections), n, layout, theta, scale, int(inverse),
+                                               sp), "epd_op_rope_axes")
+    return out
+
+
+def op_rope_axes_split(dtype, qkv, pos, heads, head_dim, sections, layout, theta, q_scale, stream=None):
+    """Packed qkv [T, 3*heads*head_dim] -> rotated head-major padded q, k, v, ready for op_attention."""
+    T = qkv.shape[0]
+    torch, want, device, sp = _op_context(dtype, {"qkv": (qkv, (T, 3 * heads * head_dim))}, stream)
+    n = len(sections)
+    ps = _check_positions(pos, T, n, qkv.device)
+    dhp = (head_dim + 15) // 16 * 16
+    q, k, v = (torch.empty((heads, T, dhp), dtype=want, device=qkv.device) for _ in range(3))
+    with device:
+        _check(load_library().epd_op_rope_axes_split(
+            dtype, _ptr(qkv), _ld(qkv, 3 * heads * head_dim), _ptr(pos), ps, _ptr(q), _ptr(k), _ptr(v), T, heads, head_dim,
+            (ctypes.c_int32 * n)(*sections), n, layout, theta, q_scale, sp), "epd_op_rope_axes_split")
+    return q, k, v
+
+
+def op_rope_axes_split_backward(dtype, dq, dk, dv, pos, head_dim, sections, layout, theta, q_scale, stream=None):
+    """Gradient of op_rope_axes_split: dq, dk, dv [heads, T, padded] -> dqkv [T, 3*heads*head_dim]."""
+    heads, T, dhp = dq.shape
+    if dhp != (head_dim + 15) // 16 * 16:
+        raise ValueError(f"head width {dhp} is not the padded width of head_dim {head_dim}")
+    torch, want, device, sp = _op_context(dtype, {n: (t, (heads, T, dhp)) for n, t in
+                                                  (("dq", dq), ("dk", dk), ("dv", dv))}, stream)
+    for t in (dq, dk, dv):
+        if not t.is_contiguous():
+            raise ValueError("dq, dk, dv must be contiguous")
+    n = len(sections)
+    ps = _check_positions(pos, T, n, dq.device)
+    dqkv = torch.empty((T, 3 * heads * head_dim), dtype=want, device=dq.device)
+    with device:
+        _check(load_library().epd_op_rope_axes_split_backward(
+            dtype, _ptr(dq), _ptr(dk), _ptr(dv), _ptr(pos), ps, _ptr(dqkv), 3 * heads * head_dim, T, heads, head_dim,
+            (ctypes.c_int32 * n)(*sections), n, layout, theta, q_scale, sp), "epd_op_rope_axes_split_backward")
+    return dqkv
 
 
 def set_wait_limit(cycles: int) -> None:

@@ -73,6 +73,9 @@ inline int limited_sms(int device_sms) {
   return (lim > 0 && lim < device_sms) ? lim : device_sms;
 }
 
+// Records the CUDA error behind an EPD_ECUDA return for epd_last_cuda_error() (encoder.cu).
+void note_cuda_error(cudaError_t e);
+
 // ---- plain-FMA kernels (kernels_fma.cu) -----------------------------------------------------
 cudaError_t linear_fma(int dtype, const void* x, int64_t ldx, const void* w, int64_t ldw, const void* bias,
                        void* out, int64_t ldo, int64_t M, int64_t N, int64_t K, int flags, cudaStream_t s);

@@ -146,6 +146,12 @@ namespace {
 // The CUDA error behind the most recent EPD_ECUDA of this thread (see epd_last_cuda_error()).
 thread_local cudaError_t g_last_cuda_error = cudaSuccess;
 
+}  // namespace
+
+void epd::note_cuda_error(cudaError_t e) { g_last_cuda_error = e; }
+
+namespace {
+
 #define EPD_CUDA(expr)                        \
   do {                                        \
     cudaError_t e__ = (expr);                 \

@@ -1,0 +1,371 @@
+// Gated feed-forward block and its gradient, and the gradient of a linear layer: host side, and the plain-FMA kernels
+// (the float path, and bf16 shapes the tensor-core kernels do not take).
+//
+//   g = x Wg^T + bg,  u = x Wu^T + bu,  a = act(g) u,  y = a Wo^T + bo       (Wg over Wu: one [2N, K] matrix)
+//   da = dy Wo,  dg = da u act'(g),  du = da act(g),
+//   dx = [dg|du] W,  dW = [dg|du]^T x,  db = sum over rows of [dg|du],  dWo = dy^T a,  dbo = sum over rows of dy
+#include "gated.cuh"
+
+namespace epd {
+namespace {
+
+// =============================================================================================
+// Matrix product with plain FMAs: out[m, n] = sum_k A(m, k) B(n, k), every operand either contraction-contiguous
+// ("K-major": element (r, k) at r * ld + k) or row-contiguous ("MN-major": at k * ld + r).  128 x 128 tile,
+// 256 threads with 8 x 8 outputs each (two groups of 4 rows by two groups of 4 columns), the next block of the
+// contraction fetched into registers while the present one is multiplied.
+// =============================================================================================
+constexpr int FT = 128, FK = 8;
+
+enum { EPI_PLAIN = 0, EPI_GATE = 1, EPI_GATE_GRAD = 2 };
+
+struct FmaArgs {
+  const void *a, *b, *bias;
+  int64_t lda, ldb;
+  int64_t M, N, K;
+  void* out;                 // PLAIN: [M, N]; GATE: a [M, N]; GATE_GRAD: unused
+  int64_t ldo;
+  void* pre;                 // GATE: g|u [M, 2N] to write, or NULL; GATE_GRAD: g|u to read
+  int64_t ldp;
+  void* dpre;                // GATE_GRAD: dg|du [M, 2N]
+  int64_t lddp;
+  int gate;
+};
+
+template <typename T, bool A_MN, bool B_MN, int EPI>
+__global__ void __launch_bounds__(256)
+matmul_fma_kernel(const FmaArgs p) {
+  __shared__ float sa[FK][FT + 4];
+  __shared__ float sb[FK][FT + 4];
+  constexpr int COLS = EPI == EPI_GATE ? FT / 2 : FT;     // output columns of a tile
+  const T* A = static_cast<const T*>(p.a);
+  const T* B = static_cast<const T*>(p.b);
+  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
+  const int64_t m0 = (int64_t)blockIdx.x * FT, n0 = (int64_t)blockIdx.y * COLS;
+  float ra[4], rb[4];
+  auto fetch = [&](int64_t k0) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int e = threadIdx.x + 256 * i;
+      {
+        const int r = A_MN ? e % FT : e / FK, kk = A_MN ? e / FT : e % FK;
+        const int64_t m = m0 + r, k = k0 + kk;
+        ra[i] = (m < p.M && k < p.K) ? to_float<T>(A_MN ? A[k * p.lda + m] : A[m * p.lda + k]) : 0.0f;
+      }
+      {
+        const int r = B_MN ? e % FT : e / FK, kk = B_MN ? e / FT : e % FK;
+        // gated: the tile's second half of columns is the up projection of the first half's
+        const int64_t c = n0 + (EPI == EPI_GATE ? r % COLS : r), k = k0 + kk;
+        const int64_t n = EPI == EPI_GATE && r >= COLS ? p.N + c : c;
+        rb[i] = (c < p.N && k < p.K) ? to_float<T>(B_MN ? B[k * p.ldb + n] : B[n * p.ldb + k]) : 0.0f;
+      }
+    }
+  };
+  auto put = [&] {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int e = threadIdx.x + 256 * i;
+      sa[A_MN ? e / FT : e % FK][A_MN ? e % FT : e / FK] = ra[i];
+      sb[B_MN ? e / FT : e % FK][B_MN ? e % FT : e / FK] = rb[i];
+    }
+  };
+  float acc[8][8] = {};
+  fetch(0);
+  for (int64_t k0 = 0; k0 < p.K; k0 += FK) {
+    put();
+    __syncthreads();
+    if (k0 + FK < p.K) fetch(k0 + FK);
+#pragma unroll
+    for (int kk = 0; kk < FK; ++kk) {
+      float a[8], b[8];
+      *reinterpret_cast<float4*>(a) = *reinterpret_cast<const float4*>(&sa[kk][ty * 4]);
+      *reinterpret_cast<float4*>(a + 4) = *reinterpret_cast<const float4*>(&sa[kk][64 + ty * 4]);
+      *reinterpret_cast<float4*>(b) = *reinterpret_cast<const float4*>(&sb[kk][tx * 4]);
+      *reinterpret_cast<float4*>(b + 4) = *reinterpret_cast<const float4*>(&sb[kk][64 + tx * 4]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[i][j] = fmaf(a[i], b[j], acc[i][j]);
+    }
+    __syncthreads();
+  }
+  const T* bias = static_cast<const T*>(p.bias);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int64_t m = m0 + (i < 4 ? ty * 4 + i : 64 + ty * 4 + i - 4);
+    if (m >= p.M) continue;
+#pragma unroll
+    for (int j = 0; j < (EPI == EPI_GATE ? 4 : 8); ++j) {
+      const int64_t n = n0 + (j < 4 ? tx * 4 + j : 64 + tx * 4 + j - 4);
+      if (n >= p.N) continue;
+      if constexpr (EPI == EPI_PLAIN) {
+        static_cast<T*>(p.out)[m * p.ldo + n] = from_float<T>(acc[i][j] + (bias ? to_float<T>(bias[n]) : 0.0f));
+      } else if constexpr (EPI == EPI_GATE) {
+        const float g = acc[i][j] + (bias ? to_float<T>(bias[n]) : 0.0f);
+        const float u = acc[i][j + 4] + (bias ? to_float<T>(bias[p.N + n]) : 0.0f);
+        static_cast<T*>(p.out)[m * p.ldo + n] = from_float<T>(gate_act(p.gate, g) * u);
+        if (p.pre) {
+          static_cast<T*>(p.pre)[m * p.ldp + n] = from_float<T>(g);
+          static_cast<T*>(p.pre)[m * p.ldp + p.N + n] = from_float<T>(u);
+        }
+      } else {
+        const float g = to_float<T>(static_cast<const T*>(p.pre)[m * p.ldp + n]);
+        const float u = to_float<T>(static_cast<const T*>(p.pre)[m * p.ldp + p.N + n]);
+        float act, slope;
+        gate_act_slope(p.gate, g, &act, &slope);
+        static_cast<T*>(p.dpre)[m * p.lddp + n] = from_float<T>(acc[i][j] * u * slope);
+        static_cast<T*>(p.dpre)[m * p.lddp + p.N + n] = from_float<T>(acc[i][j] * act);
+      }
+    }
+  }
+}
+
+template <typename T, bool A_MN, bool B_MN, int EPI>
+cudaError_t matmul_fma_t(const FmaArgs& p, cudaStream_t s) {
+  const int64_t cols = EPI == EPI_GATE ? FT / 2 : FT;
+  const int64_t gx = (p.M + FT - 1) / FT, gy = (p.N + cols - 1) / cols;
+  if (gx > 0x7fffffff || gy > 65535) return cudaErrorInvalidValue;
+  matmul_fma_kernel<T, A_MN, B_MN, EPI><<<dim3((unsigned)gx, (unsigned)gy), 256, 0, s>>>(p);
+  return cudaGetLastError();
+}
+template <bool A_MN, bool B_MN, int EPI>
+cudaError_t matmul_fma(int dtype, const FmaArgs& p, cudaStream_t s) {
+  return dtype == EPD_DTYPE_F32 ? matmul_fma_t<float, A_MN, B_MN, EPI>(p, s)
+                                : matmul_fma_t<__nv_bfloat16, A_MN, B_MN, EPI>(p, s);
+}
+
+// =============================================================================================
+// Column sums out[n] = sum_m x[m, n] in two launches, the same order of additions on every call: each block adds
+// kSumRows rows of 256 columns into a float partial sum, the second launch adds the partial sums.
+// =============================================================================================
+constexpr int kSumRows = 128;
+
+template <typename T>
+__global__ void __launch_bounds__(256)
+column_sum_partial_kernel(const T* __restrict__ x, int64_t ldx, int64_t M, int64_t N, float* __restrict__ part) {
+  const int64_t n = (int64_t)blockIdx.y * 256 + threadIdx.x;
+  if (n >= N) return;
+  const int64_t m0 = (int64_t)blockIdx.x * kSumRows, m1 = min(M, m0 + kSumRows);
+  float s = 0.0f;
+  for (int64_t m = m0; m < m1; ++m) s += to_float<T>(x[m * ldx + n]);
+  part[(int64_t)blockIdx.x * N + n] = s;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256)
+column_sum_final_kernel(const float* __restrict__ part, int64_t blocks, int64_t N, T* __restrict__ out) {
+  const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (n >= N) return;
+  float s = 0.0f;
+  for (int64_t b = 0; b < blocks; ++b) s += part[b * N + n];
+  out[n] = from_float<T>(s);
+}
+
+size_t align256(size_t v) { return (v + 255) / 256 * 256; }
+size_t column_sum_bytes(int64_t M, int64_t N) { return align256((size_t)((M + kSumRows - 1) / kSumRows) * N * 4); }
+
+template <typename T>
+cudaError_t column_sum_t(const void* x, int64_t ldx, int64_t M, int64_t N, void* out, float* part, cudaStream_t s) {
+  const int64_t blocks = (M + kSumRows - 1) / kSumRows;
+  if ((N + 255) / 256 > 65535) return cudaErrorInvalidValue;
+  column_sum_partial_kernel<T><<<dim3((unsigned)blocks, (unsigned)((N + 255) / 256)), 256, 0, s>>>(
+      static_cast<const T*>(x), ldx, M, N, part);
+  column_sum_final_kernel<T><<<(unsigned)((N + 255) / 256), 256, 0, s>>>(part, blocks, N, static_cast<T*>(out));
+  return cudaGetLastError();
+}
+cudaError_t column_sum(int dtype, const void* x, int64_t ldx, int64_t M, int64_t N, void* out, float* part,
+                       cudaStream_t s) {
+  return dtype == EPD_DTYPE_F32 ? column_sum_t<float>(x, ldx, M, N, out, part, s)
+                                : column_sum_t<__nv_bfloat16>(x, ldx, M, N, out, part, s);
+}
+
+// =============================================================================================
+// The products of the block, each on the kernel that takes its shape
+// =============================================================================================
+cudaError_t gated_linear(int dtype, const void* x, int64_t ldx, const void* w, int64_t ldw, const void* bias, void* out,
+                         int64_t ldo, void* pre, int64_t ldp, int64_t M, int64_t N, int64_t K, int gate, cudaStream_t s) {
+  FmaArgs p = {};
+  p.a = x; p.lda = ldx;
+  p.b = w; p.ldb = ldw;
+  p.bias = bias;
+  p.out = out; p.ldo = ldo;
+  p.pre = pre; p.ldp = ldp;
+  p.M = M; p.N = N; p.K = K;
+  p.gate = gate;
+  return matmul_fma<false, false, EPI_GATE>(dtype, p, s);
+}
+
+// dpre[M, 2N] from dout[M, D], w_out[D, N] and pre[M, 2N]
+cudaError_t gate_gradient(int dtype, const void* dout, int64_t lddo, const void* w_out, int64_t ldw, const void* pre,
+                          int64_t ldp, void* dpre, int64_t lddp, int64_t M, int64_t N, int64_t D, int gate,
+                          cudaStream_t s) {
+  FmaArgs p = {};
+  p.a = dout; p.lda = lddo;
+  p.b = w_out; p.ldb = ldw;
+  p.pre = const_cast<void*>(pre); p.ldp = ldp;
+  p.dpre = dpre; p.lddp = lddp;
+  p.M = M; p.N = N; p.K = D;
+  p.gate = gate;
+  return matmul_fma<false, true, EPI_GATE_GRAD>(dtype, p, s);
+}
+
+// dx[M, K] = dout[M, N] . w[N, K]
+cudaError_t input_gradient(int dtype, const void* dout, int64_t lddo, const void* w, int64_t ldw, void* dx, int64_t lddx,
+                           int64_t M, int64_t N, int64_t K, cudaStream_t s) {
+  FmaArgs p = {};
+  p.a = dout; p.lda = lddo;
+  p.b = w; p.ldb = ldw;
+  p.out = dx; p.ldo = lddx;
+  p.M = M; p.N = K; p.K = N;
+  return matmul_fma<false, true, EPI_PLAIN>(dtype, p, s);
+}
+
+// dw[N, K] = dout[M, N]^T . x[M, K]
+cudaError_t weight_gradient(int dtype, const void* dout, int64_t lddo, const void* x, int64_t ldx, void* dw, int64_t lddw,
+                            int64_t M, int64_t N, int64_t K, cudaStream_t s) {
+  FmaArgs p = {};
+  p.a = dout; p.lda = lddo;
+  p.b = x; p.ldb = ldx;
+  p.out = dw; p.ldo = lddw;
+  p.M = N; p.N = K; p.K = M;
+  return matmul_fma<true, true, EPI_PLAIN>(dtype, p, s);
+}
+
+int finish(cudaError_t e) {
+  if (e == cudaSuccess) return EPD_OK;
+  note_cuda_error(e);
+  return EPD_ECUDA;
+}
+#define EPD_TRY(expr)                          \
+  do {                                         \
+    cudaError_t e__ = (expr);                  \
+    if (e__ != cudaSuccess) return finish(e__); \
+  } while (0)
+
+bool extent_ok(int64_t v) { return v >= 1 && v <= (1 << 28); }
+bool dtype_ok(int32_t dtype) { return dtype == EPD_DTYPE_F32 || dtype == EPD_DTYPE_BF16; }
+bool gate_ok(int32_t gate) { return gate == EPD_GATE_SILU || gate == EPD_GATE_GELU_TANH || gate == EPD_GATE_GELU_ERF; }
+// Every pointer a multiple of the element size (NULL is).
+template <typename... P>
+bool aligned_to(size_t es, P... ptr) {
+  return ((... | (uintptr_t)ptr) % es) == 0;
+}
+cudaError_t zero_rows(int dtype, void* p, int64_t ld, int64_t rows, int64_t cols, cudaStream_t s) {
+  if (!p) return cudaSuccess;
+  const size_t es = dtype == EPD_DTYPE_F32 ? 4 : 2;
+  return cudaMemset2DAsync(p, (size_t)ld * es, 0, (size_t)cols * es, (size_t)rows, s);
+}
+
+}  // namespace
+}  // namespace epd
+
+extern "C" {
+
+int epd_op_gated_linear(int32_t dtype, const void* x, int64_t ldx, const void* w, int64_t ldw, const void* bias, void* out,
+                        int64_t ldo, void* pre, int64_t ldp, int64_t M, int64_t N, int64_t K, int32_t gate,
+                        void* stream) {
+  using namespace epd;
+  if (!dtype_ok(dtype) || !gate_ok(gate) || M < 0 || M > (1 << 28) || !extent_ok(N) || !extent_ok(K)) return EPD_EINVAL;
+  if (ldx < K || ldw < K || ldo < N || (pre && ldp < 2 * N)) return EPD_EINVAL;
+  if (M == 0) return EPD_OK;
+  if (!x || !w || !out || !aligned_to(dtype == EPD_DTYPE_F32 ? 4 : 2, x, w, bias, out, pre)) return EPD_EINVAL;
+  return finish(gated_linear(dtype, x, ldx, w, ldw, bias, out, ldo, pre, ldp, M, N, K, gate,
+                             static_cast<cudaStream_t>(stream)));
+}
+
+int epd_op_gated_mlp(int32_t dtype, const void* x, int64_t ldx, const void* w_in, int64_t ldw_in, const void* b_in,
+                     const void* w_out, int64_t ldw_out, const void* b_out, void* hidden, int64_t ldh, void* pre,
+                     int64_t ldp, void* out, int64_t ldo, int64_t M, int64_t N, int64_t K, int64_t D, int32_t gate,
+                     int32_t flags, void* stream) {
+  using namespace epd;
+  if (!dtype_ok(dtype) || !gate_ok(gate) || M < 0 || M > (1 << 28) || !extent_ok(N) || !extent_ok(K) || !extent_ok(D))
+    return EPD_EINVAL;
+  if (flags & ~(EPD_LINEAR_ACCUMULATE | EPD_LINEAR_OUT_F32)) return EPD_EINVAL;
+  if (ldx < K || ldw_in < K || ldw_out < N || ldh < N || ldo < D || (pre && ldp < 2 * N)) return EPD_EINVAL;
+  if (M == 0) return EPD_OK;
+  const size_t es = dtype == EPD_DTYPE_F32 ? 4 : 2;
+  if (!x || !w_in || !w_out || !hidden || !out || !aligned_to(es, x, w_in, b_in, w_out, b_out, hidden, pre, out) ||
+      ((flags != 0) && !aligned_to(4, out)))
+    return EPD_EINVAL;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  EPD_TRY(gated_linear(dtype, x, ldx, w_in, ldw_in, b_in, hidden, ldh, pre, ldp, M, N, K, gate, s));
+  return epd_op_linear(dtype, hidden, ldh, w_out, ldw_out, b_out, out, ldo, M, D, N, flags, stream);
+}
+
+size_t epd_gated_mlp_backward_workspace_bytes(int32_t dtype, int64_t M, int64_t N, int64_t D) {
+  using namespace epd;
+  if (!dtype_ok(dtype) || M < 0 || M > (1 << 28) || !extent_ok(N) || !extent_ok(D)) return 0;
+  const size_t es = dtype == EPD_DTYPE_F32 ? 4 : 2;
+  return align256((size_t)M * 2 * N * es) + column_sum_bytes(M, 2 * N > D ? 2 * N : D) + 256;
+}
+
+int epd_op_gated_mlp_backward(int32_t dtype, const void* dout, int64_t lddo, const void* x, int64_t ldx, const void* w_in,
+                              int64_t ldw_in, const void* w_out, int64_t ldw_out, const void* hidden, int64_t ldh,
+                              const void* pre, int64_t ldp, void* dx, int64_t lddx, void* dw_in, int64_t lddw_in,
+                              void* db_in, void* dw_out, int64_t lddw_out, void* db_out, void* workspace,
+                              size_t workspace_bytes, int64_t M, int64_t N, int64_t K, int64_t D, int32_t gate,
+                              void* stream) {
+  using namespace epd;
+  if (!dtype_ok(dtype) || !gate_ok(gate) || M < 0 || M > (1 << 28) || !extent_ok(N) || !extent_ok(K) || !extent_ok(D))
+    return EPD_EINVAL;
+  if (lddo < D || ldx < K || ldw_in < K || ldw_out < N || ldh < N || ldp < 2 * N || (dx && lddx < K) ||
+      (dw_in && lddw_in < K) || (dw_out && lddw_out < N))
+    return EPD_EINVAL;
+  const size_t es = dtype == EPD_DTYPE_F32 ? 4 : 2;
+  if (!aligned_to(es, dout, x, w_in, w_out, hidden, pre, dx, dw_in, db_in, dw_out, db_out)) return EPD_EINVAL;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (M == 0) {      // sums over no rows
+    EPD_TRY(zero_rows(dtype, dw_in, lddw_in, 2 * N, K, s));
+    EPD_TRY(zero_rows(dtype, dw_out, lddw_out, D, N, s));
+    EPD_TRY(zero_rows(dtype, db_in, 2 * N, 1, 2 * N, s));
+    EPD_TRY(zero_rows(dtype, db_out, D, 1, D, s));
+    return EPD_OK;
+  }
+  const bool inner = dx || dw_in || db_in;        // anything in front of the product
+  if (!dout || (inner && (!pre || !w_out)) || (dx && !w_in) || (dw_in && !x) || (dw_out && !hidden)) return EPD_EINVAL;
+  if (!workspace || (uintptr_t)workspace % 256) return EPD_EINVAL;
+  if (workspace_bytes < epd_gated_mlp_backward_workspace_bytes(dtype, M, N, D)) return EPD_ENOMEM;
+  void* dpre = workspace;
+  float* part = reinterpret_cast<float*>(static_cast<char*>(workspace) + align256((size_t)M * 2 * N * es));
+  if (db_out) EPD_TRY(column_sum(dtype, dout, lddo, M, D, db_out, part, s));
+  if (dw_out) EPD_TRY(weight_gradient(dtype, dout, lddo, hidden, ldh, dw_out, lddw_out, M, D, N, s));
+  if (!inner) return EPD_OK;
+  EPD_TRY(gate_gradient(dtype, dout, lddo, w_out, ldw_out, pre, ldp, dpre, 2 * N, M, N, D, gate, s));
+  if (db_in) EPD_TRY(column_sum(dtype, dpre, 2 * N, M, 2 * N, db_in, part, s));
+  if (dw_in) EPD_TRY(weight_gradient(dtype, dpre, 2 * N, x, ldx, dw_in, lddw_in, M, 2 * N, K, s));
+  if (dx) EPD_TRY(input_gradient(dtype, dpre, 2 * N, w_in, ldw_in, dx, lddx, M, 2 * N, K, s));
+  return EPD_OK;
+}
+
+size_t epd_linear_backward_workspace_bytes(int32_t dtype, int64_t M, int64_t N) {
+  using namespace epd;
+  if (!dtype_ok(dtype) || M < 0 || M > (1 << 28) || !extent_ok(N)) return 0;
+  return column_sum_bytes(M, N) + 256;
+}
+
+int epd_op_linear_backward(int32_t dtype, const void* dout, int64_t lddo, const void* x, int64_t ldx, const void* w,
+                           int64_t ldw, void* dx, int64_t lddx, void* dw, int64_t lddw, void* db, void* workspace,
+                           size_t workspace_bytes, int64_t M, int64_t N, int64_t K, void* stream) {
+  using namespace epd;
+  if (!dtype_ok(dtype) || M < 0 || M > (1 << 28) || !extent_ok(N) || !extent_ok(K)) return EPD_EINVAL;
+  if (lddo < N || (dx && (ldw < K || lddx < K)) || (dw && (ldx < K || lddw < K))) return EPD_EINVAL;
+  const size_t es = dtype == EPD_DTYPE_F32 ? 4 : 2;
+  if (!aligned_to(es, dout, x, w, dx, dw, db)) return EPD_EINVAL;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (M == 0) {
+    EPD_TRY(zero_rows(dtype, dw, lddw, N, K, s));
+    EPD_TRY(zero_rows(dtype, db, N, 1, N, s));
+    return EPD_OK;
+  }
+  if (!dout || (dx && !w) || (dw && !x)) return EPD_EINVAL;
+  if (db) {
+    if (!workspace || (uintptr_t)workspace % 256) return EPD_EINVAL;
+    if (workspace_bytes < epd_linear_backward_workspace_bytes(dtype, M, N)) return EPD_ENOMEM;
+    EPD_TRY(column_sum(dtype, dout, lddo, M, N, db, static_cast<float*>(workspace), s));
+  }
+  if (dw) EPD_TRY(weight_gradient(dtype, dout, lddo, x, ldx, dw, lddw, M, N, K, s));
+  if (dx) EPD_TRY(input_gradient(dtype, dout, lddo, w, ldw, dx, lddx, M, N, K, s));
+  return EPD_OK;
+}
+
+}  // extern "C"

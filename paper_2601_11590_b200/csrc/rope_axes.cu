@@ -1,0 +1,385 @@
+// Rotary embedding with several position axes (time, row, column, ...): on any strided [tokens, heads, head_dim]
+// tensor, and fused with the head split in front of the attention step, each with its gradient.
+//
+// Rotation pair i of a head belongs to axis a(i) and turns by  t = pos[a(i)] * w_i :
+//   (x, y) -> (x cos t - y sin t, y cos t + x sin t).
+// The rotation is orthogonal, so its gradient is the rotation by -t; the gradient of the head split is the way back
+// from the head-major rows to the packed row.  All of it is one kernel: a list of up to three tensors, source and
+// destination strides, an angle sign and a factor per tensor.
+//
+// HBM bound: every element is read once and written once.  A thread keeps one slot of a head (U neighbouring pairs:
+// two U-wide vectors) of one token and walks heads and tensors with it, so the token's cosines and sines are loaded
+// into its registers once; they are formed once per block, in shared memory: the turn count pos * w_i / 2 pi in
+// double precision, its distance to the nearest whole number rounded to float, then one sincospif.  A far position
+// so keeps its fraction of a turn to 2^-26.
+#include <math.h>
+
+#include "common.cuh"
+
+namespace epd {
+namespace {
+
+constexpr int kMaxPairs = kMaxHeadDim / 2;
+constexpr int kMaxAxes = 4;
+constexpr int kMaxTokens = 8;       // tokens of a block
+
+// Runs of pairs: pair run_pair[r] + f turns head dimensions run_base[r] + f and run_base[r] + run_len[r] + f.
+struct AxesPlan {
+  double turns[kMaxPairs];          // turns per unit of position
+  uint8_t axis[kMaxPairs];
+  int n_runs, pairs;
+  int run_base[kMaxAxes], run_len[kMaxAxes], run_pair[kMaxAxes];
+};
+
+struct AxesArgs {
+  const void* src[3];
+  void* dst[3];
+  float scale[3];
+  int rotate[3];
+  int n_tensors, heads, dh;
+  int pad;                          // elements behind head_dim that the destination rows carry (written), or 0
+  int64_t src_token, src_head, dst_token, dst_head;   // strides in elements
+  const int32_t* pos;
+  int64_t pos_stride;
+  int64_t T;
+  float sign;                       // -1: the rotation by -t
+};
+
+template <int BYTES> struct Vec;
+template <> struct Vec<2> { using type = uint16_t; };
+template <> struct Vec<4> { using type = uint32_t; };
+template <> struct Vec<8> { using type = uint2; };
+template <> struct Vec<16> { using type = uint4; };
+
+template <typename T, int U>
+__device__ __forceinline__ void load_vec(const T* p, T (&v)[U]) {
+  using V = typename Vec<U * (int)sizeof(T)>::type;
+  *reinterpret_cast<V*>(v) = *reinterpret_cast<const V*>(p);
+}
+template <typename T, int U>
+__device__ __forceinline__ void store_vec(T* p, const T (&v)[U]) {
+  using V = typename Vec<U * (int)sizeof(T)>::type;
+  *reinterpret_cast<V*>(p) = *reinterpret_cast<const V*>(v);
+}
+
+template <typename T, int U>
+__global__ void __launch_bounds__(512)
+rope_axes_kernel(const __grid_constant__ AxesPlan plan, const __grid_constant__ AxesArgs a, int tok_per_block, int slots,
+                 int groups) {
+  pdl_launch_dependents();
+  pdl_wait();
+  __shared__ float2 s_cs[kMaxTokens][kMaxPairs];
+  const int64_t j0 = (int64_t)blockIdx.x * tok_per_block;
+  const int ntok = (int)min((int64_t)tok_per_block, a.T - j0);
+  for (int i = threadIdx.x; i < ntok * plan.pairs; i += blockDim.x) {
+    const int t = i / plan.pairs, p = i - t * plan.pairs;
+    const int32_t pos = a.pos[plan.axis[p] * a.pos_stride + j0 + t];
+    const double turns = (double)pos * plan.turns[p];
+    float sn, cs;
+    sincospif(2.0f * (float)(turns - rint(turns)), &sn, &cs);
+    s_cs[t][p] = make_float2(cs, a.sign * sn);
+  }
+  __syncthreads();
+  const int per_group = tok_per_block * slots;
+  const int group = threadIdx.x / per_group;
+  const int within = threadIdx.x - group * per_group;
+  const int t = within / slots, slot = within - t * slots;
+  if (group >= groups || t >= ntok) return;
+  const int64_t j = j0 + t;
+  const int units = plan.pairs / U;
+  const int first_head = (int)blockIdx.y * groups + group, head_step = groups * gridDim.y;
+  alignas(16) T x[U], y[U];
+  if (slot < units) {
+    // U pairs of one run
+    int r = 0, f = slot * U;
+    while (f >= plan.run_len[r]) f -= plan.run_len[r++];
+    const int d0 = plan.run_base[r] + f, d1 = d0 + plan.run_len[r];
+    float cs[U], sn[U];
+#pragma unroll
+    for (int e = 0; e < U; ++e) {
+      const float2 v = s_cs[t][plan.run_pair[r] + f + e];
+      cs[e] = v.x;
+      sn[e] = v.y;
+    }
+    for (int w = 0; w < a.n_tensors; ++w) {
+      const T* src = static_cast<const T*>(a.src[w]) + j * a.src_token;
+      T* dst = static_cast<T*>(a.dst[w]) + j * a.dst_token;
+      const float sc = a.scale[w];
+      if (a.rotate[w]) {
+#pragma unroll 4
+        for (int h = first_head; h < a.heads; h += head_step) {
+          load_vec<T, U>(src + h * a.src_head + d0, x);
+          load_vec<T, U>(src + h * a.src_head + d1, y);
+#pragma unroll
+          for (int e = 0; e < U; ++e) {
+            const float p = to_float<T>(x[e]), q = to_float<T>(y[e]);
+            x[e] = from_float<T>((p * cs[e] - q * sn[e]) * sc);
+            y[e] = from_float<T>((q * cs[e] + p * sn[e]) * sc);
+          }
+          store_vec<T, U>(dst + h * a.dst_head + d0, x);
+          store_vec<T, U>(dst + h * a.dst_head + d1, y);
+        }
+      } else {
+#pragma unroll 4
+        for (int h = first_head; h < a.heads; h += head_step) {
+          load_vec<T, U>(src + h * a.src_head + d0, x);
+          load_vec<T, U>(src + h * a.src_head + d1, y);
+          store_vec<T, U>(dst + h * a.dst_head + d0, x);
+          store_vec<T, U>(dst + h * a.dst_head + d1, y);
+        }
+      }
+    }
+    return;
+  }
+  // dimensions behind the last pair: copied (times the tensor's factor); then the padding of the destination rows
+  const int d = 2 * plan.pairs + (slot - units) * U;
+  for (int w = 0; w < a.n_tensors; ++w) {
+    const T* src = static_cast<const T*>(a.src[w]) + j * a.src_token;
+    T* dst = static_cast<T*>(a.dst[w]) + j * a.dst_token;
+    const float sc = a.scale[w];
+    for (int h = first_head; h < a.heads; h += head_step) {
+      if (d < a.dh) {
+        load_vec<T, U>(src + h * a.src_head + d, x);
+        if (a.rotate[w]) {
+#pragma unroll
+          for (int e = 0; e < U; ++e) x[e] = from_float<T>(to_float<T>(x[e]) * sc);
+        }
+      } else {
+        // column head_dim of v (the tensor that is not rotated) is 1: the attention step's P V then yields the row sums
+#pragma unroll
+        for (int e = 0; e < U; ++e) x[e] = from_float<T>(!a.rotate[w] && d + e == a.dh ? 1.0f : 0.0f);
+      }
+      store_vec<T, U>(dst + h * a.dst_head + d, x);
+    }
+  }
+}
+
+// False if the description is not one of a head_dim-wide head.
+bool make_plan(AxesPlan* p, int head_dim, const int32_t* sections, int n_axes, int layout, float theta) {
+  if (n_axes < 1 || n_axes > kMaxAxes || !sections || !isfinite(theta)) return false;
+  if (layout != EPD_ROPE_BLOCKS && layout != EPD_ROPE_SECTIONS && layout != EPD_ROPE_INTERLEAVED) return false;
+  int64_t pairs = 0;
+  for (int a = 0; a < n_axes; ++a) {
+    if (sections[a] < 0) return false;
+    pairs += sections[a];
+  }
+  if (2 * pairs > head_dim) return false;
+  p->pairs = (int)pairs;
+  p->n_runs = 0;
+  const double kInvTwoPi = 0.15915494309189533576888376337251;
+  const double log2_theta = theta > 0.0f ? log2((double)theta) : 0.0;
+  auto ladder = [&](int f, int n) { return theta > 0.0f ? exp2(-log2_theta * f / n) * kInvTwoPi : 0.0; };
+  if (layout == EPD_ROPE_BLOCKS) {
+    int pair = 0;
+    for (int a = 0; a < n_axes; ++a) {
+      const int n = sections[a];
+      if (n == 0) continue;
+      p->run_base[p->n_runs] = 2 * pair;
+      p->run_len[p->n_runs] = n;
+      p->run_pair[p->n_runs++] = pair;
+      for (int f = 0; f < n; ++f, ++pair) {
+        p->axis[pair] = (uint8_t)a;
+        p->turns[pair] = ladder(f, n);
+      }
+    }
+    return true;
+  }
+  int left[kMaxAxes];
+  for (int a = 0; a < n_axes; ++a) left[a] = sections[a];
+  int turn = 0;
+  for (int i = 0; i < (int)pairs; ++i) {
+    if (layout == EPD_ROPE_INTERLEAVED) {
+      while (left[turn] == 0) turn = (turn + 1) % n_axes;
+      p->axis[i] = (uint8_t)turn;
+      --left[turn];
+      turn = (turn + 1) % n_axes;
+    } else {
+      while (left[turn] == 0) ++turn;
+      p->axis[i] = (uint8_t)turn;
+      --left[turn];
+    }
+    p->turns[i] = ladder(i, (int)pairs);
+  }
+  if (pairs > 0) {
+    p->n_runs = 1;
+    p->run_base[0] = 0;
+    p->run_len[0] = (int)pairs;
+    p->run_pair[0] = 0;
+  }
+  return true;
+}
+
+template <typename T, int U>
+cudaError_t launch(const AxesPlan& p, const AxesArgs& a, cudaStream_t s) {
+  const int slots = p.pairs / U + (a.dh + a.pad - 2 * p.pairs) / U;
+  // tokens of a block: as many as leave two blocks for every SM, and no more than fill 512 threads
+  int tok = kMaxTokens;
+  while (tok > 1 && (a.T < (int64_t)tok * 296 || tok * slots > 512)) tok >>= 1;
+  const int per_group = tok * slots;
+  int groups = 256 / per_group > 0 ? 256 / per_group : 1;
+  if (groups > a.heads) groups = a.heads;
+  // few tokens: the heads are dealt to several blocks
+  const int64_t blocks = (a.T + tok - 1) / tok;
+  int split = 1;
+  while (blocks * split < 296 && split * groups * 2 <= a.heads) split *= 2;
+  if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
+  return launch_pdl(rope_axes_kernel<T, U>, dim3((unsigned)blocks, (unsigned)split), dim3((per_group * groups + 31) / 32 * 32),
+                    0, s, p, a, tok, slots, groups);
+}
+
+// Widest vector that every run, every stride and every pointer allows.
+cudaError_t dispatch(int dtype, const AxesPlan& p, const AxesArgs& a, cudaStream_t s) {
+  if (a.T == 0) return cudaSuccess;
+  const int es = dtype == EPD_DTYPE_F32 ? 4 : 2;
+  int u = 16 / es;
+  auto fits = [&](int w) {
+    for (int r = 0; r < p.n_runs; ++r)
+      if (p.run_len[r] % w || p.run_base[r] % w) return false;
+    if (a.dh % w || a.pad % w || a.src_token % w || a.src_head % w || a.dst_token % w || a.dst_head % w) return false;
+    for (int i = 0; i < a.n_tensors; ++i)
+      if (((uintptr_t)a.src[i] | (uintptr_t)a.dst[i]) % (w * es)) return false;
+    return true;
+  };
+  while (u > 1 && !fits(u)) u >>= 1;
+  if (dtype == EPD_DTYPE_F32) {
+    if (u == 4) return launch<float, 4>(p, a, s);
+    if (u == 2) return launch<float, 2>(p, a, s);
+    return launch<float, 1>(p, a, s);
+  }
+  if (u == 8) return launch<__nv_bfloat16, 8>(p, a, s);
+  if (u == 4) return launch<__nv_bfloat16, 4>(p, a, s);
+  if (u == 2) return launch<__nv_bfloat16, 2>(p, a, s);
+  return launch<__nv_bfloat16, 1>(p, a, s);
+}
+
+int finish(cudaError_t e) {
+  if (e == cudaSuccess) return EPD_OK;
+  note_cuda_error(e);
+  return EPD_ECUDA;
+}
+
+bool common_ok(int32_t dtype, int64_t T, int32_t heads, int32_t head_dim, int64_t pos_stride) {
+  return (dtype == EPD_DTYPE_F32 || dtype == EPD_DTYPE_BF16) && T >= 0 && T <= (1 << 30) && heads >= 1 &&
+         heads <= 65535 && head_dim >= 1 && head_dim <= kMaxHeadDim && pos_stride >= T;
+}
+
+}  // namespace
+}  // namespace epd
+
+extern "C" {
+
+int epd_op_rope_axes(int32_t dtype, const void* x, int64_t x_token_stride, int64_t x_head_stride, const int32_t* pos,
+                     int64_t pos_stride, void* out, int64_t out_token_stride, int64_t out_head_stride, int64_t T,
+                     int32_t heads, int32_t head_dim, const int32_t* sections, int32_t n_axes, int32_t layout,
+                     float theta, float scale, int32_t inverse, void* stream) {
+  using namespace epd;
+  AxesPlan p;
+  if (!common_ok(dtype, T, heads, head_dim, pos_stride) || !make_plan(&p, head_dim, sections, n_axes, layout, theta))
+    return EPD_EINVAL;
+  // rows of a tensor must not run into one another
+  auto strides_ok = [&](int64_t token, int64_t head) {
+    return token >= 0 && head >= 0 && token < ((int64_t)1 << 32) && head < ((int64_t)1 << 40) &&
+           (heads == 1 || head >= head_dim) &&
+           (T <= 1 || token >= head_dim) &&
+           (heads == 1 || T <= 1 || token >= head * (heads - 1) + head_dim || head >= token * (T - 1) + head_dim);
+  };
+  if (!strides_ok(x_token_stride, x_head_stride) || !strides_ok(out_token_stride, out_head_stride)) return EPD_EINVAL;
+  if (T == 0) return EPD_OK;
+  if (!x || !pos || !out) return EPD_EINVAL;
+  const int es = dtype == EPD_DTYPE_F32 ? 4 : 2;
+  if ((uintptr_t)x % es || (uintptr_t)out % es || (uintptr_t)pos % 4) return EPD_EINVAL;
+  if (x == out && (x_token_stride != out_token_stride || x_head_stride != out_head_stride)) return EPD_EINVAL;
+  AxesArgs a = {};
+  a.src[0] = x;
+  a.dst[0] = out;
+  a.scale[0] = scale;
+  a.rotate[0] = 1;
+  a.n_tensors = 1;
+  a.heads = heads;
+  a.dh = head_dim;
+  a.src_token = x_token_stride;
+  a.src_head = x_head_stride;
+  a.dst_token = out_token_stride;
+  a.dst_head = out_head_stride;
+  a.pos = pos;
+  a.pos_stride = pos_stride;
+  a.T = T;
+  a.sign = inverse ? -1.0f : 1.0f;
+  return finish(dispatch(dtype, p, a, static_cast<cudaStream_t>(stream)));
+}
+
+int epd_op_rope_axes_split(int32_t dtype, const void* qkv, int64_t ldqkv, const int32_t* pos, int64_t pos_stride, void* q,
+                           void* k, void* v, int64_t T, int32_t heads, int32_t head_dim, const int32_t* sections,
+                           int32_t n_axes, int32_t layout, float theta, float q_scale, void* stream) {
+  using namespace epd;
+  AxesPlan p;
+  if (!common_ok(dtype, T, heads, head_dim, pos_stride) || !make_plan(&p, head_dim, sections, n_axes, layout, theta))
+    return EPD_EINVAL;
+  const int64_t h = (int64_t)heads * head_dim;
+  if (ldqkv < 3 * h) return EPD_EINVAL;
+  if (T == 0) return EPD_OK;
+  if (!qkv || !pos || !q || !k || !v) return EPD_EINVAL;
+  const int es = dtype == EPD_DTYPE_F32 ? 4 : 2;
+  if (((uintptr_t)qkv | (uintptr_t)q | (uintptr_t)k | (uintptr_t)v) % es || (uintptr_t)pos % 4) return EPD_EINVAL;
+  const int dhp = padded_head_dim(head_dim);
+  AxesArgs a = {};
+  void* const dst[3] = {q, k, v};
+  for (int w = 0; w < 3; ++w) {
+    a.src[w] = static_cast<const char*>(qkv) + w * h * es;
+    a.dst[w] = dst[w];
+    a.scale[w] = w == 0 ? q_scale : 1.0f;
+    a.rotate[w] = w < 2;
+  }
+  a.n_tensors = 3;
+  a.heads = heads;
+  a.dh = head_dim;
+  a.pad = dhp - head_dim;
+  a.src_token = ldqkv;
+  a.src_head = head_dim;
+  a.dst_token = dhp;
+  a.dst_head = T * dhp;
+  a.pos = pos;
+  a.pos_stride = pos_stride;
+  a.T = T;
+  a.sign = 1.0f;
+  return finish(dispatch(dtype, p, a, static_cast<cudaStream_t>(stream)));
+}
+
+int epd_op_rope_axes_split_backward(int32_t dtype, const void* dq, const void* dk, const void* dv, const int32_t* pos,
+                                    int64_t pos_stride, void* dqkv, int64_t lddqkv, int64_t T, int32_t heads,
+                                    int32_t head_dim, const int32_t* sections, int32_t n_axes, int32_t layout,
+                                    float theta, float q_scale, void* stream) {
+  using namespace epd;
+  AxesPlan p;
+  if (!common_ok(dtype, T, heads, head_dim, pos_stride) || !make_plan(&p, head_dim, sections, n_axes, layout, theta))
+    return EPD_EINVAL;
+  const int64_t h = (int64_t)heads * head_dim;
+  if (lddqkv < 3 * h) return EPD_EINVAL;
+  if (T == 0) return EPD_OK;
+  if (!dqkv || !pos || !dq || !dk || !dv) return EPD_EINVAL;
+  const int es = dtype == EPD_DTYPE_F32 ? 4 : 2;
+  if (((uintptr_t)dqkv | (uintptr_t)dq | (uintptr_t)dk | (uintptr_t)dv) % es || (uintptr_t)pos % 4) return EPD_EINVAL;
+  const int dhp = padded_head_dim(head_dim);
+  AxesArgs a = {};
+  const void* const src[3] = {dq, dk, dv};
+  for (int w = 0; w < 3; ++w) {
+    a.src[w] = src[w];
+    a.dst[w] = static_cast<char*>(dqkv) + w * h * es;
+    a.scale[w] = w == 0 ? q_scale : 1.0f;
+    a.rotate[w] = w < 2;
+  }
+  a.n_tensors = 3;
+  a.heads = heads;
+  a.dh = head_dim;
+  a.src_token = dhp;
+  a.src_head = T * dhp;
+  a.dst_token = lddqkv;
+  a.dst_head = head_dim;
+  a.pos = pos;
+  a.pos_stride = pos_stride;
+  a.T = T;
+  a.sign = -1.0f;
+  return finish(dispatch(dtype, p, a, static_cast<cudaStream_t>(stream)));
+}
+
+}  // extern "C"

@@ -1,0 +1,394 @@
+"""Gated feed-forward block, its gradient and the gradient of a linear layer against the definition in float64.
+
+Tolerances (relative Frobenius error, worst row within the factor of tests/metrics.py).  Rounding to bf16 is off by at
+most 2^-8 = 3.9e-3 of a value.
+  one rounding (hidden, pre, dw_out from given bf16 inputs, ...)     4e-3
+  two roundings in a row (out behind the rounded hidden; dx, dw_in, db_in behind the rounded gradient of pre):
+  independent errors of at most 2^-8 each, sqrt(2) * 2^-8 = 5.6e-3    6e-3
+  float: sums of up to K terms in float, error about sqrt(K) * 2^-24 of the result, K <= 6000: 4.6e-6;   1e-5
+"""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2601_11590_b200 as epd
+from tests.metrics import assert_parity
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = epd.DTYPE_F32, epd.DTYPE_BF16
+GATES = [epd.GATE_SILU, epd.GATE_GELU_TANH, epd.GATE_GELU_ERF]
+ONE = {BF16: 4e-3, F32: 1e-5}
+TWO = {BF16: 6e-3, F32: 1e-5}
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    from paper_2601_11590_b200 import build
+    build.build_library()
+    epd.load_library()
+
+
+def act_and_slope(gate, g):
+    if gate == epd.GATE_SILU:
+        s = 1 / (1 + torch.exp(-g))
+        return g * s, s + g * s * (1 - s)
+    if gate == epd.GATE_GELU_TANH:
+        c = np.sqrt(2 / np.pi)
+        t = torch.tanh(c * (g + 0.044715 * g ** 3))
+        return 0.5 * g * (1 + t), 0.5 * (1 + t) + 0.5 * g * (1 - t * t) * c * (1 + 3 * 0.044715 * g * g)
+    phi = 0.5 * torch.erfc(-g / np.sqrt(2))
+    return g * phi, phi + g * torch.exp(-g * g / 2) / np.sqrt(2 * np.pi)
+
+
+def f64(t):
+    return None if t is None else t.detach().double()
+
+
+def reference_forward(x, w_in, b_in, gate):
+    N = w_in.shape[0] // 2
+    pre = f64(x) @ f64(w_in).T
+    if b_in is not None:
+        pre = pre + f64(b_in)
+    return pre, act_and_slope(gate, pre[:, :N])[0] * pre[:, N:]
+
+
+def reference_backward(dout, x, w_in, w_out, hidden, pre, gate):
+    """Gradients from the saved values as they stand (the operator's contract)."""
+    N = w_in.shape[0] // 2
+    dout, x, w_in, w_out, hidden, pre = map(f64, (dout, x, w_in, w_out, hidden, pre))
+    act, slope = act_and_slope(gate, pre[:, :N])
+    da = dout @ w_out
+    dpre = torch.cat([da * pre[:, N:] * slope, da * act], 1)
+    return {"dx": dpre @ w_in, "dw_in": dpre.T @ x, "db_in": dpre.sum(0), "dw_out": dout.T @ hidden, "db_out": dout.sum(0)}
+
+
+class Draw:
+    def __init__(self, seed, dtype):
+        self.g = torch.Generator(device="cuda").manual_seed(seed)
+        self.dt = torch.float32 if dtype == F32 else torch.bfloat16
+
+    def __call__(self, std, *shape):
+        return (torch.randn(*shape, generator=self.g, device="cuda") * std).to(self.dt)
+
+
+def block(seed, dtype, M, N, K, D=None, bias=True):
+    D = K if D is None else D
+    n = Draw(seed, dtype)
+    return dict(x=n(1.0, M, K), w_in=n(K ** -0.5, 2 * N, K), b_in=n(0.3, 2 * N) if bias else None,
+                w_out=n(N ** -0.5, D, N), b_out=n(0.3, D) if bias else None, dout=n(0.1, M, D))
+
+
+def parity(got, ref, tol, what):
+    assert_parity(got.double().cpu().numpy(), ref.double().cpu().numpy(), tol, what)
+
+
+def check_block(dtype, b, gate):
+    out, hidden, pre = epd.op_gated_mlp(dtype, b["x"], b["w_in"], b["b_in"], b["w_out"], b["b_out"], gate, save=True)
+    pre_ref, hid_ref = reference_forward(b["x"], b["w_in"], b["b_in"], gate)
+    out_ref = hid_ref @ f64(b["w_out"]).T
+    if b["b_out"] is not None:
+        out_ref = out_ref + f64(b["b_out"])
+    parity(pre, pre_ref, ONE[dtype], "pre")
+    parity(hidden, hid_ref, ONE[dtype], "hidden")
+    parity(out, out_ref, TWO[dtype], "out")
+    # without saving the projections, and as a single step: the same bits
+    assert torch.equal(epd.op_gated_mlp(dtype, b["x"], b["w_in"], b["b_in"], b["w_out"], b["b_out"], gate), out)
+    assert torch.equal(epd.op_gated_linear(dtype, b["x"], b["w_in"], b["b_in"], gate), hidden)
+    g = epd.op_gated_mlp_backward(dtype, b["dout"], b["x"], b["w_in"], b["w_out"], hidden, pre, gate,
+                                  bias=b["b_in"] is not None)
+    ref = reference_backward(b["dout"], b["x"], b["w_in"], b["w_out"], hidden, pre, gate)
+    for name in g:
+        parity(g[name], ref[name], ONE[dtype] if name in ("dw_out", "db_out") else TWO[dtype], name)
+    return out, hidden, pre, g
+
+
+# token counts on both sides of every kernel's limit, and of its tiles
+@pytest.mark.parametrize("M", [1, 2, 7, 8, 9, 16, 17, 32, 33, 64, 65, 127, 129, 255, 257, 700])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_block_over_token_counts(dtype, M):
+    check_block(dtype, block(100 + M, dtype, M, 320, 192, bias=M % 2 == 1), GATES[M % 3])
+
+
+@pytest.mark.parametrize("N,K,D", [
+    (8, 8, 8),            # smaller than one tile in every direction
+    (136, 72, 40),        # ragged in every direction, D != K
+    (1080, 1152, 1152),   # several tiles
+    (1152, 264, 4304),    # ragged last output tile
+    (24, 5120, 16),       # long contraction, few columns
+    (4304, 64, 64),       # short contraction
+])
+@pytest.mark.parametrize("M", [1, 5, 40, 300])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_block_over_widths(dtype, M, N, K, D):
+    check_block(dtype, block(7, dtype, M, N, K, D), epd.GATE_SILU)
+
+
+@pytest.mark.parametrize("N,K,D", [(7, 5, 3), (33, 100, 11), (1, 1, 1)])
+@pytest.mark.parametrize("M", [1, 3, 130])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_block_odd_widths(dtype, M, N, K, D):
+    """Widths that are no multiples of 8: the plain-FMA kernels in bf16."""
+    b = block(8, dtype, M, N, K, D)
+    out, hidden, pre = epd.op_gated_mlp(dtype, b["x"], b["w_in"], b["b_in"], b["w_out"], b["b_out"], epd.GATE_GELU_ERF,
+                                        save=True)
+    pre_ref, hid_ref = reference_forward(b["x"], b["w_in"], b["b_in"], epd.GATE_GELU_ERF)
+    # element by element (a result may be a single number): 2^-8 of the value per rounding in bf16, and the terms' sum
+    # of moduli times the number of additions times 2^-24 for the float sums
+    def near(got, ref, moduli, terms, roundings):
+        step = 2.0 ** -8 if dtype == BF16 else 2.0 ** -24
+        bound = roundings * step * ref.abs() + (terms + 8) * 2.0 ** -23 * moduli + 1e-30
+        assert bool(((got.double() - ref).abs() <= bound).all())
+    near(pre, pre_ref, f64(b["x"]).abs() @ f64(b["w_in"]).abs().T + 2, K, 1)
+    out_from_saved = f64(hidden) @ f64(b["w_out"]).T + f64(b["b_out"])
+    near(out, out_from_saved, f64(hidden).abs() @ f64(b["w_out"]).abs().T + 2, N, 1)
+    parity(hidden, hid_ref, TWO[dtype], "hidden")
+    g = epd.op_gated_mlp_backward(dtype, b["dout"], b["x"], b["w_in"], b["w_out"], hidden, pre, epd.GATE_GELU_ERF)
+    ref = reference_backward(b["dout"], b["x"], b["w_in"], b["w_out"], hidden, pre, epd.GATE_GELU_ERF)
+    near(g["dw_out"], ref["dw_out"], f64(b["dout"]).abs().T @ f64(hidden).abs(), M, 1)
+    near(g["db_out"], ref["db_out"], f64(b["dout"]).abs().sum(0), M, 1)
+    # behind the rounded gradient of pre every term carries its own 2^-8
+    act, slope = act_and_slope(epd.GATE_GELU_ERF, f64(pre)[:, :N])
+    da = f64(b["dout"]) @ f64(b["w_out"])
+    da_mod = f64(b["dout"]).abs() @ f64(b["w_out"]).abs()
+    mod = torch.cat([da_mod * (f64(pre)[:, N:] * slope).abs(), da_mod * act.abs()], 1)
+    dmod = torch.cat([(da * f64(pre)[:, N:] * slope).abs(), (da * act).abs()], 1)
+    step = 2.0 ** -8 if dtype == BF16 else 2.0 ** -24
+    for name, lead, last in (("dx", lambda t: t, f64(b["w_in"])), ("dw_in", lambda t: t.T, f64(b["x"]))):
+        r = ref[name]
+        term = lead(dmod) @ last.abs()
+        total = lead(mod) @ last.abs()
+        bound = step * (r.abs() + 1.01 * term) + (D + 2 * N + M + 16) * 2.0 ** -22 * total + 1e-30
+        assert bool(((g[name].double() - r).abs() <= bound).all()), name
+
+
+def test_block_at_the_encoder_widths():
+    for M, N, K, gate in ((777, 4304, 1152, epd.GATE_GELU_TANH), (30, 12800, 3200, epd.GATE_GELU_ERF),
+                          (1, 12800, 3200, epd.GATE_SILU)):
+        check_block(BF16, block(M, BF16, M, N, K), gate)
+
+
+@pytest.mark.parametrize("M,offset", [(1, 0), (1, 8), (20, 0), (20, 8), (300, 8), (20, 1), (300, 3)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_strided_operands_and_untouched_neighbours(dtype, M, offset):
+    """Every matrix a window of a larger one filled with NaN: nothing outside is read into a result or written.  Offsets
+    that are no multiples of 8 leave the tensor-core kernels."""
+    N, K, D = 88, 72, 56
+    dt = torch.float32 if dtype == F32 else torch.bfloat16
+    b = block(3, dtype, M, N, K, D)
+
+    def window(t, rows, cols):
+        big = torch.full((rows + 3, cols + 40), float("nan"), dtype=dt, device="cuda")
+        w = big[1:1 + rows, offset:offset + cols]
+        if t is not None:
+            w.copy_(t)
+        return big, w
+    ins = {n: window(b[n], *b[n].shape)[1] for n in ("x", "w_in", "w_out", "dout")}
+    outs = {n: window(None, *s) for n, s in (("out", (M, D)), ("hidden", (M, N)), ("pre", (M, 2 * N)))}
+    epd.op_gated_mlp(dtype, ins["x"], ins["w_in"], b["b_in"], ins["w_out"], b["b_out"], epd.GATE_SILU,
+                     out=outs["out"][1], hidden=outs["hidden"][1], pre=outs["pre"][1])
+    pre_ref, hid_ref = reference_forward(b["x"], b["w_in"], b["b_in"], epd.GATE_SILU)
+    parity(outs["pre"][1], pre_ref, ONE[dtype], "pre")
+    parity(outs["hidden"][1], hid_ref, ONE[dtype], "hidden")
+    parity(outs["out"][1], hid_ref @ f64(b["w_out"]).T + f64(b["b_out"]), TWO[dtype], "out")
+    g = epd.op_gated_mlp_backward(dtype, ins["dout"], ins["x"], ins["w_in"], ins["w_out"], outs["hidden"][1],
+                                  outs["pre"][1], epd.GATE_SILU)
+    ref = reference_backward(b["dout"], b["x"], b["w_in"], b["w_out"], outs["hidden"][1], outs["pre"][1], epd.GATE_SILU)
+    for name in g:
+        parity(g[name], ref[name], TWO[dtype], name)
+    for n, (big, w) in outs.items():
+        w.fill_(float("nan"))
+        assert bool(torch.isnan(big).all()), n
+
+
+@pytest.mark.parametrize("M", [1, 12, 200])
+def test_residual_update_and_float_output(M):
+    b = block(4, BF16, M, 320, 192)
+    _, hid_ref = reference_forward(b["x"], b["w_in"], b["b_in"], epd.GATE_GELU_TANH)
+    ref = hid_ref @ f64(b["w_out"]).T + f64(b["b_out"])
+    r0 = torch.randn(M, 192, device="cuda")
+    args = (BF16, b["x"], b["w_in"], b["b_in"], b["w_out"], b["b_out"], epd.GATE_GELU_TANH)
+    # one rounding (hidden) behind float sums
+    parity(epd.op_gated_mlp(*args, flags=epd.LINEAR_OUT_F32), ref, ONE[BF16], "float out")
+    x = r0.clone()
+    epd.op_gated_mlp(*args, out=x, flags=epd.LINEAR_ACCUMULATE)
+    parity(x, ref + r0.double(), ONE[BF16], "residual")
+    with pytest.raises(ValueError):
+        epd.op_gated_mlp(*args, flags=epd.LINEAR_ACCUMULATE)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("M", [3, 150])
+def test_large_and_infinite_gates(dtype, M):
+    """Gates far out on both sides: the activation and its slope reach their limits, nothing overflows to NaN."""
+    N, K = 64, 64
+    x = torch.zeros(M, K, device="cuda")
+    x[:, 0] = 1
+    w = torch.zeros(2 * N, K, device="cuda")
+    w[:N, 0] = torch.tensor([-1e37, -1e20, -1e5, -200.0, -30.0, -1.0, -0.0, 0.0, 1.0, 30.0, 200.0, 1e5, 1e20, 1e37, 8.0, -8.0],
+                            device="cuda").repeat(N // 16)
+    w[N:, 0] = 0.5
+    n = Draw(5, dtype)
+    dt = n.dt
+    x, w = x.to(dt), w.to(dt)
+    w_out, dout = torch.eye(N, device="cuda").to(dt), n(1.0, M, N)
+    for gate in GATES:
+        _, hidden, pre = epd.op_gated_mlp(dtype, x, w, None, w_out, None, gate, save=True)
+        hid_ref = reference_forward(x, w, None, gate)[1]
+        assert bool(torch.isfinite(hidden.float()).all())
+        assert torch.allclose(hidden.double(), hid_ref, rtol=2.0 ** -7, atol=1e-6)
+        g = epd.op_gated_mlp_backward(dtype, dout, x, w, w_out, hidden, pre, gate, bias=False, need_dw=False)
+        # dx[:, 0] = sum of dg * w_gate + du * w_up: check the gradient of pre itself through an identity in place of w_in
+        eye = torch.eye(2 * N, device="cuda").to(dt)
+        xe = torch.zeros(M, 2 * N, device="cuda", dtype=dt)
+        d = epd.op_gated_mlp_backward(dtype, dout, xe, eye, w_out, hidden, pre, gate, bias=False, need_dw=False)["dx"]
+        p = pre.double()
+        act, slope = act_and_slope(gate, p[:, :N].clamp(-1e3, 1e3))
+        act = torch.where(p[:, :N] > 1e3, p[:, :N], act)
+        ref = torch.cat([dout.double() * p[:, N:] * slope, dout.double() * act], 1)
+        assert torch.allclose(d.double(), ref, rtol=2.0 ** -6, atol=1e-6)
+        assert "dw_in" not in g and "db_in" not in g
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("M", [6, 140])
+def test_rows_do_not_mix(dtype, M):
+    """A row of NaN or infinities changes its own row of hidden, out and dx, and no other."""
+    b = block(11, dtype, M, 96, 64)
+    args = (b["w_in"], b["b_in"], b["w_out"], b["b_out"], epd.GATE_SILU)
+    out, hidden, pre = epd.op_gated_mlp(dtype, b["x"], *args, save=True)
+    dx = epd.op_gated_mlp_backward(dtype, b["dout"], b["x"], b["w_in"], b["w_out"], hidden, pre, epd.GATE_SILU)["dx"]
+    x2, d2 = b["x"].clone(), b["dout"].clone()
+    x2[M // 2] = float("nan")
+    d2[M // 3] = float("inf")
+    out2, hidden2, pre2 = epd.op_gated_mlp(dtype, x2, *args, save=True)
+    dx2 = epd.op_gated_mlp_backward(dtype, d2, x2, b["w_in"], b["w_out"], hidden2, pre2, epd.GATE_SILU)["dx"]
+    keep = torch.ones(M, dtype=torch.bool, device="cuda")
+    keep[M // 2] = False
+    assert torch.equal(out[keep], out2[keep]) and torch.equal(hidden[keep], hidden2[keep])
+    assert bool(torch.isnan(out2[M // 2].float()).all())
+    keep[M // 3] = False
+    assert torch.equal(dx[keep], dx2[keep])
+
+
+def test_gradient_against_differences():
+    """Directional derivatives of the 64-bit definition by central differences against the float kernel's gradient: the
+    kernel is off by at most 1e-5 of the gradient's norm, times the direction's norm (Cauchy-Schwarz); the quotient's own
+    error is step^2 = 1e-10 of the third derivative and 1e-9 of rounding."""
+    M, N, K = 37, 48, 40
+    for gate in GATES:
+        b = block(21, F32, M, N, K)
+        _, hidden, pre = epd.op_gated_mlp(F32, b["x"], b["w_in"], b["b_in"], b["w_out"], b["b_out"], gate, save=True)
+        g = epd.op_gated_mlp_backward(F32, b["dout"], b["x"], b["w_in"], b["w_out"], hidden, pre, gate)
+        names = {"x": "dx", "w_in": "dw_in", "b_in": "db_in", "w_out": "dw_out", "b_out": "db_out"}
+
+        def loss(v):
+            h = reference_forward(v["x"], v["w_in"], v["b_in"], gate)[1]
+            return float(((h @ f64(v["w_out"]).T + f64(v["b_out"])) * f64(b["dout"])).sum())
+        for i, (name, grad) in enumerate(names.items()):
+            dirn = torch.randn(b[name].shape, generator=torch.Generator().manual_seed(i), dtype=torch.float64).cuda()
+            up, down = dict(b), dict(b)
+            up[name], down[name] = f64(b[name]) + 1e-5 * dirn, f64(b[name]) - 1e-5 * dirn
+            quotient = (loss(up) - loss(down)) / 2e-5
+            along = float((g[grad].double() * dirn).sum())
+            scale = float((g[grad].double() ** 2).sum() ** 0.5)
+            assert abs(quotient - along) <= 1e-5 * scale * float(dirn.norm()), (gate, name)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("M,N,K", [(1, 8, 8), (130, 136, 72), (391, 520, 264), (600, 24, 1032), (65, 3456, 128)])
+def test_linear_backward(dtype, M, N, K):
+    n = Draw(31, dtype)
+    x, w, dout = n(1.0, M, K), n(K ** -0.5, N, K), n(0.1, M, N)
+    g = epd.op_linear_backward(dtype, dout, x, w)
+    parity(g["dx"], f64(dout) @ f64(w), ONE[dtype], "dx")
+    parity(g["dw"], f64(dout).T @ f64(x), ONE[dtype], "dw")
+    parity(g["db"], f64(dout).sum(0), ONE[dtype], "db")
+    only = epd.op_linear_backward(dtype, dout, x, w, bias=False, need_dw=False)
+    assert set(only) == {"dx"} and torch.equal(only["dx"], g["dx"])
+    only = epd.op_linear_backward(dtype, dout, x, w, bias=False, need_dx=False)
+    assert set(only) == {"dw"} and torch.equal(only["dw"], g["dw"])
+
+
+def test_many_rows_in_the_gradient():
+    """Row counts beyond one block of the column sums, and a contraction over many rows."""
+    check_block(BF16, block(41, BF16, 5000, 136, 72), epd.GATE_SILU)
+    check_block(F32, block(42, F32, 3001, 40, 24), epd.GATE_GELU_ERF)
+
+
+def test_no_rows():
+    for dtype in (BF16, F32):
+        b = block(51, dtype, 0, 16, 24)
+        out, hidden, pre = epd.op_gated_mlp(dtype, b["x"], b["w_in"], b["b_in"], b["w_out"], b["b_out"], 0, save=True)
+        assert out.shape == (0, 24)
+        g = epd.op_gated_mlp_backward(dtype, b["dout"], b["x"], b["w_in"], b["w_out"], hidden, pre, 0)
+        for name in ("dw_in", "db_in", "dw_out", "db_out"):
+            assert not bool(g[name].any()), name
+        g = epd.op_linear_backward(dtype, b["dout"], b["x"], torch.ones(24, 24, device="cuda").to(b["x"].dtype))
+        assert not bool(g["dw"].any()) and not bool(g["db"].any())
+
+
+@pytest.mark.parametrize("M", [1, 24, 333])
+def test_repeated_calls_streams_and_graphs_give_the_same_bits(M):
+    b = block(61, BF16, M, 320, 192)
+    args = (BF16, b["x"], b["w_in"], b["b_in"], b["w_out"], b["b_out"], epd.GATE_SILU)
+
+    def step():
+        out, hidden, pre = epd.op_gated_mlp(*args, save=True)
+        return [out] + list(epd.op_gated_mlp_backward(BF16, b["dout"], b["x"], b["w_in"], b["w_out"], hidden, pre,
+                                                      epd.GATE_SILU).values())
+    want = step()
+    assert all(torch.equal(p, q) for p, q in zip(want, step()))
+    torch.cuda.synchronize()
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    got = []
+    for s in (s1, s2, s1, s2):
+        with torch.cuda.stream(s):
+            got.append(step())
+    torch.cuda.synchronize()
+    for r in got:
+        assert all(torch.equal(p, q) for p, q in zip(want, r))
+    graph = torch.cuda.CUDAGraph()
+    x0 = b["x"].clone()
+    with torch.cuda.graph(graph):
+        captured = step()
+    b["x"].zero_()
+    graph.replay()
+    b["x"].copy_(x0)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(want, captured))
+
+
+def test_limited_sms_change_no_result():
+    b = block(71, BF16, 700, 520, 264)
+    want = check_block(BF16, b, epd.GATE_SILU)
+    epd.set_sm_limit(20)
+    try:
+        got = check_block(BF16, b, epd.GATE_SILU)
+    finally:
+        epd.set_sm_limit(0)
+    for p, q in zip(want[:3], got[:3]):
+        assert torch.equal(p, q)
+    assert all(torch.equal(want[3][n], got[3][n]) for n in want[3])
+
+
+def test_binding_refuses_mismatched_tensors():
+    b = block(81, BF16, 4, 16, 24)
+    ok = (b["x"], b["w_in"], b["b_in"], b["w_out"], b["b_out"])
+    for i, bad in ((0, b["x"].float()), (0, b["x"].cpu()), (1, b["w_in"][:-1]), (2, b["b_in"][:3]), (3, b["w_out"].t()),
+                   (0, b["x"].t().contiguous().t())):
+        a = list(ok)
+        a[i] = bad
+        with pytest.raises((ValueError, epd.EpdError)):
+            epd.op_gated_mlp(BF16, *a, epd.GATE_SILU)
+    with pytest.raises(epd.EpdError) as e:
+        epd.op_gated_mlp(BF16, *ok, 3)
+    assert e.value.status == epd.EPD_EINVAL
+    _, hidden, pre = epd.op_gated_mlp(BF16, *ok, epd.GATE_SILU, save=True)
+    with pytest.raises(epd.EpdError) as e:
+        epd.op_gated_mlp_backward(BF16, b["dout"], b["x"], b["w_in"], b["w_out"], hidden, pre, epd.GATE_SILU,
+                                  workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
+    assert e.value.status == epd.EPD_ENOMEM
