@@ -184,6 +184,8 @@ cudaError_t column_sum(int dtype, const void* x, int64_t ldx, int64_t M, int64_t
 // =============================================================================================
 cudaError_t gated_linear(int dtype, const void* x, int64_t ldx, const void* w, int64_t ldw, const void* bias, void* out,
                          int64_t ldo, void* pre, int64_t ldp, int64_t M, int64_t N, int64_t K, int gate, cudaStream_t s) {
+  if (dtype == EPD_DTYPE_BF16 && gated_tc_supported({{x, ldx}, {w, ldw}, {out, ldo}, {pre, ldp}}, {N, K}))
+    return gated_tc_forward(x, ldx, w, ldw, bias, out, ldo, pre, ldp, M, N, K, gate, nullptr, s);
   FmaArgs p = {};
   p.a = x; p.lda = ldx;
   p.b = w; p.ldb = ldw;
@@ -199,6 +201,8 @@ cudaError_t gated_linear(int dtype, const void* x, int64_t ldx, const void* w, i
 cudaError_t gate_gradient(int dtype, const void* dout, int64_t lddo, const void* w_out, int64_t ldw, const void* pre,
                           int64_t ldp, void* dpre, int64_t lddp, int64_t M, int64_t N, int64_t D, int gate,
                           cudaStream_t s) {
+  if (dtype == EPD_DTYPE_BF16 && gated_tc_supported({{dout, lddo}, {w_out, ldw}, {pre, ldp}, {dpre, lddp}}, {N, D}))
+    return gated_tc_gradient(dout, lddo, w_out, ldw, pre, ldp, dpre, lddp, M, N, D, gate, s);
   FmaArgs p = {};
   p.a = dout; p.lda = lddo;
   p.b = w_out; p.ldb = ldw;
@@ -212,6 +216,8 @@ cudaError_t gate_gradient(int dtype, const void* dout, int64_t lddo, const void*
 // dx[M, K] = dout[M, N] . w[N, K]
 cudaError_t input_gradient(int dtype, const void* dout, int64_t lddo, const void* w, int64_t ldw, void* dx, int64_t lddx,
                            int64_t M, int64_t N, int64_t K, cudaStream_t s) {
+  if (dtype == EPD_DTYPE_BF16 && gated_tc_supported({{dout, lddo}, {w, ldw}, {dx, lddx}}, {N, K}))
+    return matmul_tc(false, dout, lddo, w, ldw, dx, lddx, M, K, N, s);
   FmaArgs p = {};
   p.a = dout; p.lda = lddo;
   p.b = w; p.ldb = ldw;
@@ -223,6 +229,8 @@ cudaError_t input_gradient(int dtype, const void* dout, int64_t lddo, const void
 // dw[N, K] = dout[M, N]^T . x[M, K]
 cudaError_t weight_gradient(int dtype, const void* dout, int64_t lddo, const void* x, int64_t ldx, void* dw, int64_t lddw,
                             int64_t M, int64_t N, int64_t K, cudaStream_t s) {
+  if (dtype == EPD_DTYPE_BF16 && gated_tc_supported({{dout, lddo}, {x, ldx}, {dw, lddw}}, {N, K}))
+    return matmul_tc(true, dout, lddo, x, ldx, dw, lddw, N, K, M, s);
   FmaArgs p = {};
   p.a = dout; p.lda = lddo;
   p.b = x; p.ldb = ldx;
