@@ -627,35 +627,45 @@ def op_qkv_rope(x, w, bias, pos_row, pos_col, heads, head_dim, theta, q_scale, t
 
 # ---- gated feed-forward block, gradients ------------------------------------------------------------
 
-def _op_context(dtype, named, stream):
-    """Checks the tensors of one call (name -> (tensor or None, shape)): on one CUDA device, of the call's element type,
-    rows contiguous.  Returns (torch, element type, device context, stream pointer); the launch belongs on the tensors'
-    device, whichever is current."""
-    import torch
-    if dtype != DTYPE_F32 and dtype != DTYPE_BF16:
-        raise EpdError(EPD_EINVAL, "dtype")
-    want = torch.float32 if dtype == DTYPE_F32 else torch.bfloat16
-    device = None
-    for name, (t, shape) in named.items():
-        if t is None:
-            continue
-        if not t.is_cuda:
-            raise ValueError(f"{name}: not a CUDA tensor (there is no CPU path)")
-        device = t.device if device is None else device
-        if t.device != device:
-            raise ValueError(f"{name}: on {t.device}, the other tensors on {device}")
-        if t.dtype != want:
-            raise ValueError(f"{name}: {t.dtype}, expected {want}")
-        if tuple(t.shape) != shape:
-            raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {shape}")
-        if t.stride(-1) != 1 and t.shape[-1] > 1:
-            raise ValueError(f"{name}: the last dimension must be contiguous")
-    here = torch.cuda.current_device() == device.index
+_torch_module = None
+
+
+def _op_type(dtype):
+    """torch, and the element type of a call's tensors."""
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    if dtype == DTYPE_BF16:
+        return _torch_module, _torch_module.bfloat16
+    if dtype == DTYPE_F32:
+        return _torch_module, _torch_module.float32
+    raise EpdError(EPD_EINVAL, "dtype")
+
+
+def _expect(name, t, want, device, shape):
+    """A tensor of a call: on the call's device, of its element type and shape, rows contiguous."""
+    if t.dtype is want and t.device == device and t.shape == shape and (t.stride(-1) == 1 or shape[-1] <= 1):
+        return
+    if not t.is_cuda:
+        raise ValueError(f"{name}: not a CUDA tensor (there is no CPU path)")
+    raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}, "
+                     f"expected {want} {tuple(shape)} on {device}, the last dimension contiguous")
+
+
+def _launch_on(torch, device, stream):
+    """(context, stream pointer) of a call: the launch belongs on the tensors' device, whichever is current."""
+    if device.type != "cuda":
+        raise ValueError("not a CUDA tensor (there is no CPU path)")
     if stream is None:
         stream = torch.cuda.current_stream(device)
     elif stream.device != device:
         raise ValueError(f"stream on {stream.device}, tensors on {device}")
-    return torch, want, (contextlib.nullcontext() if here else torch.cuda.device(device)), stream.cuda_stream
+    here = torch.cuda.current_device() == device.index
+    return (_HERE if here else torch.cuda.device(device)), stream.cuda_stream
+
+
+_HERE = contextlib.nullcontext()
 
 
 def _ld(t, cols) -> int:
@@ -663,21 +673,24 @@ def _ld(t, cols) -> int:
     return cols if t is None or t.shape[0] <= 1 else t.stride(0)
 
 
-def _out_tensor(name, t, shape, dtype, device):
-    if t.dtype != dtype or tuple(t.shape) != shape or t.device != device or (t.stride(-1) != 1 and shape[-1] > 1):
-        raise ValueError(f"{name}: expected {dtype} {shape} on {device}, rows contiguous")
-    return t
-
-
 def op_gated_linear(dtype, x, w, bias, gate, out=None, pre=None, stream=None):
     """act(x . w[:N]^T + bias[:N]) * (x . w[N:]^T + bias[N:]) for w [2N, K]; `pre` [M, 2N] receives both projections."""
     M, K = x.shape
     N = w.shape[0] // 2
-    torch, want, device, sp = _op_context(dtype, {"x": (x, (M, K)), "w": (w, (2 * N, K)), "bias": (bias, (2 * N,)),
-                                                  "out": (out, (M, N)), "pre": (pre, (M, 2 * N))}, stream)
+    torch, want = _op_type(dtype)
+    dev = x.device
+    ctx, sp = _launch_on(torch, dev, stream)
+    _expect("x", x, want, dev, (M, K))
+    _expect("w", w, want, dev, (2 * N, K))
+    if bias is not None:
+        _expect("bias", bias, want, dev, (2 * N,))
+    if pre is not None:
+        _expect("pre", pre, want, dev, (M, 2 * N))
     if out is None:
-        out = torch.empty((M, N), dtype=want, device=x.device)
-    with device:
+        out = torch.empty((M, N), dtype=want, device=dev)
+    else:
+        _expect("out", out, want, dev, (M, N))
+    with ctx:
         _check(load_library().epd_op_gated_linear(dtype, _ptr(x), _ld(x, K), _ptr(w), _ld(w, K), _ptr(bias), _ptr(out),
                                                   _ld(out, N), _ptr(pre), _ld(pre, 2 * N), M, N, K, gate, sp),
                "epd_op_gated_linear")
@@ -690,21 +703,32 @@ def op_gated_mlp(dtype, x, w_in, b_in, w_out, b_out, gate, out=None, hidden=None
     op_gated_mlp_backward takes.  flags: LINEAR_ACCUMULATE adds into a float `out` (which has to be given)."""
     M, K = x.shape
     N, D = w_in.shape[0] // 2, w_out.shape[0]
-    torch, want, device, sp = _op_context(
-        dtype, {"x": (x, (M, K)), "w_in": (w_in, (2 * N, K)), "b_in": (b_in, (2 * N,)), "w_out": (w_out, (D, N)),
-                "b_out": (b_out, (D,)), "hidden": (hidden, (M, N)), "pre": (pre, (M, 2 * N))}, stream)
+    torch, want = _op_type(dtype)
+    dev = x.device
+    ctx, sp = _launch_on(torch, dev, stream)
+    _expect("x", x, want, dev, (M, K))
+    _expect("w_in", w_in, want, dev, (2 * N, K))
+    _expect("w_out", w_out, want, dev, (D, N))
+    if b_in is not None:
+        _expect("b_in", b_in, want, dev, (2 * N,))
+    if b_out is not None:
+        _expect("b_out", b_out, want, dev, (D,))
     out_type = torch.float32 if flags & (LINEAR_ACCUMULATE | LINEAR_OUT_F32) else want
-    if out is None:
-        if flags & LINEAR_ACCUMULATE:
-            raise ValueError("LINEAR_ACCUMULATE adds into `out`: give one")
-        out = torch.empty((M, D), dtype=out_type, device=x.device)
+    if out is not None:
+        _expect("out", out, out_type, dev, (M, D))
+    elif flags & LINEAR_ACCUMULATE:
+        raise ValueError("LINEAR_ACCUMULATE adds into `out`: give one")
     else:
-        _out_tensor("out", out, (M, D), out_type, x.device)
+        out = torch.empty((M, D), dtype=out_type, device=dev)
     if hidden is None:
-        hidden = torch.empty((M, N), dtype=want, device=x.device)
-    if pre is None and save:
-        pre = torch.empty((M, 2 * N), dtype=want, device=x.device)
-    with device:
+        hidden = torch.empty((M, N), dtype=want, device=dev)
+    else:
+        _expect("hidden", hidden, want, dev, (M, N))
+    if pre is not None:
+        _expect("pre", pre, want, dev, (M, 2 * N))
+    elif save:
+        pre = torch.empty((M, 2 * N), dtype=want, device=dev)
+    with ctx:
         _check(load_library().epd_op_gated_mlp(
             dtype, _ptr(x), _ld(x, K), _ptr(w_in), _ld(w_in, K), _ptr(b_in), _ptr(w_out), _ld(w_out, N), _ptr(b_out),
             _ptr(hidden), _ld(hidden, N), _ptr(pre), _ld(pre, 2 * N), _ptr(out), _ld(out, D), M, N, K, D, gate, flags, sp),
@@ -717,9 +741,11 @@ def op_gated_mlp_backward(dtype, dout, x, w_in, w_out, hidden, pre, gate, bias=T
     """Gradients of op_gated_mlp: {"dx", "dw_in", "dw_out", "db_in", "db_out"} (those asked for)."""
     M, K = x.shape
     N, D = w_in.shape[0] // 2, w_out.shape[0]
-    torch, want, device, sp = _op_context(
-        dtype, {"dout": (dout, (M, D)), "x": (x, (M, K)), "w_in": (w_in, (2 * N, K)), "w_out": (w_out, (D, N)),
-                "hidden": (hidden, (M, N)), "pre": (pre, (M, 2 * N))}, stream)
+    torch, want = _op_type(dtype)
+    ctx, sp = _launch_on(torch, x.device, stream)
+    for name, t, shape in (("dout", dout, (M, D)), ("x", x, (M, K)), ("w_in", w_in, (2 * N, K)), ("w_out", w_out, (D, N)),
+                           ("hidden", hidden, (M, N)), ("pre", pre, (M, 2 * N))):
+        _expect(name, t, want, x.device, shape)
     g = {}
     if need_dx:
         g["dx"] = torch.empty((M, K), dtype=want, device=x.device)
@@ -732,7 +758,7 @@ def op_gated_mlp_backward(dtype, dout, x, w_in, w_out, hidden, pre, gate, bias=T
     lib = load_library()
     nbytes = lib.epd_gated_mlp_backward_workspace_bytes(dtype, M, N, D)
     workspace = _workspace(torch, workspace, nbytes, x.device)
-    with device:
+    with ctx:
         _check(lib.epd_op_gated_mlp_backward(
             dtype, _ptr(dout), _ld(dout, D), _ptr(x), _ld(x, K), _ptr(w_in), _ld(w_in, K), _ptr(w_out), _ld(w_out, N),
             _ptr(hidden), _ld(hidden, N), _ptr(pre), _ld(pre, 2 * N), _ptr(g.get("dx")), K, _ptr(g.get("dw_in")), K,
@@ -753,7 +779,10 @@ def op_linear_backward(dtype, dout, x, w, bias=True, need_dx=True, need_dw=True,
     """Gradients of a linear layer x . w^T + bias: {"dx", "dw", "db"} (those asked for)."""
     M, K = x.shape
     N = w.shape[0]
-    torch, want, device, sp = _op_context(dtype, {"dout": (dout, (M, N)), "x": (x, (M, K)), "w": (w, (N, K))}, stream)
+    torch, want = _op_type(dtype)
+    ctx, sp = _launch_on(torch, x.device, stream)
+    for name, t, shape in (("dout", dout, (M, N)), ("x", x, (M, K)), ("w", w, (N, K))):
+        _expect(name, t, want, x.device, shape)
     g = {}
     if need_dx:
         g["dx"] = torch.empty((M, K), dtype=want, device=x.device)
@@ -763,7 +792,7 @@ def op_linear_backward(dtype, dout, x, w, bias=True, need_dx=True, need_dw=True,
         g["db"] = torch.empty(N, dtype=want, device=x.device)
     lib = load_library()
     workspace = _workspace(torch, workspace, lib.epd_linear_backward_workspace_bytes(dtype, M, N), x.device)
-    with device:
+    with ctx:
         _check(lib.epd_op_linear_backward(
             dtype, _ptr(dout), _ld(dout, N), _ptr(x), _ld(x, K), _ptr(w), _ld(w, K), _ptr(g.get("dx")), K,
             _ptr(g.get("dw")), K, _ptr(g.get("db")), _ptr(workspace), workspace.numel() * workspace.element_size(), M, N,
@@ -773,9 +802,8 @@ def op_linear_backward(dtype, dout, x, w, bias=True, need_dx=True, need_dw=True,
 
 # ---- rotary embedding with several axes ---------------------------------------------------------------
 
-def _check_positions(pos, T, n_axes, device) -> int:
-    import torch
-    if pos.dtype != torch.int32 or tuple(pos.shape) != (n_axes, T) or pos.device != device or \
+def _check_positions(torch, pos, T, n_axes, device) -> int:
+    if pos.dtype is not torch.int32 or pos.shape != (n_axes, T) or pos.device != device or \
             (T > 1 and pos.stride(1) != 1):
         raise ValueError(f"pos: expected int32 {(n_axes, T)} on {device}, each axis contiguous")
     return max(T, pos.stride(0)) if n_axes > 1 else T
@@ -784,17 +812,22 @@ def _check_positions(pos, T, n_axes, device) -> int:
 def op_rope_axes(dtype, x, pos, sections, layout, theta, scale=1.0, inverse=False, out=None, stream=None):
     """Rotates x [T, heads, head_dim] (any token and head strides) by int32 positions pos [axes, T]; `out` may be x."""
     T, heads, dh = x.shape
-    torch, want, device, sp = _op_context(dtype, {"x": (x, (T, heads, dh)), "out": (out, (T, heads, dh))}, stream)
+    torch, want = _op_type(dtype)
+    dev = x.device
+    ctx, sp = _launch_on(torch, dev, stream)
+    _expect("x", x, want, dev, x.shape)
     n = len(sections)
-    ps = _check_positions(pos, T, n, x.device)
+    ps = _check_positions(torch, pos, T, n, dev)
     if out is None:
-        out = torch.empty((T, heads, dh), dtype=want, device=x.device)
+        out = torch.empty((T, heads, dh), dtype=want, device=dev)
+    else:
+        _expect("out", out, want, dev, x.shape)
 
     def strides(t):                     # one token or one head may have any stride
         head = t.stride(1) if heads > 1 else dh
         return (t.stride(0) if T > 1 else 0), head
     (xt, xh), (ot, oh) = strides(x), strides(out)
-    with device:
+    with ctx:
         _check(load_library().epd_op_rope_axes(dtype, _ptr(x), xt, xh, _ptr(pos), ps, _ptr(out), ot, oh, T, heads, dh,
                                                (ctypes.c_int32 * n)(*sections), n, layout, theta, scale, int(inverse),
                                                sp), "epd_op_rope_axes")
@@ -804,12 +837,14 @@ def op_rope_axes(dtype, x, pos, sections, layout, theta, scale=1.0, inverse=Fals
 def op_rope_axes_split(dtype, qkv, pos, heads, head_dim, sections, layout, theta, q_scale, stream=None):
     """Packed qkv [T, 3*heads*head_dim] -> rotated head-major padded q, k, v, ready for op_attention."""
     T = qkv.shape[0]
-    torch, want, device, sp = _op_context(dtype, {"qkv": (qkv, (T, 3 * heads * head_dim))}, stream)
+    torch, want = _op_type(dtype)
+    ctx, sp = _launch_on(torch, qkv.device, stream)
+    _expect("qkv", qkv, want, qkv.device, (T, 3 * heads * head_dim))
     n = len(sections)
-    ps = _check_positions(pos, T, n, qkv.device)
+    ps = _check_positions(torch, pos, T, n, qkv.device)
     dhp = (head_dim + 15) // 16 * 16
     q, k, v = (torch.empty((heads, T, dhp), dtype=want, device=qkv.device) for _ in range(3))
-    with device:
+    with ctx:
         _check(load_library().epd_op_rope_axes_split(
             dtype, _ptr(qkv), _ld(qkv, 3 * heads * head_dim), _ptr(pos), ps, _ptr(q), _ptr(k), _ptr(v), T, heads, head_dim,
             (ctypes.c_int32 * n)(*sections), n, layout, theta, q_scale, sp), "epd_op_rope_axes_split")
@@ -821,15 +856,16 @@ def op_rope_axes_split_backward(dtype, dq, dk, dv, pos, head_dim, sections, layo
     heads, T, dhp = dq.shape
     if dhp != (head_dim + 15) // 16 * 16:
         raise ValueError(f"head width {dhp} is not the padded width of head_dim {head_dim}")
-    torch, want, device, sp = _op_context(dtype, {n: (t, (heads, T, dhp)) for n, t in
-                                                  (("dq", dq), ("dk", dk), ("dv", dv))}, stream)
-    for t in (dq, dk, dv):
+    torch, want = _op_type(dtype)
+    ctx, sp = _launch_on(torch, dq.device, stream)
+    for name, t in (("dq", dq), ("dk", dk), ("dv", dv)):
+        _expect(name, t, want, dq.device, dq.shape)
         if not t.is_contiguous():
-            raise ValueError("dq, dk, dv must be contiguous")
+            raise ValueError(f"{name} must be contiguous")
     n = len(sections)
-    ps = _check_positions(pos, T, n, dq.device)
+    ps = _check_positions(torch, pos, T, n, dq.device)
     dqkv = torch.empty((T, 3 * heads * head_dim), dtype=want, device=dq.device)
-    with device:
+    with ctx:
         _check(load_library().epd_op_rope_axes_split_backward(
             dtype, _ptr(dq), _ptr(dk), _ptr(dv), _ptr(pos), ps, _ptr(dqkv), 3 * heads * head_dim, T, heads, head_dim,
             (ctypes.c_int32 * n)(*sections), n, layout, theta, q_scale, sp), "epd_op_rope_axes_split_backward")

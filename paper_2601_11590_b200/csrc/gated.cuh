@@ -105,4 +105,13 @@ cudaError_t gated_tc_gradient(const void* dout, int64_t lddo, const void* w_out,
 cudaError_t matmul_tc(bool a_mn, const void* a, int64_t lda, const void* b, int64_t ldb, void* out, int64_t ldo, int64_t M,
                       int64_t N, int64_t K, cudaStream_t s);
 
+// ---- one token to kFewRows tokens (gated_few_rows.cu) -------------------------------------------
+constexpr int kFewRows = 32;
+cudaError_t gated_few_rows(const void* x, int64_t ldx, const void* w, int64_t ldw, const void* bias, void* out, int64_t ldo,
+                           void* pre, int64_t ldp, int64_t M, int64_t N, int64_t K, int gate, cudaStream_t s);
+// out[M, N] = x . w^T + bias; flags EPD_LINEAR_ACCUMULATE / EPD_LINEAR_OUT_F32.  behind_gated: the kernel in front on the
+// stream is gated_few_rows.
+cudaError_t linear_few_rows(const void* x, int64_t ldx, const void* w, int64_t ldw, const void* bias, void* out, int64_t ldo,
+                            int64_t M, int64_t N, int64_t K, int flags, bool behind_gated, cudaStream_t s);
+
 }  // namespace epd

@@ -182,8 +182,15 @@ cudaError_t column_sum(int dtype, const void* x, int64_t ldx, int64_t M, int64_t
 // =============================================================================================
 // The products of the block, each on the kernel that takes its shape
 // =============================================================================================
+// Few rows: what the kernels that stream the weights can load in 16-byte pieces.
+bool few_rows(int dtype, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t M, int64_t K) {
+  return dtype == EPD_DTYPE_BF16 && M <= kFewRows && K % 8 == 0 && ldx % 8 == 0 && ldw % 8 == 0 &&
+         (((uintptr_t)x | (uintptr_t)w) & 15) == 0;
+}
+
 cudaError_t gated_linear(int dtype, const void* x, int64_t ldx, const void* w, int64_t ldw, const void* bias, void* out,
                          int64_t ldo, void* pre, int64_t ldp, int64_t M, int64_t N, int64_t K, int gate, cudaStream_t s) {
+  if (few_rows(dtype, x, ldx, w, ldw, M, K)) return gated_few_rows(x, ldx, w, ldw, bias, out, ldo, pre, ldp, M, N, K, gate, s);
   if (dtype == EPD_DTYPE_BF16 && gated_tc_supported({{x, ldx}, {w, ldw}, {out, ldo}, {pre, ldp}}, {N, K}))
     return gated_tc_forward(x, ldx, w, ldw, bias, out, ldo, pre, ldp, M, N, K, gate, nullptr, s);
   FmaArgs p = {};
@@ -297,6 +304,9 @@ int epd_op_gated_mlp(int32_t dtype, const void* x, int64_t ldx, const void* w_in
     return EPD_EINVAL;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   EPD_TRY(gated_linear(dtype, x, ldx, w_in, ldw_in, b_in, hidden, ldh, pre, ldp, M, N, K, gate, s));
+  if (few_rows(dtype, hidden, ldh, w_out, ldw_out, M, N))
+    return finish(linear_few_rows(hidden, ldh, w_out, ldw_out, b_out, out, ldo, M, D, N, flags,
+                                  few_rows(dtype, x, ldx, w_in, ldw_in, M, K), s));
   return epd_op_linear(dtype, hidden, ldh, w_out, ldw_out, b_out, out, ldo, M, D, N, flags, stream);
 }
 
