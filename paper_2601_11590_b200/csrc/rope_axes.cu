@@ -14,7 +14,7 @@
 // so keeps its fraction of a turn to 2^-26.
 #include <math.h>
 
-#include "common.cuh"
+#include "tcgen05_common.cuh"
 
 namespace epd {
 namespace {
@@ -38,6 +38,7 @@ struct AxesArgs {
   int rotate[3];
   int n_tensors, heads, dh;
   int pad;                          // elements behind head_dim that the destination rows carry (written), or 0
+  int src_pad;                      // elements behind head_dim that the source rows carry (not used), or 0
   int64_t src_token, src_head, dst_token, dst_head;   // strides in elements
   const int32_t* pos;
   int64_t pos_stride;
@@ -154,6 +155,164 @@ rope_axes_kernel(const __grid_constant__ AxesPlan plan, const __grid_constant__ 
   }
 }
 
+// Two float operations in one instruction.
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t&>(r))
+      : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)));
+  return r;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(reinterpret_cast<uint64_t&>(r))
+      : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)), "l"(reinterpret_cast<uint64_t&>(c)));
+  return r;
+}
+__device__ __forceinline__ float2 unpack2(const float* p) { return make_float2(p[0], p[1]); }
+__device__ __forceinline__ float2 unpack2(const __nv_bfloat16* p) {
+  return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(p));
+}
+__device__ __forceinline__ void pack2(float* p, float2 v) { p[0] = v.x; p[1] = v.y; }
+__device__ __forceinline__ void pack2(__nv_bfloat16* p, float2 v) {
+  *reinterpret_cast<__nv_bfloat162*>(p) = __floats2bfloat162_rn(v.x, v.y);
+}
+
+// The same through shared memory: a block brings the rows of a few tokens in with 16-byte asynchronous copies, and every
+// thread writes whole 16-byte pieces of the destination, reading its own piece and the partners' elements (PW at a time)
+// from shared memory.  Global memory then sees full pieces in both directions whatever the sections, where the kernel above
+// reads and writes runs of U elements: 81628 tokens of 16 heads x 72 with sections of 12 took it 556 us.  A thread keeps its
+// token and its piece of the head, so the cosines and sines of the piece sit in its registers for all heads and tensors.
+constexpr int kStagedThreads = 320;
+struct Staging {
+  int tok;                          // tokens of a block
+  int pieces;                       // 16-byte pieces of a destination row of one head
+  int groups;                       // threads that share a (token, piece) and deal the heads among themselves
+  int head_major;                   // the source holds a head's tokens together
+  int copy_pieces;                  // 16-byte pieces of one contiguous stretch of the source
+  int copies;                       // stretches of a block; row-major: one per token, head-major: one per tensor and head
+  int s_token, s_head, s_tensor;    // strides in shared memory, elements
+};
+
+template <typename T, int PW>
+__global__ void __launch_bounds__(kStagedThreads, sizeof(T) == 2 && PW == 1 ? 3 : 4)
+rope_axes_staged_kernel(const __grid_constant__ AxesPlan plan, const __grid_constant__ AxesArgs a,
+                        const __grid_constant__ Staging g) {
+  pdl_launch_dependents();
+  pdl_wait();
+  constexpr int VEC = 16 / (int)sizeof(T);
+  extern __shared__ __align__(16) uint8_t staged[];
+  float2* s_cs = reinterpret_cast<float2*>(staged);
+  T* s_x = reinterpret_cast<T*>(staged + (size_t)g.tok * plan.pairs * sizeof(float2) + (g.tok * plan.pairs % 2) * sizeof(float2));
+  const int64_t j0 = (int64_t)blockIdx.x * g.tok;
+  const int ntok = (int)min((int64_t)g.tok, a.T - j0);
+  // stretch i of the block -> shared memory, back to back
+  const int stretches = g.head_major ? g.copies : ntok;
+  const int full = g.copy_pieces, part = g.head_major ? ntok * (g.copy_pieces / g.tok) : g.copy_pieces;
+  for (int i = threadIdx.x; i < stretches * part; i += blockDim.x) {
+    const int n = i / part, v = i - n * part;
+    const T* src;
+    if (g.head_major) {
+      const int w = n / a.heads, h = n - w * a.heads;
+      src = static_cast<const T*>(w == 0 ? a.src[0] : w == 1 ? a.src[1] : a.src[2]) + h * a.src_head + j0 * a.src_token;
+    } else {
+      src = static_cast<const T*>(a.src[0]) + (j0 + n) * a.src_token;
+    }
+    const uint32_t to = (uint32_t)__cvta_generic_to_shared(s_x + ((size_t)n * full + v) * VEC);
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(src + v * VEC) : "memory");
+  }
+  asm volatile("cp.async.commit_group;" ::: "memory");
+  for (int i = threadIdx.x; i < ntok * plan.pairs; i += blockDim.x) {
+    const int t = i / plan.pairs, p = i - t * plan.pairs;
+    const int32_t pos = a.pos[plan.axis[p] * a.pos_stride + j0 + t];
+    const double turns = (double)pos * plan.turns[p];
+    float sn, cs;
+    sincospif(2.0f * (float)(turns - rint(turns)), &sn, &cs);
+    s_cs[i] = make_float2(cs, a.sign * sn);
+  }
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
+  __syncthreads();
+
+  const int per_group = g.tok * g.pieces;
+  const int group = threadIdx.x / per_group;
+  const int within = threadIdx.x - group * per_group;
+  const int t = within / g.pieces, d0 = (within - t * g.pieces) * VEC;
+  if (group >= g.groups || t >= ntok) return;
+  int partner[VEC / PW];              // distance to the partners of a group of PW elements; 0: not rotated
+  int angle[VEC / PW];                // where the group's angles begin in s_cs
+#pragma unroll
+  for (int u = 0; u < VEC / PW; ++u) {
+    const int d = d0 + u * PW;
+    partner[u] = angle[u] = 0;
+    if (d < 2 * plan.pairs) {
+      int r = 0;
+      while (d >= plan.run_base[r] + 2 * plan.run_len[r]) ++r;
+      const int len = plan.run_len[r], f = d - plan.run_base[r];
+      partner[u] = f < len ? len : -len;
+      angle[u] = t * plan.pairs + plan.run_pair[r] + (f < len ? f : f - len);
+    }
+  }
+  const T* sx = s_x + t * g.s_token + d0 + group * g.s_head;
+  const bool padding = d0 >= a.dh;
+  const int s_step = g.groups * g.s_head;
+  const int64_t d_step = g.groups * a.dst_head;
+  for (int w = 0; w < a.n_tensors; ++w, sx += g.s_tensor) {
+    T* dst = static_cast<T*>(w == 0 ? a.dst[0] : w == 1 ? a.dst[1] : a.dst[2]) + (j0 + t) * a.dst_token + group * a.dst_head + d0;
+    const T* s = sx;
+    if (padding) {
+      // column head_dim of v is 1 (the rest of the padding 0): the attention step's P V then yields the row sums
+      alignas(16) T x[VEC];
+      const bool one = w == 2;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) x[e] = from_float<T>(one && d0 + e == a.dh ? 1.0f : 0.0f);
+      for (int h = group; h < a.heads; h += g.groups, dst += d_step) store_vec<T, VEC>(dst, x);
+    } else if (w == 2) {
+#pragma unroll 2
+      for (int h = group; h < a.heads; h += g.groups, dst += d_step, s += s_step) {
+        alignas(16) T x[VEC];
+        load_vec<T, VEC>(s, x);
+        store_vec<T, VEC>(dst, x);
+      }
+    } else {
+      const float sc = w == 0 ? a.scale[0] : a.scale[1];
+      float2 c2[VEC / 2], s2[VEC / 2];
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) {
+        const int u = k / PW;
+        float2 v = make_float2(1.0f, 0.0f);
+        if (partner[u] != 0) {
+          v = s_cs[angle[u] + k % PW];
+          if (partner[u] > 0) v.y = -v.y;
+        }
+        (k & 1 ? c2[k / 2].y : c2[k / 2].x) = v.x * sc;
+        (k & 1 ? s2[k / 2].y : s2[k / 2].x) = v.y * sc;
+      }
+#pragma unroll 2
+      for (int h = group; h < a.heads; h += g.groups, dst += d_step, s += s_step) {
+        alignas(16) T x[VEC], y[VEC];
+        load_vec<T, VEC>(s, x);
+#pragma unroll
+        for (int u = 0; u < VEC / PW; ++u) {
+          T part[PW];
+          if (partner[u] != 0) {
+            load_vec<T, PW>(s + u * PW + partner[u], part);
+          } else {
+#pragma unroll
+            for (int e = 0; e < PW; ++e) part[e] = from_float<T>(0.0f);
+          }
+#pragma unroll
+          for (int e = 0; e < PW; ++e) y[u * PW + e] = part[e];
+        }
+#pragma unroll
+        for (int e = 0; e < VEC / 2; ++e) {
+          const float2 r = fma2(unpack2(x + 2 * e), c2[e], mul2(unpack2(y + 2 * e), s2[e]));
+          pack2(x + 2 * e, r);
+        }
+        store_vec<T, VEC>(dst, x);
+      }
+    }
+  }
+}
+
 // False if the description is not one of a head_dim-wide head.
 bool make_plan(AxesPlan* p, int head_dim, const int32_t* sections, int n_axes, int layout, float theta) {
   if (n_axes < 1 || n_axes > kMaxAxes || !sections || !isfinite(theta)) return false;
@@ -227,10 +386,90 @@ cudaError_t launch(const AxesPlan& p, const AxesArgs& a, cudaStream_t s) {
                     0, s, p, a, tok, slots, groups);
 }
 
+// Shared memory a block of the staged kernel may take: four blocks on an SM.
+constexpr size_t kStagedBytes = 54 * 1024;
+
+// The staged kernel takes whole 16-byte pieces: every contiguous stretch of the source and every row of the destination
+// starts on a 16-byte boundary and is a multiple of 16 bytes long, and there are tokens enough for a block on every SM
+// (below that the register kernel, which deals heads to blocks, has the shorter latency: one token 3.4 us).
+template <typename T>
+bool plan_staging(const AxesArgs& a, const AxesPlan& p, Staging* g, size_t* bytes) {
+  constexpr int VEC = 16 / (int)sizeof(T);
+  if (a.dh % VEC || a.pad % VEC || a.src_token % VEC || a.src_head % VEC || a.dst_token % VEC || a.dst_head % VEC) return false;
+  for (int i = 0; i < a.n_tensors; ++i)
+    if (((uintptr_t)a.src[i] | (uintptr_t)a.dst[i]) & 15) return false;
+  // row-major: a token's tensors and heads lie back to back; head-major: a head's tokens do
+  bool row = a.heads == 1 || a.src_head == a.dh;
+  for (int i = 1; i < a.n_tensors; ++i)
+    row = row && static_cast<const char*>(a.src[i]) ==
+                     static_cast<const char*>(a.src[0]) + (size_t)i * a.heads * a.dh * sizeof(T);
+  const int src_row = a.dh + a.src_pad;
+  if (!row && a.src_token != src_row) return false;
+  g->head_major = !row;
+  const int row_elems = row ? a.dh : src_row;
+  const int64_t token_bytes = (int64_t)a.n_tensors * a.heads * row_elems * (int)sizeof(T) + p.pairs * 8;
+  if (token_bytes > (int64_t)kStagedBytes) return false;
+  int tok = (int)(kStagedBytes / token_bytes);
+  tok = tok > kMaxTokens ? kMaxTokens : tok;
+  while (tok > 1 && a.T < (int64_t)tok * 2 * 148) --tok;
+  if (a.T < (int64_t)tok * 148) return false;
+  g->tok = tok;
+  g->pieces = (a.dh + a.pad) / VEC;
+  const int per_group = tok * g->pieces;
+  const int most = kStagedThreads / per_group > 0 ? kStagedThreads / per_group : 1;
+  const int rounds = (a.heads + most - 1) / most;
+  g->groups = (a.heads + rounds - 1) / rounds;      // no more than the rounds need
+  if (row) {
+    g->copies = tok;
+    g->copy_pieces = a.n_tensors * a.heads * a.dh / VEC;
+    g->s_token = a.n_tensors * a.heads * a.dh;
+    g->s_head = a.dh;
+    g->s_tensor = a.heads * a.dh;
+  } else {
+    g->copies = a.n_tensors * a.heads;
+    g->copy_pieces = tok * src_row / VEC;
+    g->s_token = src_row;
+    g->s_head = tok * src_row;
+    g->s_tensor = a.heads * tok * src_row;
+  }
+  *bytes = (size_t)tok * (size_t)token_bytes + 16;
+  return true;
+}
+
+template <typename T, int PW>
+cudaError_t launch_staged(const AxesPlan& p, const AxesArgs& a, const Staging& g, size_t bytes, cudaStream_t s) {
+  auto kern = rope_axes_staged_kernel<T, PW>;
+  static PerDeviceOnce configured;
+  cudaError_t e = once_per_device(configured, [&] {
+    return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kStagedBytes + 64);
+  });
+  if (e != cudaSuccess) return e;
+  const int64_t blocks = (a.T + g.tok - 1) / g.tok;
+  const int threads = (g.tok * g.pieces * g.groups + 31) / 32 * 32;
+  return launch_pdl(kern, dim3((unsigned)blocks), dim3(threads), bytes, s, p, a, g);
+}
+
 // Widest vector that every run, every stride and every pointer allows.
 cudaError_t dispatch(int dtype, const AxesPlan& p, const AxesArgs& a, cudaStream_t s) {
   if (a.T == 0) return cudaSuccess;
   const int es = dtype == EPD_DTYPE_F32 ? 4 : 2;
+  // elements that share a run and its partners' run: the width of a partner access
+  int pw = 16 / es;
+  for (int r = 0; r < p.n_runs; ++r)
+    while (p.run_len[r] % pw || p.run_base[r] % pw) pw >>= 1;
+  Staging g;
+  size_t bytes = 0;
+  if (dtype == EPD_DTYPE_F32 ? plan_staging<float>(a, p, &g, &bytes) : plan_staging<__nv_bfloat16>(a, p, &g, &bytes)) {
+    if (dtype == EPD_DTYPE_F32) {
+      if (pw == 4) return launch_staged<float, 4>(p, a, g, bytes, s);
+      if (pw == 2) return launch_staged<float, 2>(p, a, g, bytes, s);
+      return launch_staged<float, 1>(p, a, g, bytes, s);
+    }
+    if (pw == 8) return launch_staged<__nv_bfloat16, 8>(p, a, g, bytes, s);
+    if (pw == 4) return launch_staged<__nv_bfloat16, 4>(p, a, g, bytes, s);
+    if (pw == 2) return launch_staged<__nv_bfloat16, 2>(p, a, g, bytes, s);
+    return launch_staged<__nv_bfloat16, 1>(p, a, g, bytes, s);
+  }
   int u = 16 / es;
   auto fits = [&](int w) {
     for (int r = 0; r < p.n_runs; ++r)
@@ -371,6 +610,7 @@ int epd_op_rope_axes_split_backward(int32_t dtype, const void* dq, const void* d
   a.n_tensors = 3;
   a.heads = heads;
   a.dh = head_dim;
+  a.src_pad = dhp - head_dim;
   a.src_token = dhp;
   a.src_head = T * dhp;
   a.dst_token = lddqkv;
