@@ -7,7 +7,6 @@ an op requires the compiled library and a CUDA device.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import os
 from typing import Dict, List, Optional, Sequence
@@ -653,19 +652,30 @@ def _expect(name, t, want, device, shape):
                      f"expected {want} {tuple(shape)} on {device}, the last dimension contiguous")
 
 
-def _launch_on(torch, device, stream):
-    """(context, stream pointer) of a call: the launch belongs on the tensors' device, whichever is current."""
+def _raw_stream(torch, device) -> int:
+    """Pointer of the device's current stream.  torch.cuda.current_stream() builds a stream object on the way (2 us of the
+    10 us that a call of one token costs on the host), so the pointer is taken directly where torch offers it."""
+    get = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return get(device.index) if get is not None else torch.cuda.current_stream(device).cuda_stream
+
+
+def _launch(torch, device, stream, fn, what, *args):
+    """fn(*args, stream) with the tensors' device current, whichever was."""
     if device.type != "cuda":
         raise ValueError("not a CUDA tensor (there is no CPU path)")
     if stream is None:
-        stream = torch.cuda.current_stream(device)
+        sp = _raw_stream(torch, device)
     elif stream.device != device:
         raise ValueError(f"stream on {stream.device}, tensors on {device}")
-    here = torch.cuda.current_device() == device.index
-    return (_HERE if here else torch.cuda.device(device)), stream.cuda_stream
-
-
-_HERE = contextlib.nullcontext()
+    else:
+        sp = stream.cuda_stream
+    if torch.cuda.current_device() == device.index:
+        status = fn(*args, sp)
+    else:
+        with torch.cuda.device(device):
+            status = fn(*args, sp)
+    if status != EPD_OK:
+        raise EpdError(status, what)
 
 
 def _ld(t, cols) -> int:
@@ -679,7 +689,6 @@ def op_gated_linear(dtype, x, w, bias, gate, out=None, pre=None, stream=None):
     N = w.shape[0] // 2
     torch, want = _op_type(dtype)
     dev = x.device
-    ctx, sp = _launch_on(torch, dev, stream)
     _expect("x", x, want, dev, (M, K))
     _expect("w", w, want, dev, (2 * N, K))
     if bias is not None:
@@ -690,10 +699,8 @@ def op_gated_linear(dtype, x, w, bias, gate, out=None, pre=None, stream=None):
         out = torch.empty((M, N), dtype=want, device=dev)
     else:
         _expect("out", out, want, dev, (M, N))
-    with ctx:
-        _check(load_library().epd_op_gated_linear(dtype, _ptr(x), _ld(x, K), _ptr(w), _ld(w, K), _ptr(bias), _ptr(out),
-                                                  _ld(out, N), _ptr(pre), _ld(pre, 2 * N), M, N, K, gate, sp),
-               "epd_op_gated_linear")
+    _launch(torch, dev, stream, load_library().epd_op_gated_linear, "epd_op_gated_linear", dtype, _ptr(x), _ld(x, K), _ptr(w),
+            _ld(w, K), _ptr(bias), _ptr(out), _ld(out, N), _ptr(pre), _ld(pre, 2 * N), M, N, K, gate)
     return out
 
 
@@ -705,7 +712,6 @@ def op_gated_mlp(dtype, x, w_in, b_in, w_out, b_out, gate, out=None, hidden=None
     N, D = w_in.shape[0] // 2, w_out.shape[0]
     torch, want = _op_type(dtype)
     dev = x.device
-    ctx, sp = _launch_on(torch, dev, stream)
     _expect("x", x, want, dev, (M, K))
     _expect("w_in", w_in, want, dev, (2 * N, K))
     _expect("w_out", w_out, want, dev, (D, N))
@@ -728,11 +734,9 @@ def op_gated_mlp(dtype, x, w_in, b_in, w_out, b_out, gate, out=None, hidden=None
         _expect("pre", pre, want, dev, (M, 2 * N))
     elif save:
         pre = torch.empty((M, 2 * N), dtype=want, device=dev)
-    with ctx:
-        _check(load_library().epd_op_gated_mlp(
-            dtype, _ptr(x), _ld(x, K), _ptr(w_in), _ld(w_in, K), _ptr(b_in), _ptr(w_out), _ld(w_out, N), _ptr(b_out),
-            _ptr(hidden), _ld(hidden, N), _ptr(pre), _ld(pre, 2 * N), _ptr(out), _ld(out, D), M, N, K, D, gate, flags, sp),
-            "epd_op_gated_mlp")
+    _launch(torch, dev, stream, load_library().epd_op_gated_mlp, "epd_op_gated_mlp", dtype, _ptr(x), _ld(x, K), _ptr(w_in),
+            _ld(w_in, K), _ptr(b_in), _ptr(w_out), _ld(w_out, N), _ptr(b_out), _ptr(hidden), _ld(hidden, N), _ptr(pre),
+            _ld(pre, 2 * N), _ptr(out), _ld(out, D), M, N, K, D, gate, flags)
     return (out, hidden, pre) if save else out
 
 
@@ -742,7 +746,6 @@ def op_gated_mlp_backward(dtype, dout, x, w_in, w_out, hidden, pre, gate, bias=T
     M, K = x.shape
     N, D = w_in.shape[0] // 2, w_out.shape[0]
     torch, want = _op_type(dtype)
-    ctx, sp = _launch_on(torch, x.device, stream)
     for name, t, shape in (("dout", dout, (M, D)), ("x", x, (M, K)), ("w_in", w_in, (2 * N, K)), ("w_out", w_out, (D, N)),
                            ("hidden", hidden, (M, N)), ("pre", pre, (M, 2 * N))):
         _expect(name, t, want, x.device, shape)
@@ -758,12 +761,11 @@ def op_gated_mlp_backward(dtype, dout, x, w_in, w_out, hidden, pre, gate, bias=T
     lib = load_library()
     nbytes = lib.epd_gated_mlp_backward_workspace_bytes(dtype, M, N, D)
     workspace = _workspace(torch, workspace, nbytes, x.device)
-    with ctx:
-        _check(lib.epd_op_gated_mlp_backward(
-            dtype, _ptr(dout), _ld(dout, D), _ptr(x), _ld(x, K), _ptr(w_in), _ld(w_in, K), _ptr(w_out), _ld(w_out, N),
-            _ptr(hidden), _ld(hidden, N), _ptr(pre), _ld(pre, 2 * N), _ptr(g.get("dx")), K, _ptr(g.get("dw_in")), K,
-            _ptr(g.get("db_in")), _ptr(g.get("dw_out")), N, _ptr(g.get("db_out")), _ptr(workspace),
-            workspace.numel() * workspace.element_size(), M, N, K, D, gate, sp), "epd_op_gated_mlp_backward")
+    _launch(torch, x.device, stream, lib.epd_op_gated_mlp_backward, "epd_op_gated_mlp_backward", dtype, _ptr(dout),
+            _ld(dout, D), _ptr(x), _ld(x, K), _ptr(w_in), _ld(w_in, K), _ptr(w_out), _ld(w_out, N), _ptr(hidden),
+            _ld(hidden, N), _ptr(pre), _ld(pre, 2 * N), _ptr(g.get("dx")), K, _ptr(g.get("dw_in")), K, _ptr(g.get("db_in")),
+            _ptr(g.get("dw_out")), N, _ptr(g.get("db_out")), _ptr(workspace), workspace.numel() * workspace.element_size(), M,
+            N, K, D, gate)
     return g
 
 
@@ -780,7 +782,6 @@ def op_linear_backward(dtype, dout, x, w, bias=True, need_dx=True, need_dw=True,
     M, K = x.shape
     N = w.shape[0]
     torch, want = _op_type(dtype)
-    ctx, sp = _launch_on(torch, x.device, stream)
     for name, t, shape in (("dout", dout, (M, N)), ("x", x, (M, K)), ("w", w, (N, K))):
         _expect(name, t, want, x.device, shape)
     g = {}
@@ -792,11 +793,9 @@ def op_linear_backward(dtype, dout, x, w, bias=True, need_dx=True, need_dw=True,
         g["db"] = torch.empty(N, dtype=want, device=x.device)
     lib = load_library()
     workspace = _workspace(torch, workspace, lib.epd_linear_backward_workspace_bytes(dtype, M, N), x.device)
-    with ctx:
-        _check(lib.epd_op_linear_backward(
-            dtype, _ptr(dout), _ld(dout, N), _ptr(x), _ld(x, K), _ptr(w), _ld(w, K), _ptr(g.get("dx")), K,
-            _ptr(g.get("dw")), K, _ptr(g.get("db")), _ptr(workspace), workspace.numel() * workspace.element_size(), M, N,
-            K, sp), "epd_op_linear_backward")
+    _launch(torch, x.device, stream, lib.epd_op_linear_backward, "epd_op_linear_backward", dtype, _ptr(dout), _ld(dout, N),
+            _ptr(x), _ld(x, K), _ptr(w), _ld(w, K), _ptr(g.get("dx")), K, _ptr(g.get("dw")), K, _ptr(g.get("db")),
+            _ptr(workspace), workspace.numel() * workspace.element_size(), M, N, K)
     return g
 
 
@@ -814,7 +813,6 @@ def op_rope_axes(dtype, x, pos, sections, layout, theta, scale=1.0, inverse=Fals
     T, heads, dh = x.shape
     torch, want = _op_type(dtype)
     dev = x.device
-    ctx, sp = _launch_on(torch, dev, stream)
     _expect("x", x, want, dev, x.shape)
     n = len(sections)
     ps = _check_positions(torch, pos, T, n, dev)
@@ -827,10 +825,8 @@ def op_rope_axes(dtype, x, pos, sections, layout, theta, scale=1.0, inverse=Fals
         head = t.stride(1) if heads > 1 else dh
         return (t.stride(0) if T > 1 else 0), head
     (xt, xh), (ot, oh) = strides(x), strides(out)
-    with ctx:
-        _check(load_library().epd_op_rope_axes(dtype, _ptr(x), xt, xh, _ptr(pos), ps, _ptr(out), ot, oh, T, heads, dh,
-                                               (ctypes.c_int32 * n)(*sections), n, layout, theta, scale, int(inverse),
-                                               sp), "epd_op_rope_axes")
+    _launch(torch, dev, stream, load_library().epd_op_rope_axes, "epd_op_rope_axes", dtype, _ptr(x), xt, xh, _ptr(pos), ps,
+            _ptr(out), ot, oh, T, heads, dh, (ctypes.c_int32 * n)(*sections), n, layout, theta, scale, int(inverse))
     return out
 
 
@@ -838,16 +834,14 @@ def op_rope_axes_split(dtype, qkv, pos, heads, head_dim, sections, layout, theta
     """Packed qkv [T, 3*heads*head_dim] -> rotated head-major padded q, k, v, ready for op_attention."""
     T = qkv.shape[0]
     torch, want = _op_type(dtype)
-    ctx, sp = _launch_on(torch, qkv.device, stream)
     _expect("qkv", qkv, want, qkv.device, (T, 3 * heads * head_dim))
     n = len(sections)
     ps = _check_positions(torch, pos, T, n, qkv.device)
     dhp = (head_dim + 15) // 16 * 16
     q, k, v = (torch.empty((heads, T, dhp), dtype=want, device=qkv.device) for _ in range(3))
-    with ctx:
-        _check(load_library().epd_op_rope_axes_split(
-            dtype, _ptr(qkv), _ld(qkv, 3 * heads * head_dim), _ptr(pos), ps, _ptr(q), _ptr(k), _ptr(v), T, heads, head_dim,
-            (ctypes.c_int32 * n)(*sections), n, layout, theta, q_scale, sp), "epd_op_rope_axes_split")
+    _launch(torch, qkv.device, stream, load_library().epd_op_rope_axes_split, "epd_op_rope_axes_split", dtype, _ptr(qkv),
+            _ld(qkv, 3 * heads * head_dim), _ptr(pos), ps, _ptr(q), _ptr(k), _ptr(v), T, heads, head_dim,
+            (ctypes.c_int32 * n)(*sections), n, layout, theta, q_scale)
     return q, k, v
 
 
@@ -857,7 +851,6 @@ def op_rope_axes_split_backward(dtype, dq, dk, dv, pos, head_dim, sections, layo
     if dhp != (head_dim + 15) // 16 * 16:
         raise ValueError(f"head width {dhp} is not the padded width of head_dim {head_dim}")
     torch, want = _op_type(dtype)
-    ctx, sp = _launch_on(torch, dq.device, stream)
     for name, t in (("dq", dq), ("dk", dk), ("dv", dv)):
         _expect(name, t, want, dq.device, dq.shape)
         if not t.is_contiguous():
@@ -865,10 +858,9 @@ def op_rope_axes_split_backward(dtype, dq, dk, dv, pos, head_dim, sections, layo
     n = len(sections)
     ps = _check_positions(torch, pos, T, n, dq.device)
     dqkv = torch.empty((T, 3 * heads * head_dim), dtype=want, device=dq.device)
-    with ctx:
-        _check(load_library().epd_op_rope_axes_split_backward(
-            dtype, _ptr(dq), _ptr(dk), _ptr(dv), _ptr(pos), ps, _ptr(dqkv), 3 * heads * head_dim, T, heads, head_dim,
-            (ctypes.c_int32 * n)(*sections), n, layout, theta, q_scale, sp), "epd_op_rope_axes_split_backward")
+    _launch(torch, dq.device, stream, load_library().epd_op_rope_axes_split_backward, "epd_op_rope_axes_split_backward", dtype,
+            _ptr(dq), _ptr(dk), _ptr(dv), _ptr(pos), ps, _ptr(dqkv), 3 * heads * head_dim, T, heads, head_dim,
+            (ctypes.c_int32 * n)(*sections), n, layout, theta, q_scale)
     return dqkv
 
 

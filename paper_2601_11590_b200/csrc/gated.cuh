@@ -98,12 +98,29 @@ struct MatrixArg {
 // extent a multiple of 8.
 bool gated_tc_supported(std::initializer_list<MatrixArg> matrices, std::initializer_list<int64_t> extents);
 cudaError_t gated_tc_forward(const void* x, int64_t ldx, const void* w, int64_t ldw, const void* bias, void* out, int64_t ldo,
-                             void* pre, int64_t ldp, int64_t M, int64_t N, int64_t K, int gate, int* status, cudaStream_t s);
+                             void* pre, int64_t ldp, int64_t M, int64_t N, int64_t K, int gate, cudaStream_t s);
+// sums: [ceil(M / 32), 2N] floats, the column sums of every 32 rows of dpre, or NULL.
 cudaError_t gated_tc_gradient(const void* dout, int64_t lddo, const void* w_out, int64_t ldw, const void* pre, int64_t ldp,
-                              void* dpre, int64_t lddp, int64_t M, int64_t N, int64_t D, int gate, cudaStream_t s);
-// out[M, N] = A . B with A [M, K] (or, a_mn, [K, M]) and B [K, N], all bf16.
-cudaError_t matmul_tc(bool a_mn, const void* a, int64_t lda, const void* b, int64_t ldb, void* out, int64_t ldo, int64_t M,
-                      int64_t N, int64_t K, cudaStream_t s);
+                              void* dpre, int64_t lddp, float* sums, int64_t M, int64_t N, int64_t D, int gate,
+                              cudaStream_t s);
+// out[M, N] = A . B with A [M, K] (or, a_mn, [K, M]) and B [K, N], all bf16; out NULL: not formed, but planned for.
+struct ProductArg {
+  const void* a;
+  int64_t lda;
+  bool a_mn;
+  const void* b;
+  int64_t ldb;
+  void* out;
+  int64_t ldo;
+  int64_t M, N, K;
+};
+// Up to three products that do not depend on one another.
+cudaError_t matmul_tc_group(const ProductArg* list, int n, cudaStream_t s);
+// A linear layer (bias or NULL; EPD_LINEAR_ACCUMULATE / EPD_LINEAR_OUT_F32) whose tiles are too few for the machine, the
+// contraction of every tile shared among the pairs of a cluster.  Only where linear_tc_split_pays().
+bool linear_tc_split_pays(int64_t M, int64_t N, int64_t K);
+cudaError_t linear_tc_split(const void* x, int64_t ldx, const void* w, int64_t ldw, const void* bias, void* out, int64_t ldo,
+                            int64_t M, int64_t N, int64_t K, int flags, cudaStream_t s);
 
 // ---- one token to kFewRows tokens (gated_few_rows.cu) -------------------------------------------
 constexpr int kFewRows = 32;

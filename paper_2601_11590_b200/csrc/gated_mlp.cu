@@ -135,48 +135,103 @@ cudaError_t matmul_fma(int dtype, const FmaArgs& p, cudaStream_t s) {
 }
 
 // =============================================================================================
-// Column sums out[n] = sum_m x[m, n] in two launches, the same order of additions on every call: each block adds
-// kSumRows rows of 256 columns into a float partial sum, the second launch adds the partial sums.
+// Column sums out[n] = sum_m x[m, n]: float sums of kSumRows rows each, then the sum of those, always in the same order (no
+// atomics).  First launch: 32 threads side by side with a 16-byte piece of the row each, 8 threads along the rows.
+// HBM bound.
 // =============================================================================================
-constexpr int kSumRows = 128;
+constexpr int kSumRows = 64;
 
-template <typename T>
+template <typename T, int VEC>
 __global__ void __launch_bounds__(256)
 column_sum_partial_kernel(const T* __restrict__ x, int64_t ldx, int64_t M, int64_t N, float* __restrict__ part) {
-  const int64_t n = (int64_t)blockIdx.y * 256 + threadIdx.x;
-  if (n >= N) return;
-  const int64_t m0 = (int64_t)blockIdx.x * kSumRows, m1 = min(M, m0 + kSumRows);
-  float s = 0.0f;
-  for (int64_t m = m0; m < m1; ++m) s += to_float<T>(x[m * ldx + n]);
-  part[(int64_t)blockIdx.x * N + n] = s;
+  pdl_launch_dependents();
+  pdl_wait();
+  __shared__ float s_sum[8][32 * VEC + 1];
+  const int c = threadIdx.x & 31, r = threadIdx.x >> 5;
+  const int64_t n = ((int64_t)blockIdx.y * 32 + c) * VEC, m0 = (int64_t)blockIdx.x * kSumRows;
+  float acc[VEC] = {};
+  if (n < N) {
+#pragma unroll
+    for (int i = 0; i < kSumRows / 8; ++i) {
+      const int64_t m = m0 + r + 8 * i;
+      if (m < M) {
+        alignas(16) T v[VEC];
+        if constexpr (VEC > 1) *reinterpret_cast<uint4*>(v) = *reinterpret_cast<const uint4*>(x + m * ldx + n);
+        else v[0] = x[m * ldx + n];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) acc[e] += to_float<T>(v[e]);
+      }
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) s_sum[r][c * VEC + e] = acc[e];
+  __syncthreads();
+  for (int i = threadIdx.x; i < 32 * VEC; i += 256) {
+    const int64_t col = (int64_t)blockIdx.y * 32 * VEC + i;
+    if (col >= N) continue;
+    float s = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) s += s_sum[k][i];
+    part[(int64_t)blockIdx.x * N + col] = s;
+  }
 }
 
+// Second launch, for up to two sums at once: 32 columns by 8 threads along the partial sums.
+struct FinalSum {
+  const float* part;
+  int64_t groups, N;
+  void* out;
+};
 template <typename T>
 __global__ void __launch_bounds__(256)
-column_sum_final_kernel(const float* __restrict__ part, int64_t blocks, int64_t N, T* __restrict__ out) {
-  const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (n >= N) return;
+column_sum_final_kernel(const FinalSum a, const FinalSum b) {
+  pdl_launch_dependents();
+  pdl_wait();
+  __shared__ float s_sum[8][33];
+  const int64_t blocks_a = (a.N + 31) / 32;
+  const bool second = blockIdx.x >= blocks_a;
+  const FinalSum& f = second ? b : a;
+  const int c = threadIdx.x & 31, r = threadIdx.x >> 5;
+  const int64_t n = (blockIdx.x - (second ? blocks_a : 0)) * 32 + c;
   float s = 0.0f;
-  for (int64_t b = 0; b < blocks; ++b) s += part[b * N + n];
-  out[n] = from_float<T>(s);
+  if (n < f.N) {
+#pragma unroll 8
+    for (int64_t g = r; g < f.groups; g += 8) s += f.part[g * f.N + n];
+  }
+  s_sum[r][c] = s;
+  __syncthreads();
+  if (r == 0 && n < f.N) {
+    float t = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) t += s_sum[k][c];
+    static_cast<T*>(f.out)[n] = from_float<T>(t);
+  }
 }
 
 size_t align256(size_t v) { return (v + 255) / 256 * 256; }
-size_t column_sum_bytes(int64_t M, int64_t N) { return align256((size_t)((M + kSumRows - 1) / kSumRows) * N * 4); }
+int64_t sum_groups(int64_t M) { return (M + kSumRows - 1) / kSumRows; }
+size_t column_sum_bytes(int64_t M, int64_t N) { return align256((size_t)sum_groups(M) * N * 4); }
 
-template <typename T>
-cudaError_t column_sum_t(const void* x, int64_t ldx, int64_t M, int64_t N, void* out, float* part, cudaStream_t s) {
-  const int64_t blocks = (M + kSumRows - 1) / kSumRows;
-  if ((N + 255) / 256 > 65535) return cudaErrorInvalidValue;
-  column_sum_partial_kernel<T><<<dim3((unsigned)blocks, (unsigned)((N + 255) / 256)), 256, 0, s>>>(
-      static_cast<const T*>(x), ldx, M, N, part);
-  column_sum_final_kernel<T><<<(unsigned)((N + 255) / 256), 256, 0, s>>>(part, blocks, N, static_cast<T*>(out));
-  return cudaGetLastError();
+template <typename T, int VEC>
+cudaError_t column_sum_partial_t(const void* x, int64_t ldx, int64_t M, int64_t N, float* part, cudaStream_t s) {
+  const int64_t gy = (N + 32 * VEC - 1) / (32 * VEC);
+  if (gy > 65535) return cudaErrorInvalidValue;
+  return launch_pdl(column_sum_partial_kernel<T, VEC>, dim3((unsigned)sum_groups(M), (unsigned)gy), dim3(256), 0, s,
+                    static_cast<const T*>(x), ldx, M, N, part);
 }
-cudaError_t column_sum(int dtype, const void* x, int64_t ldx, int64_t M, int64_t N, void* out, float* part,
-                       cudaStream_t s) {
-  return dtype == EPD_DTYPE_F32 ? column_sum_t<float>(x, ldx, M, N, out, part, s)
-                                : column_sum_t<__nv_bfloat16>(x, ldx, M, N, out, part, s);
+cudaError_t column_sum_partial(int dtype, const void* x, int64_t ldx, int64_t M, int64_t N, float* part, cudaStream_t s) {
+  const int vec = dtype == EPD_DTYPE_F32 ? 4 : 8;
+  const bool whole = ((uintptr_t)x & 15) == 0 && ldx % vec == 0 && N % vec == 0;
+  if (dtype == EPD_DTYPE_F32)
+    return whole ? column_sum_partial_t<float, 4>(x, ldx, M, N, part, s) : column_sum_partial_t<float, 1>(x, ldx, M, N, part, s);
+  return whole ? column_sum_partial_t<__nv_bfloat16, 8>(x, ldx, M, N, part, s)
+               : column_sum_partial_t<__nv_bfloat16, 1>(x, ldx, M, N, part, s);
+}
+cudaError_t column_sum_final(int dtype, const FinalSum& a, const FinalSum& b, cudaStream_t s) {
+  const int64_t blocks = (a.N + 31) / 32 + (b.N + 31) / 32;
+  if (blocks == 0) return cudaSuccess;
+  if (dtype == EPD_DTYPE_F32) return launch_pdl(column_sum_final_kernel<float>, dim3((unsigned)blocks), dim3(256), 0, s, a, b);
+  return launch_pdl(column_sum_final_kernel<__nv_bfloat16>, dim3((unsigned)blocks), dim3(256), 0, s, a, b);
 }
 
 // =============================================================================================
@@ -192,7 +247,7 @@ cudaError_t gated_linear(int dtype, const void* x, int64_t ldx, const void* w, i
                          int64_t ldo, void* pre, int64_t ldp, int64_t M, int64_t N, int64_t K, int gate, cudaStream_t s) {
   if (few_rows(dtype, x, ldx, w, ldw, M, K)) return gated_few_rows(x, ldx, w, ldw, bias, out, ldo, pre, ldp, M, N, K, gate, s);
   if (dtype == EPD_DTYPE_BF16 && gated_tc_supported({{x, ldx}, {w, ldw}, {out, ldo}, {pre, ldp}}, {N, K}))
-    return gated_tc_forward(x, ldx, w, ldw, bias, out, ldo, pre, ldp, M, N, K, gate, nullptr, s);
+    return gated_tc_forward(x, ldx, w, ldw, bias, out, ldo, pre, ldp, M, N, K, gate, s);
   FmaArgs p = {};
   p.a = x; p.lda = ldx;
   p.b = w; p.ldb = ldw;
@@ -204,12 +259,15 @@ cudaError_t gated_linear(int dtype, const void* x, int64_t ldx, const void* w, i
   return matmul_fma<false, false, EPI_GATE>(dtype, p, s);
 }
 
-// dpre[M, 2N] from dout[M, D], w_out[D, N] and pre[M, 2N]
+// dpre[M, 2N] from dout[M, D], w_out[D, N] and pre[M, 2N]; its column sums in groups of rows into part (NULL: not formed),
+// the number of groups into *groups.
 cudaError_t gate_gradient(int dtype, const void* dout, int64_t lddo, const void* w_out, int64_t ldw, const void* pre,
-                          int64_t ldp, void* dpre, int64_t lddp, int64_t M, int64_t N, int64_t D, int gate,
-                          cudaStream_t s) {
-  if (dtype == EPD_DTYPE_BF16 && gated_tc_supported({{dout, lddo}, {w_out, ldw}, {pre, ldp}, {dpre, lddp}}, {N, D}))
-    return gated_tc_gradient(dout, lddo, w_out, ldw, pre, ldp, dpre, lddp, M, N, D, gate, s);
+                          int64_t ldp, void* dpre, int64_t lddp, float* part, int64_t* groups, int64_t M, int64_t N,
+                          int64_t D, int gate, cudaStream_t s) {
+  if (dtype == EPD_DTYPE_BF16 && gated_tc_supported({{dout, lddo}, {w_out, ldw}, {pre, ldp}, {dpre, lddp}}, {N, D})) {
+    *groups = (M + 31) / 32;
+    return gated_tc_gradient(dout, lddo, w_out, ldw, pre, ldp, dpre, lddp, part, M, N, D, gate, s);
+  }
   FmaArgs p = {};
   p.a = dout; p.lda = lddo;
   p.b = w_out; p.ldb = ldw;
@@ -217,33 +275,43 @@ cudaError_t gate_gradient(int dtype, const void* dout, int64_t lddo, const void*
   p.dpre = dpre; p.lddp = lddp;
   p.M = M; p.N = N; p.K = D;
   p.gate = gate;
-  return matmul_fma<false, true, EPI_GATE_GRAD>(dtype, p, s);
+  const cudaError_t e = matmul_fma<false, true, EPI_GATE_GRAD>(dtype, p, s);
+  *groups = sum_groups(M);
+  return e != cudaSuccess || !part ? e : column_sum_partial(dtype, dpre, lddp, M, 2 * N, part, s);
 }
 
 // dx[M, K] = dout[M, N] . w[N, K]
-cudaError_t input_gradient(int dtype, const void* dout, int64_t lddo, const void* w, int64_t ldw, void* dx, int64_t lddx,
-                           int64_t M, int64_t N, int64_t K, cudaStream_t s) {
-  if (dtype == EPD_DTYPE_BF16 && gated_tc_supported({{dout, lddo}, {w, ldw}, {dx, lddx}}, {N, K}))
-    return matmul_tc(false, dout, lddo, w, ldw, dx, lddx, M, K, N, s);
-  FmaArgs p = {};
-  p.a = dout; p.lda = lddo;
-  p.b = w; p.ldb = ldw;
-  p.out = dx; p.ldo = lddx;
-  p.M = M; p.N = K; p.K = N;
-  return matmul_fma<false, true, EPI_PLAIN>(dtype, p, s);
+ProductArg input_gradient(const void* dout, int64_t lddo, const void* w, int64_t ldw, void* dx, int64_t lddx, int64_t M,
+                          int64_t N, int64_t K) {
+  return ProductArg{dout, lddo, false, w, ldw, dx, lddx, M, K, N};
+}
+// dw[N, K] = dout[M, N]^T . x[M, K]
+ProductArg weight_gradient(const void* dout, int64_t lddo, const void* x, int64_t ldx, void* dw, int64_t lddw, int64_t M,
+                           int64_t N, int64_t K) {
+  return ProductArg{dout, lddo, true, x, ldx, dw, lddw, N, K, M};
 }
 
-// dw[N, K] = dout[M, N]^T . x[M, K]
-cudaError_t weight_gradient(int dtype, const void* dout, int64_t lddo, const void* x, int64_t ldx, void* dw, int64_t lddw,
-                            int64_t M, int64_t N, int64_t K, cudaStream_t s) {
-  if (dtype == EPD_DTYPE_BF16 && gated_tc_supported({{dout, lddo}, {x, ldx}, {dw, lddw}}, {N, K}))
-    return matmul_tc(true, dout, lddo, x, ldx, dw, lddw, N, K, M, s);
-  FmaArgs p = {};
-  p.a = dout; p.lda = lddo;
-  p.b = x; p.ldb = ldx;
-  p.out = dw; p.ldo = lddw;
-  p.M = N; p.N = K; p.K = M;
-  return matmul_fma<true, true, EPI_PLAIN>(dtype, p, s);
+// The products of the list (those with an output): together on the tensor cores where they can take them, else on FMAs.
+cudaError_t products(int dtype, std::initializer_list<ProductArg> list, cudaStream_t s) {
+  ProductArg tc[3];
+  int n = 0;
+  for (const ProductArg& a : list) {
+    // what lies contiguous in memory comes in pieces of 8: A's rows or its contraction, and the columns
+    if (dtype == EPD_DTYPE_BF16 &&
+        gated_tc_supported({{a.a, a.lda}, {a.b, a.ldb}, {a.out, a.ldo}}, {a.a_mn ? a.M : a.K, a.N})) {
+      tc[n++] = a;
+      continue;
+    }
+    if (!a.out) continue;
+    FmaArgs p = {};
+    p.a = a.a; p.lda = a.lda;
+    p.b = a.b; p.ldb = a.ldb;
+    p.out = a.out; p.ldo = a.ldo;
+    p.M = a.M; p.N = a.N; p.K = a.K;
+    const cudaError_t e = a.a_mn ? matmul_fma<true, true, EPI_PLAIN>(dtype, p, s) : matmul_fma<false, true, EPI_PLAIN>(dtype, p, s);
+    if (e != cudaSuccess) return e;
+  }
+  return n > 0 ? matmul_tc_group(tc, n, s) : cudaSuccess;
 }
 
 int finish(cudaError_t e) {
@@ -307,6 +375,9 @@ int epd_op_gated_mlp(int32_t dtype, const void* x, int64_t ldx, const void* w_in
   if (few_rows(dtype, hidden, ldh, w_out, ldw_out, M, N))
     return finish(linear_few_rows(hidden, ldh, w_out, ldw_out, b_out, out, ldo, M, D, N, flags,
                                   few_rows(dtype, x, ldx, w_in, ldw_in, M, K), s));
+  if (dtype == EPD_DTYPE_BF16 && ldo % 8 == 0 && linear_tc_split_pays(M, D, N) &&
+      gated_tc_supported({{hidden, ldh}, {w_out, ldw_out}, {out, ldo}}, {D, N}))
+    return finish(linear_tc_split(hidden, ldh, w_out, ldw_out, b_out, out, ldo, M, D, N, flags, s));
   return epd_op_linear(dtype, hidden, ldh, w_out, ldw_out, b_out, out, ldo, M, D, N, flags, stream);
 }
 
@@ -314,7 +385,8 @@ size_t epd_gated_mlp_backward_workspace_bytes(int32_t dtype, int64_t M, int64_t 
   using namespace epd;
   if (!dtype_ok(dtype) || M < 0 || M > (1 << 28) || !extent_ok(N) || !extent_ok(D)) return 0;
   const size_t es = dtype == EPD_DTYPE_F32 ? 4 : 2;
-  return align256((size_t)M * 2 * N * es) + column_sum_bytes(M, 2 * N > D ? 2 * N : D) + 256;
+  // dpre, then the partial sums of its columns (a group per 32 rows at most), then those of dout's
+  return align256((size_t)M * 2 * N * es) + align256((size_t)((M + 31) / 32) * 2 * N * 4) + column_sum_bytes(M, D) + 256;
 }
 
 int epd_op_gated_mlp_backward(int32_t dtype, const void* dout, int64_t lddo, const void* x, int64_t ldx, const void* w_in,
@@ -343,16 +415,27 @@ int epd_op_gated_mlp_backward(int32_t dtype, const void* dout, int64_t lddo, con
   if (!dout || (inner && (!pre || !w_out)) || (dx && !w_in) || (dw_in && !x) || (dw_out && !hidden)) return EPD_EINVAL;
   if (!workspace || (uintptr_t)workspace % 256) return EPD_EINVAL;
   if (workspace_bytes < epd_gated_mlp_backward_workspace_bytes(dtype, M, N, D)) return EPD_ENOMEM;
-  void* dpre = workspace;
-  float* part = reinterpret_cast<float*>(static_cast<char*>(workspace) + align256((size_t)M * 2 * N * es));
-  if (db_out) EPD_TRY(column_sum(dtype, dout, lddo, M, D, db_out, part, s));
-  if (dw_out) EPD_TRY(weight_gradient(dtype, dout, lddo, hidden, ldh, dw_out, lddw_out, M, D, N, s));
-  if (!inner) return EPD_OK;
-  EPD_TRY(gate_gradient(dtype, dout, lddo, w_out, ldw_out, pre, ldp, dpre, 2 * N, M, N, D, gate, s));
-  if (db_in) EPD_TRY(column_sum(dtype, dpre, 2 * N, M, 2 * N, db_in, part, s));
-  if (dw_in) EPD_TRY(weight_gradient(dtype, dpre, 2 * N, x, ldx, dw_in, lddw_in, M, 2 * N, K, s));
-  if (dx) EPD_TRY(input_gradient(dtype, dpre, 2 * N, w_in, ldw_in, dx, lddx, M, 2 * N, K, s));
-  return EPD_OK;
+  char* ws = static_cast<char*>(workspace);
+  void* dpre = ws;
+  float* part_in = reinterpret_cast<float*>(ws + align256((size_t)M * 2 * N * es));
+  float* part_out = reinterpret_cast<float*>(reinterpret_cast<char*>(part_in) + align256((size_t)((M + 31) / 32) * 2 * N * 4));
+  FinalSum sum_in = {}, sum_out = {};
+  if (db_out) {
+    EPD_TRY(column_sum_partial(dtype, dout, lddo, M, D, part_out, s));
+    sum_out = FinalSum{part_out, sum_groups(M), D, db_out};
+  }
+  if (inner) {
+    int64_t groups = 0;
+    EPD_TRY(gate_gradient(dtype, dout, lddo, w_out, ldw_out, pre, ldp, dpre, 2 * N, db_in ? part_in : nullptr, &groups, M, N,
+                          D, gate, s));
+    if (db_in) sum_in = FinalSum{part_in, groups, 2 * N, db_in};
+  }
+  EPD_TRY(column_sum_final(dtype, sum_in, sum_out, s));
+  return finish(products(dtype,
+                         {input_gradient(dpre, 2 * N, w_in, ldw_in, dx, lddx, M, 2 * N, K),
+                          weight_gradient(dpre, 2 * N, x, ldx, dw_in, lddw_in, M, 2 * N, K),
+                          weight_gradient(dout, lddo, hidden, ldh, dw_out, lddw_out, M, D, N)},
+                         s));
 }
 
 size_t epd_linear_backward_workspace_bytes(int32_t dtype, int64_t M, int64_t N) {
@@ -379,11 +462,14 @@ int epd_op_linear_backward(int32_t dtype, const void* dout, int64_t lddo, const 
   if (db) {
     if (!workspace || (uintptr_t)workspace % 256) return EPD_EINVAL;
     if (workspace_bytes < epd_linear_backward_workspace_bytes(dtype, M, N)) return EPD_ENOMEM;
-    EPD_TRY(column_sum(dtype, dout, lddo, M, N, db, static_cast<float*>(workspace), s));
+    float* part = static_cast<float*>(workspace);
+    EPD_TRY(column_sum_partial(dtype, dout, lddo, M, N, part, s));
+    EPD_TRY(column_sum_final(dtype, FinalSum{part, sum_groups(M), N, db}, FinalSum{}, s));
   }
-  if (dw) EPD_TRY(weight_gradient(dtype, dout, lddo, x, ldx, dw, lddw, M, N, K, s));
-  if (dx) EPD_TRY(input_gradient(dtype, dout, lddo, w, ldw, dx, lddx, M, N, K, s));
-  return EPD_OK;
+  return finish(products(dtype,
+                         {input_gradient(dout, lddo, w, ldw, dx, lddx, M, N, K),
+                          weight_gradient(dout, lddo, x, ldx, dw, lddw, M, N, K)},
+                         s));
 }
 
 }  // extern "C"

@@ -5,12 +5,19 @@
 //              second the 128 up rows of the same columns, so that a thread of the epilogue holds both projections of
 //              its 128 output columns: act(g) * u leaves the kernel, g and u only when the gradient will need them.
 //   GATE_GRAD  A = dout [M, D] contraction-contiguous, B = w_out [D, N] row-contiguous: the tile is da = dout . w_out; the
-//              epilogue reads g and u and writes dg = da u act'(g), du = da act(g): da itself is never written.
-//   NN         A contraction-contiguous, B row-contiguous: dx = dout . w
-//   TN         both row-contiguous: dw = dout^T . x
+//              epilogue reads g and u and writes dg = da u act'(g), du = da act(g): da itself is never written.  Their
+//              column sums over each 32 rows (the bias gradient's first half) leave with them.
+//   GROUP      up to three products with a row-contiguous B: dx = dout . w (A contraction-contiguous) and dw = dout^T . x
+//              (A row-contiguous too), which do not depend on one another and share the machine's last, half-empty round.
+//   LINEAR     x . w^T + bias, both contraction-contiguous, for few rows (SPLIT only).
 // A row-contiguous ("MN-major") operand is staged as boxes of 64 rows x 64 contraction steps: TMA brings 128 contiguous
 // bytes of 64 rows per step, 128-byte swizzled, and the tensor core transposes on the way (descriptor: 8 KB between
 // boxes, 1 KB between groups of 8 steps), so no operand is ever transposed in memory.
+//
+// SPLIT: where the tiles would leave half of the machine or more idle (few rows: 13 tiles of a 200-block contraction for 74
+// tokens of the 6B-class block), 2 or 4 pairs of one cluster share a tile, each taking a part of the contraction.  At the
+// end every pair owns a part of the tile's columns; the others write their sums for it into the owner's shared memory
+// (the operand ring, free by then), and the owner adds them to its own in order: no atomics, no second launch.
 //
 // Roles per CTA (10 warps): warp 0 TMA producer, warp 1 issues the products (in the pair's first CTA) and owns tensor memory,
 // warps 2..9 epilogue, two per TMEM lane quarter, each taking half of the tile's columns in steps of 32: tcgen05.ld, the
@@ -25,7 +32,7 @@ namespace {
 
 using namespace tc;
 
-enum { MODE_GATE = 0, MODE_GATE_GRAD = 1, MODE_NN = 2, MODE_TN = 3 };
+enum { MODE_GATE = 0, MODE_GATE_GRAD = 1, MODE_GROUP = 2, MODE_LINEAR = 3 };
 
 constexpr int BM = 128;            // rows of A per CTA (256 per pair)
 constexpr int BN = 256;            // accumulator columns
@@ -47,7 +54,7 @@ template <int MODE> struct Smem {
   // full[S], empty[S], tmem_full[2], tmem_empty[2], drain, spare; per epilogue warp 3 fetch barriers; TMEM base, abort flag
   static constexpr int kFetchOffset = kBarOffset + (2 * kStages + 6) * 8;
   static constexpr int kBiasOffset = kFetchOffset + kEpiWarps * 3 * 8 + 16;
-  static constexpr int kTotal = kBiasOffset + (MODE == MODE_GATE ? kEpiWarps * 128 * 4 : 0);
+  static constexpr int kTotal = kBiasOffset + (MODE == MODE_GATE || MODE == MODE_LINEAR ? kEpiWarps * 128 * 4 : 0);
   static constexpr int kDynamic = kTotal + 1024;
   static_assert(kDynamic <= 232448, "exceeds the shared memory of one CTA");
   static_assert(kDynamic > 116 * 1024, "one CTA per SM is assumed by the TMEM allocation");
@@ -106,11 +113,15 @@ __device__ __forceinline__ void umma_pair(uint32_t tmem_d, uint64_t desc_a, uint
       ::"r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-__device__ __forceinline__ void umma_commit_both(uint64_t* bar) {
+// Arrives on the barrier at this offset in both CTAs of the pair whose first CTA is `leader` in the cluster.
+__device__ __forceinline__ void umma_commit_both(uint64_t* bar, uint32_t leader) {
   asm volatile(
       "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-      ::"r"(smem_u32(bar)), "h"((uint16_t)3)
+      ::"r"(smem_u32(bar)), "h"((uint16_t)(3u << leader))
       : "memory");
+}
+__device__ __forceinline__ void store_cluster(uint32_t cluster_addr, uint32_t v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_addr), "r"(v) : "memory");
 }
 // bf16 x bf16 -> float, M = 256 over the pair, N = BN; a_mn / b_mn: operand row-contiguous.
 __host__ __device__ constexpr uint32_t instr_desc(bool a_mn, bool b_mn) {
@@ -143,16 +154,25 @@ __device__ __forceinline__ void tile_coords(int tile, int m_tiles, int n_tiles, 
   nt = o.by_rows ? c : w;
 }
 
-struct Maps {
-  CUtensorMap a, b;
-  CUtensorMap o0, o1, o2;      // GATE: out, g, u; GATE_GRAD: dg, du; else out
-  CUtensorMap l0, l1;          // GATE_GRAD: g, u
+constexpr int kSubs = 3;
+struct Sub {                   // one product: out[M, N] = A . B over K
+  CUtensorMap a, b, out;
+  int M, N, K;
+  int a_mn;                    // A row-contiguous
+  int first;                   // number of its first tile in the launch
+  Order order;
 };
 struct Problem {
-  int M, N, K;                 // N: columns of an output matrix
+  Sub sub[kSubs];              // GROUP: up to three, in the order of the launch's tiles; else the first
+  CUtensorMap o1, o2;          // GATE: g, u; GATE_GRAD: out and o1 are dg, du
+  CUtensorMap l0, l1;          // GATE_GRAD: g, u
+  int subs, tiles;
+  int tile0;                   // SPLIT: the launch's first tile
+  int split;                   // pairs that share a tile (SPLIT), else 1
   int save_pre;                // GATE: g and u are written
-  const __nv_bfloat16* bias;   // GATE: [2N] or NULL
-  Order order;
+  int out_f32, accumulate;     // LINEAR
+  const __nv_bfloat16* bias;   // GATE: [2N] or NULL; LINEAR: [N] or NULL
+  float* sums;                 // GATE_GRAD: column sums of 32 rows each, [ceil(M / 32), 2N], or NULL
   long long wait_limit;
   int* status;
 };
@@ -166,14 +186,29 @@ __device__ __forceinline__ uint8_t* box_piece(uint8_t* buf, int lane, int j) {
   return buf + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4);
 }
 
-template <int MODE, int GATE>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
-gated_pair_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Problem p) {
+// Adds up 32 columns over the warp's 32 rows (one row per lane): lane l returns the sum of column l.  Always the same order.
+__device__ __forceinline__ float column_sum32(float (&v)[32], int lane) {
+#pragma unroll
+  for (int w = 16; w > 0; w >>= 1) {
+    const bool upper = lane & w;
+#pragma unroll
+    for (int i = 0; i < w; ++i) {
+      const float keep = upper ? v[i + w] : v[i], give = upper ? v[i] : v[i + w];
+      v[i] = keep + __shfl_xor_sync(0xffffffffu, give, w);
+    }
+  }
+  return v[0];
+}
+
+template <int MODE, int GATE, bool SPLIT>
+__global__ void __launch_bounds__(kThreads, 1)
+gated_pair_kernel(const __grid_constant__ Problem p) {
   using L = Smem<MODE>;
   constexpr int STAGES = L::kStages;
-  constexpr bool A_MN = MODE == MODE_TN, B_MN = MODE != MODE_GATE;
+  constexpr bool B_MN = MODE == MODE_GATE_GRAD || MODE == MODE_GROUP;
   constexpr int TILE_COLS = MODE == MODE_GATE ? BN / 2 : BN;     // output columns of a tile
-  constexpr int kSteps = TILE_COLS / 2 / 32;                     // 32-column steps of an epilogue warp
+  constexpr int kSteps = TILE_COLS / 32;                         // 32-column steps of a tile
+  static_assert(MODE != MODE_LINEAR || SPLIT, "whole tiles of a linear layer run on its own kernel");
 
   pdl_launch_dependents();
   extern __shared__ uint8_t smem_raw[];
@@ -188,13 +223,28 @@ gated_pair_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Pro
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_base_slot + 1);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t rank = cluster_rank();
-  const WaitCtx wc{abort_flag, map_to_rank(smem_u32(const_cast<int*>(abort_flag)), rank ^ 1u), p.wait_limit};
-  const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
-  const int m_tiles = (p.M + 2 * BM - 1) / (2 * BM), n_tiles = (p.N + TILE_COLS - 1) / TILE_COLS;
-  const int num_tiles = m_tiles * n_tiles;
-  const int k_blocks = (p.K + BK - 1) / BK;
+  const uint32_t cta = cluster_rank();
+  const uint32_t rank = cta & 1, leader = cta & ~1u;             // place in the pair; the pair's first CTA
+  const int slice = SPLIT ? (int)(cta >> 1) : 0;                 // part of the contraction
+  const int split = SPLIT ? p.split : 1;
+  const WaitCtx wc{abort_flag, map_to_rank(smem_u32(const_cast<int*>(abort_flag)), cta ^ 1u), p.wait_limit};
+  const int first_tile = SPLIT ? p.tile0 + blockIdx.x / (2 * split) : blockIdx.x >> 1;
+  const int tile_step = SPLIT ? p.tiles : gridDim.x >> 1;        // SPLIT: one tile per cluster
   uint32_t loads_issued = 0;
+
+  // Tile number -> product, place of the tile, part of the contraction (in blocks of BK)
+  auto locate = [&](int tile, int& mt, int& nt, int& kb0, int& kb1) -> const Sub& {
+    int i = 0;
+    if constexpr (MODE == MODE_GROUP) {
+      while (i + 1 < p.subs && tile >= p.sub[i + 1].first) ++i;
+    }
+    const Sub& u = p.sub[i];
+    tile_coords(tile - u.first, (u.M + 2 * BM - 1) / (2 * BM), (u.N + TILE_COLS - 1) / TILE_COLS, u.order, mt, nt);
+    const int blocks = (u.K + BK - 1) / BK;
+    kb0 = SPLIT ? slice * blocks / split : 0;
+    kb1 = SPLIT ? (slice + 1) * blocks / split : blocks;
+    return u;
+  };
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
@@ -216,41 +266,284 @@ gated_pair_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Pro
   const uint32_t tmem_base = *tmem_base_slot;
   pdl_wait();   // nothing above touches global memory
 
+  // Epilogue state that lives on past the role's loop in a split launch
+  const int q = warp & 3;                          // TMEM lane quarter this warp may read
+  const int half = (warp - 2) >> 2;                // which half of the columns (warps 2..9)
+  uint8_t* bufs = smem + L::kBufOffset + (warp - 2) * L::kBufs * kBufBytes;
+  uint64_t* fbar = fetch + (warp - 2) * 3;
+  float* bs = reinterpret_cast<float*>(smem + L::kBiasOffset) + (warp - 2) * 128;   // biases of up to 2 steps: 64, 64 (up)
+  // 32-column steps this warp finishes: half of the tile's, or half of those its pair owns
+  const int step0 = SPLIT ? slice * kSteps / split + half : half * (kSteps / 2);
+  const int step_end = SPLIT ? (slice + 1) * kSteps / split : step0 + kSteps / 2;
+  constexpr int kStepBy = SPLIT ? 2 : 1;
+  uint32_t step = 0;                               // steps done by this warp over all its tiles
+  uint32_t fetched = 0;                            // GATE_GRAD: steps whose g and u have been asked for
+  int acc = 0;
+  // GATE_GRAD: asks for g and u of the step at (row, column)
+  auto fetch_pre = [&](int row, int col) {
+    if (lane == 0) {
+      uint64_t* b = &fbar[fetched % 3];
+      uint8_t* to = bufs + (fetched % 3) * 2 * kBufBytes;
+      mbar_expect_tx(b, 2 * kBufBytes);
+      tma_load_2d(to, &p.l0, col, row, b);
+      tma_load_2d(to + kBufBytes, &p.l1, col, row, b);
+    }
+    __syncwarp();
+    ++fetched;
+  };
+  // Where the sums of the other parts lie in an owner's ring: [part before it, parts after it][step][g | u][column][128 rows]
+  constexpr int kPer = MODE == MODE_GATE ? 64 : 32;              // columns of accumulators per step
+  auto partial_at = [&](int part, int local_step, int col) {     // in floats
+    return ((part * (kSteps / split) + local_step) * kPer + col) * BM;
+  };
+  // The steps of one tile, from tensor memory (and, SPLIT, the other parts' sums) to the output.  False: a wait expired.
+  auto finish_tile = [&](const Sub& u, int mt, int nt, int next_tile) -> bool {
+    const int row0 = mt * (2 * BM) + (int)rank * BM + q * 32, n0 = nt * TILE_COLS;
+    const uint32_t taddr = tmem_base + acc * BN + ((uint32_t)(q * 32) << 16);
+    const float* ring = reinterpret_cast<const float*>(smem);
+    auto add_parts = [&](uint32_t (&v)[32], int st, int which) {
+      if constexpr (SPLIT) {
+        // the pair's own part, then the others in order: a column has one owner, so its sum always runs the same way
+        const float* r = ring + partial_at(0, st - slice * kSteps / split, which * 32) + q * 32 + lane;
+#pragma unroll 1
+        for (int o = 1; o < split; ++o, r += (kSteps / split) * kPer * BM) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + r[i * BM]);
+        }
+      }
+    };
+    if constexpr (MODE == MODE_GATE || MODE == MODE_LINEAR) {
+      __syncwarp();
+      int ls = 0;
+      for (int st = step0; st < step_end; st += kStepBy, ++ls) {
+        const int col = n0 + st * 32 + lane;
+        const bool in = p.bias != nullptr && col < u.N;
+        bs[ls * 32 + lane] = in ? __bfloat162float(p.bias[col]) : 0.0f;
+        if (MODE == MODE_GATE) bs[64 + ls * 32 + lane] = in ? __bfloat162float(p.bias[u.N + (int64_t)col]) : 0.0f;
+      }
+      __syncwarp();
+    }
+    auto release = [&](int st) {
+      if (!SPLIT && st + kStepBy >= step_end) {
+        // this warp has read all of its accumulator columns
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(map_to_rank(smem_u32(&tmem_empty[acc]), leader));
+      }
+    };
+    int ls = 0;
+#pragma unroll 1
+    for (int st = step0; st < step_end; st += kStepBy, ++ls, ++step) {
+      const int col = n0 + st * 32;
+      const bool inside = row0 < u.M && col < u.N;
+      if constexpr (MODE == MODE_GATE) {
+        uint32_t g[32], w[32];
+        tmem_ld32(taddr + st * 32, g);
+        tmem_ld32(taddr + BN / 2 + st * 32, w);
+        tmem_ld_wait();
+        release(st);
+        add_parts(g, st, 0);
+        add_parts(w, st, 1);
+        if (lane == 0) bulk_wait_read<0>();       // the boxes' last stores have left shared memory
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          uint32_t o4[4], g4[4], u4[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int i = 8 * j + 2 * e;
+            const float2 bg = *reinterpret_cast<const float2*>(bs + ls * 32 + i);
+            const float2 bu = *reinterpret_cast<const float2*>(bs + 64 + ls * 32 + i);
+            const float g0 = __uint_as_float(g[i]) + bg.x, g1 = __uint_as_float(g[i + 1]) + bg.y;
+            const float u0 = __uint_as_float(w[i]) + bu.x, u1 = __uint_as_float(w[i + 1]) + bu.y;
+            o4[e] = pack2(gate_act_fast<GATE>(g0) * u0, gate_act_fast<GATE>(g1) * u1);
+            g4[e] = pack2(g0, g1);
+            u4[e] = pack2(u0, u1);
+          }
+          *reinterpret_cast<uint4*>(box_piece(bufs, lane, j)) = make_uint4(o4[0], o4[1], o4[2], o4[3]);
+          if (p.save_pre) {
+            *reinterpret_cast<uint4*>(box_piece(bufs + kBufBytes, lane, j)) = make_uint4(g4[0], g4[1], g4[2], g4[3]);
+            *reinterpret_cast<uint4*>(box_piece(bufs + 2 * kBufBytes, lane, j)) = make_uint4(u4[0], u4[1], u4[2], u4[3]);
+          }
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+          if (inside) {
+            tma_store_2d(&u.out, col, row0, bufs);
+            if (p.save_pre) {
+              tma_store_2d(&p.o1, col, row0, bufs + kBufBytes);
+              tma_store_2d(&p.o2, col, row0, bufs + 2 * kBufBytes);
+            }
+          }
+          bulk_commit();
+        }
+      } else if constexpr (MODE == MODE_GATE_GRAD) {
+        // the next step's g and u: into the pair of boxes whose store was issued two steps ago
+        int next_row = row0, next_col = col + kStepBy * 32;
+        bool more = true;
+        if (st + kStepBy >= step_end) {
+          more = next_tile < p.tiles;
+          if (more) {
+            int nm, nn, k0, k1;
+            locate(next_tile, nm, nn, k0, k1);
+            next_row = nm * (2 * BM) + (int)rank * BM + q * 32;
+            next_col = nn * TILE_COLS + step0 * 32;
+          }
+        }
+        if (more) {
+          if (lane == 0) bulk_wait_read<1>();
+          __syncwarp();
+          fetch_pre(next_row, next_col);
+        }
+        uint32_t da[32];
+        tmem_ld32(taddr + st * 32, da);
+        tmem_ld_wait();
+        release(st);
+        add_parts(da, st, 0);
+        if (!mbar_wait_warp(&fbar[step % 3], (step / 3) & 1, wc)) return false;
+        uint8_t* gb = bufs + (step % 3) * 2 * kBufBytes;
+        uint8_t* ub = gb + kBufBytes;
+        float dg[32], du[32];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          uint4* gp = reinterpret_cast<uint4*>(box_piece(gb, lane, j));
+          uint4* up = reinterpret_cast<uint4*>(box_piece(ub, lane, j));
+          const uint4 gv = *gp, uv = *up;
+          const uint32_t gw[4] = {gv.x, gv.y, gv.z, gv.w}, uw[4] = {uv.x, uv.y, uv.z, uv.w};
+          uint32_t dg4[4], du4[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float2 gf = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&gw[e]));
+            const float2 uf = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&uw[e]));
+            const int i = 8 * j + 2 * e;
+            const float d0 = __uint_as_float(da[i]), d1 = __uint_as_float(da[i + 1]);
+            float a0, s0, a1, s1;
+            gate_act_slope_fast<GATE>(gf.x, &a0, &s0);
+            gate_act_slope_fast<GATE>(gf.y, &a1, &s1);
+            dg[i] = d0 * uf.x * s0;
+            dg[i + 1] = d1 * uf.y * s1;
+            du[i] = d0 * a0;
+            du[i + 1] = d1 * a1;
+            dg4[e] = pack2(dg[i], dg[i + 1]);
+            du4[e] = pack2(du[i], du[i + 1]);
+          }
+          *gp = make_uint4(dg4[0], dg4[1], dg4[2], dg4[3]);
+          *up = make_uint4(du4[0], du4[1], du4[2], du4[3]);
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+          if (inside) {
+            tma_store_2d(&u.out, col, row0, gb);
+            tma_store_2d(&p.o1, col, row0, ub);
+          }
+          bulk_commit();
+        }
+        if (p.sums != nullptr && row0 < u.M) {
+          // rows beyond the last one hold zeros: their dout rows were filled with zeros
+          const float sg = column_sum32(dg, lane), su = column_sum32(du, lane);
+          if (col + lane < u.N) {
+            float* to = p.sums + (int64_t)(row0 / 32) * (2 * (int64_t)u.N) + col + lane;
+            to[0] = sg;
+            to[u.N] = su;
+          }
+        }
+      } else {
+        uint32_t v[32];
+        tmem_ld32(taddr + st * 32, v);
+        tmem_ld_wait();
+        release(st);
+        add_parts(v, st, 0);
+        if constexpr (MODE == MODE_LINEAR) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + bs[ls * 32 + i]);
+        }
+        if (MODE == MODE_LINEAR && p.out_f32) {
+          // 32 floats a row: a 128-byte-swizzled box over two of the staging boxes
+          if (lane == 0) bulk_wait_read<0>();
+          __syncwarp();
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            *reinterpret_cast<uint4*>(bufs + lane * 128 + ((j ^ (lane & 7)) << 4)) =
+                make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) {
+            if (inside) {
+              if (p.accumulate) tma_reduce_add_2d(&u.out, col, row0, bufs);
+              else tma_store_2d(&u.out, col, row0, bufs);
+            }
+            bulk_commit();
+          }
+          continue;
+        }
+        uint8_t* buf = bufs + (step % 3) * kBufBytes;
+        if (lane == 0) bulk_wait_read<2>();       // the box's store three steps ago
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          uint32_t w[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[e] = pack2(__uint_as_float(v[8 * j + 2 * e]), __uint_as_float(v[8 * j + 2 * e + 1]));
+          *reinterpret_cast<uint4*>(box_piece(buf, lane, j)) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+          if (inside) tma_store_2d(&u.out, col, row0, buf);
+          bulk_commit();
+        }
+      }
+    }
+    return true;
+  };
+  auto finish_stores = [&] {
+    if (lane == 0) {
+      bulk_wait_all();
+      // after an abort: boxes asked for and not waited for are still on their way
+      for (uint32_t f = step; f < fetched; ++f) mbar_wait_drain(&fbar[f % 3], (f / 3) & 1);
+    }
+    __syncwarp();
+  };
+  bool tile_ready = false;                         // SPLIT: this warp's accumulator is complete
+
   if (warp == 0) {
     // ------------------------------------------------------------------ TMA producer (both CTAs)
     if (lane == 0) {
-      prefetch_map(&maps.a);
-      prefetch_map(&maps.b);
+      prefetch_map(&p.sub[0].a);
+      prefetch_map(&p.sub[0].b);
     }
     int stage = 0;
     uint32_t phase = 0;
     bool ok = true;
-    const uint64_t pol_a = l2_policy(p.order.by_rows, p.order.stream_normal);
-    const uint64_t pol_b = l2_policy(!p.order.by_rows, p.order.stream_normal);
-    for (int tile = pair; tile < num_tiles && ok; tile += n_pairs) {
-      int mt, nt;
-      tile_coords(tile, m_tiles, n_tiles, p.order, mt, nt);
+    for (int tile = first_tile; tile < p.tiles && ok; tile += tile_step) {
+      int mt, nt, kb0, kb1;
+      const Sub& u = locate(tile, mt, nt, kb0, kb1);
+      const uint64_t pol_a = l2_policy(u.order.by_rows, u.order.stream_normal);
+      const uint64_t pol_b = l2_policy(!u.order.by_rows, u.order.stream_normal);
       const int m0 = mt * (2 * BM) + (int)rank * BM;
       // this CTA's half of the B tile; GATE: gate rows in the first CTA, up rows in the second
-      const int n0 = MODE == MODE_GATE ? nt * TILE_COLS + (int)rank * p.N : nt * BN + (int)rank * (BN / 2);
-      for (int kb = 0; kb < k_blocks; ++kb) {
+      const int n0 = MODE == MODE_GATE ? nt * TILE_COLS + (int)rank * u.N : nt * BN + (int)rank * (BN / 2);
+      const bool a_mn = MODE == MODE_GROUP && u.a_mn;
+      for (int kb = kb0; kb < kb1; ++kb) {
         if (!mbar_wait_warp<true>(&empty[stage], phase ^ 1, wc)) { ok = false; break; }
         uint8_t* sa = smem + stage * kStageBytes;
         uint8_t* sb = sa + kTileBytes;
-        const uint32_t bar = map_to_rank(smem_u32(&full[stage]), 0);
+        const uint32_t bar = map_to_rank(smem_u32(&full[stage]), leader);
         if (elect_one()) {
           if (rank == 0) mbar_expect_tx(&full[stage], 2 * kStageBytes);   // both CTAs' bytes
-          if constexpr (A_MN) {
-            tma_load_pair(sa, &maps.a, m0, kb * BK, bar, pol_a);
-            tma_load_pair(sa + kBoxBytes, &maps.a, m0 + 64, kb * BK, bar, pol_a);
+          if (a_mn) {
+            tma_load_pair(sa, &u.a, m0, kb * BK, bar, pol_a);
+            tma_load_pair(sa + kBoxBytes, &u.a, m0 + 64, kb * BK, bar, pol_a);
           } else {
-            tma_load_pair(sa, &maps.a, kb * BK, m0, bar, pol_a);
+            tma_load_pair(sa, &u.a, kb * BK, m0, bar, pol_a);
           }
           if constexpr (B_MN) {
-            tma_load_pair(sb, &maps.b, n0, kb * BK, bar, pol_b);
-            tma_load_pair(sb + kBoxBytes, &maps.b, n0 + 64, kb * BK, bar, pol_b);
+            tma_load_pair(sb, &u.b, n0, kb * BK, bar, pol_b);
+            tma_load_pair(sb + kBoxBytes, &u.b, n0 + 64, kb * BK, bar, pol_b);
           } else {
-            tma_load_pair(sb, &maps.b, kb * BK, n0, bar, pol_b);
+            tma_load_pair(sb, &u.b, kb * BK, n0, bar, pol_b);
           }
         }
         __syncwarp();
@@ -262,34 +555,37 @@ gated_pair_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Pro
   } else if (warp == 1) {
     // ------------------------------------------------------------------ issues the products (leader only)
     if (rank == 0) {
-      constexpr uint32_t idesc = instr_desc(A_MN, B_MN);
-      // 16 contraction steps: 32 bytes inside a swizzled row, or two groups of 8 steps of 1024 bytes (descriptor units of 16)
-      constexpr uint32_t a_step = A_MN ? 2048 / 16 : 2, b_step = B_MN ? 2048 / 16 : 2;
       int stage = 0;
       uint32_t phase = 0;
-      int acc = 0;
       uint32_t acc_phase = 0;
       bool ok = true;
-      for (int tile = pair; tile < num_tiles && ok; tile += n_pairs) {
+      for (int tile = first_tile; tile < p.tiles && ok; tile += tile_step) {
+        int mt, nt, kb0, kb1;
+        const Sub& u = locate(tile, mt, nt, kb0, kb1);
+        const bool a_mn = MODE == MODE_GROUP && u.a_mn;
+        const uint32_t idesc = instr_desc(false, B_MN) | ((uint32_t)a_mn << 15);
+        // 16 contraction steps: 32 bytes inside a swizzled row, or two groups of 8 steps of 1024 bytes (units of 16 bytes)
+        const uint32_t a_step = a_mn ? 2048 / 16 : 2;
+        constexpr uint32_t b_step = B_MN ? 2048 / 16 : 2;
         if (!mbar_wait_warp<true>(&tmem_empty[acc], acc_phase ^ 1, wc)) break;
         tc_fence_after();
         const uint32_t d_tmem = tmem_base + acc * BN;
-        for (int kb = 0; kb < k_blocks; ++kb) {
+        for (int kb = kb0; kb < kb1; ++kb) {
           if (!mbar_wait_warp<true>(&full[stage], phase, wc)) { ok = false; break; }
           tc_fence_after();
           const uint32_t sa = smem_u32(smem + stage * kStageBytes);
-          const uint64_t da = A_MN ? smem_desc_mn_sw128(sa) : smem_desc_k_sw128(sa);
+          const uint64_t da = a_mn ? smem_desc_mn_sw128(sa) : smem_desc_k_sw128(sa);
           const uint64_t db = B_MN ? smem_desc_mn_sw128(sa + kTileBytes) : smem_desc_k_sw128(sa + kTileBytes);
           if (elect_one()) {
 #pragma unroll
-            for (int k = 0; k < BK / 16; ++k) umma_pair(d_tmem, da + a_step * k, db + b_step * k, idesc, (kb | k) != 0);
-            umma_commit_both(&empty[stage]);
+            for (int k = 0; k < BK / 16; ++k) umma_pair(d_tmem, da + a_step * k, db + b_step * k, idesc, kb > kb0 || k != 0);
+            umma_commit_both(&empty[stage], leader);
           }
           __syncwarp();
           if (++stage == STAGES) { stage = 0; phase ^= 1; }
         }
         if (!ok) break;
-        if (elect_one()) umma_commit_both(&tmem_full[acc]);
+        if (elect_one()) umma_commit_both(&tmem_full[acc], leader);
         __syncwarp();
         if (++acc == 2) { acc = 0; acc_phase ^= 1; }
       }
@@ -297,201 +593,66 @@ gated_pair_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Pro
     __syncwarp();
   } else {
     // ------------------------------------------------------------------ epilogue (both CTAs)
-    const int q = warp & 3;                          // TMEM lane quarter this warp may read
-    const int half = (warp - 2) >> 2;                // which half of the columns
-    uint8_t* bufs = smem + L::kBufOffset + (warp - 2) * L::kBufs * kBufBytes;
-    uint64_t* fbar = fetch + (warp - 2) * 3;
-    float* bs = reinterpret_cast<float*>(smem + L::kBiasOffset) + (warp - 2) * 128;   // GATE: 64 gate, 64 up
-    const uint32_t tmem_empty_leader = map_to_rank(smem_u32(&tmem_empty[0]), 0);
-    if (lane == 0) prefetch_map(&maps.o0);
-    int acc = 0;
+    if (lane == 0) prefetch_map(&p.sub[0].out);
     uint32_t acc_phase = 0;
-    uint32_t step = 0;                               // steps done by this warp over all its tiles
-    uint32_t fetched = 0;                            // GATE_GRAD: steps whose g and u have been asked for
-    // GATE_GRAD: asks for g and u of step c of the tile at (row, column)
-    auto fetch_pre = [&](int row, int col) {
-      if (lane == 0) {
-        uint64_t* b = &fbar[fetched % 3];
-        uint8_t* to = bufs + (fetched % 3) * 2 * kBufBytes;
-        mbar_expect_tx(b, 2 * kBufBytes);
-        tma_load_2d(to, &maps.l0, col, row, b);
-        tma_load_2d(to + kBufBytes, &maps.l1, col, row, b);
-      }
-      __syncwarp();
-      ++fetched;
-    };
-    auto origin = [&](int tile, int& row0, int& n0) {
-      int mt, nt;
-      tile_coords(tile, m_tiles, n_tiles, p.order, mt, nt);
-      row0 = mt * (2 * BM) + (int)rank * BM + q * 32;
-      n0 = nt * TILE_COLS + half * (TILE_COLS / 2);
-    };
     if constexpr (MODE == MODE_GATE_GRAD) {
-      if (pair < num_tiles) {
-        int row0, n0;
-        origin(pair, row0, n0);
-        fetch_pre(row0, n0);
+      if (first_tile < p.tiles && step0 < step_end) {
+        int mt, nt, kb0, kb1;
+        locate(first_tile, mt, nt, kb0, kb1);
+        fetch_pre(mt * (2 * BM) + (int)rank * BM + q * 32, nt * TILE_COLS + step0 * 32);
       }
     }
-    for (int tile = pair; tile < num_tiles; tile += n_pairs) {
-      int row0, n0;
-      origin(tile, row0, n0);
-      if constexpr (MODE == MODE_GATE) {
-        __syncwarp();
-        for (int i = lane; i < 128; i += 32) {
-          const int col = n0 + (i & 63);
-          bs[i] = p.bias != nullptr && col < p.N ? __bfloat162float(p.bias[(i >> 6) * (int64_t)p.N + col]) : 0.0f;
-        }
-        __syncwarp();
+    if constexpr (SPLIT) {
+      tile_ready = mbar_wait_warp<true>(&tmem_full[0], 0, wc);
+    } else {
+      for (int tile = first_tile; tile < p.tiles; tile += tile_step) {
+        if (!mbar_wait_warp<true>(&tmem_full[acc], acc_phase, wc)) break;
+        tc_fence_after();
+        int mt, nt, kb0, kb1;
+        const Sub& u = locate(tile, mt, nt, kb0, kb1);
+        if (!finish_tile(u, mt, nt, tile + tile_step)) break;
+        if (++acc == 2) { acc = 0; acc_phase ^= 1; }
       }
-      if (!mbar_wait_warp<true>(&tmem_full[acc], acc_phase, wc)) break;
-      tc_fence_after();
-      const uint32_t taddr = tmem_base + acc * BN + half * (TILE_COLS / 2) + ((uint32_t)(q * 32) << 16);
-      bool ok = true;
-#pragma unroll 1
-      for (int c = 0; c < kSteps; ++c, ++step) {
-        const int col = n0 + c * 32;
-        const bool inside = row0 < p.M && col < p.N;
-        if constexpr (MODE == MODE_GATE) {
-          uint32_t g[32], u[32];
-          tmem_ld32(taddr + c * 32, g);
-          tmem_ld32(taddr + BN / 2 + c * 32, u);
-          tmem_ld_wait();
-          if (c == kSteps - 1) {
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(tmem_empty_leader + acc * 8);
-          }
-          if (lane == 0) bulk_wait_read<0>();       // the boxes' last stores have left shared memory
-          __syncwarp();
+      finish_stores();
+    }
+  }
+
+  if constexpr (SPLIT) {
+    // Every thread of the cluster passes these barriers, whatever became of its waits.
+    cluster_sync();               // every pair's products are complete: the rings are free
+    tc_fence_after();
+    const uint32_t ring = smem_u32(smem);
+    if (warp >= 2 && tile_ready) {
+      for (int st = 0; st < kSteps; ++st) {
+        const int owner = st * split / kSteps, ls = st - owner * kSteps / split;
+        if (owner == slice || (ls & 1) != half) continue;
+        const int part = slice < owner ? slice : slice - 1;
+        const uint32_t to = map_to_rank(ring, (uint32_t)owner * 2 + rank) + (q * 32 + lane) * 4;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            uint32_t o4[4], g4[4], u4[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int i = 8 * j + 2 * e;
-              const float2 bg = *reinterpret_cast<const float2*>(bs + c * 32 + i);
-              const float2 bu = *reinterpret_cast<const float2*>(bs + 64 + c * 32 + i);
-              const float g0 = __uint_as_float(g[i]) + bg.x, g1 = __uint_as_float(g[i + 1]) + bg.y;
-              const float u0 = __uint_as_float(u[i]) + bu.x, u1 = __uint_as_float(u[i + 1]) + bu.y;
-              o4[e] = pack2(gate_act_fast<GATE>(g0) * u0, gate_act_fast<GATE>(g1) * u1);
-              g4[e] = pack2(g0, g1);
-              u4[e] = pack2(u0, u1);
-            }
-            *reinterpret_cast<uint4*>(box_piece(bufs, lane, j)) = make_uint4(o4[0], o4[1], o4[2], o4[3]);
-            if (p.save_pre) {
-              *reinterpret_cast<uint4*>(box_piece(bufs + kBufBytes, lane, j)) = make_uint4(g4[0], g4[1], g4[2], g4[3]);
-              *reinterpret_cast<uint4*>(box_piece(bufs + 2 * kBufBytes, lane, j)) = make_uint4(u4[0], u4[1], u4[2], u4[3]);
-            }
-          }
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          __syncwarp();
-          if (lane == 0) {
-            if (inside) {
-              tma_store_2d(&maps.o0, col, row0, bufs);
-              if (p.save_pre) {
-                tma_store_2d(&maps.o1, col, row0, bufs + kBufBytes);
-                tma_store_2d(&maps.o2, col, row0, bufs + 2 * kBufBytes);
-              }
-            }
-            bulk_commit();
-          }
-        } else if constexpr (MODE == MODE_GATE_GRAD) {
-          // the next step's g and u: into the pair of boxes whose store was issued two steps ago
-          int next_row = row0, next_col = col + 32;
-          bool more = true;
-          if (c == kSteps - 1) {
-            more = tile + n_pairs < num_tiles;
-            if (more) origin(tile + n_pairs, next_row, next_col);
-          }
-          if (more) {
-            if (lane == 0) bulk_wait_read<1>();
-            __syncwarp();
-            fetch_pre(next_row, next_col);
-          }
-          uint32_t da[32];
-          tmem_ld32(taddr + c * 32, da);
-          tmem_ld_wait();
-          if (c == kSteps - 1) {
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(tmem_empty_leader + acc * 8);
-          }
-          if (!mbar_wait_warp(&fbar[step % 3], (step / 3) & 1, wc)) { ok = false; break; }
-          uint8_t* gb = bufs + (step % 3) * 2 * kBufBytes;
-          uint8_t* ub = gb + kBufBytes;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            uint4* gp = reinterpret_cast<uint4*>(box_piece(gb, lane, j));
-            uint4* up = reinterpret_cast<uint4*>(box_piece(ub, lane, j));
-            const uint4 gv = *gp, uv = *up;
-            const uint32_t gw[4] = {gv.x, gv.y, gv.z, gv.w}, uw[4] = {uv.x, uv.y, uv.z, uv.w};
-            uint32_t dg4[4], du4[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float2 gf = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&gw[e]));
-              const float2 uf = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&uw[e]));
-              const float d0 = __uint_as_float(da[8 * j + 2 * e]), d1 = __uint_as_float(da[8 * j + 2 * e + 1]);
-              float a0, s0, a1, s1;
-              gate_act_slope_fast<GATE>(gf.x, &a0, &s0);
-              gate_act_slope_fast<GATE>(gf.y, &a1, &s1);
-              dg4[e] = pack2(d0 * uf.x * s0, d1 * uf.y * s1);
-              du4[e] = pack2(d0 * a0, d1 * a1);
-            }
-            *gp = make_uint4(dg4[0], dg4[1], dg4[2], dg4[3]);
-            *up = make_uint4(du4[0], du4[1], du4[2], du4[3]);
-          }
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          __syncwarp();
-          if (lane == 0) {
-            if (inside) {
-              tma_store_2d(&maps.o0, col, row0, gb);
-              tma_store_2d(&maps.o1, col, row0, ub);
-            }
-            bulk_commit();
-          }
-        } else {
+        for (int which = 0; which < kPer / 32; ++which) {
           uint32_t v[32];
-          tmem_ld32(taddr + c * 32, v);
+          tmem_ld32(tmem_base + ((uint32_t)(q * 32) << 16) + which * (BN / 2) + st * 32, v);
           tmem_ld_wait();
-          if (c == kSteps - 1) {
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(tmem_empty_leader + acc * 8);
-          }
-          uint8_t* buf = bufs + (step % 3) * kBufBytes;
-          if (lane == 0) bulk_wait_read<2>();       // the box's store three steps ago
-          __syncwarp();
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            uint32_t w[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = pack2(__uint_as_float(v[8 * j + 2 * e]), __uint_as_float(v[8 * j + 2 * e + 1]));
-            *reinterpret_cast<uint4*>(box_piece(buf, lane, j)) = make_uint4(w[0], w[1], w[2], w[3]);
-          }
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          __syncwarp();
-          if (lane == 0) {
-            if (inside) tma_store_2d(&maps.o0, col, row0, buf);
-            bulk_commit();
-          }
+          for (int i = 0; i < 32; ++i) store_cluster(to + partial_at(part, ls, which * 32 + i) * 4, v[i]);
         }
       }
-      if (!ok) break;
-      if (++acc == 2) { acc = 0; acc_phase ^= 1; }
     }
-    if (lane == 0) {
-      bulk_wait_all();
-      // after an abort: boxes asked for and not waited for are still on their way
-      for (uint32_t f = step; f < fetched; ++f) mbar_wait_drain(&fbar[f % 3], (f / 3) & 1);
+    cluster_sync();               // the parts' sums have arrived
+    if (warp >= 2) {
+      if (tile_ready) {
+        int mt, nt, kb0, kb1;
+        const Sub& u = locate(first_tile, mt, nt, kb0, kb1);
+        finish_tile(u, mt, nt, p.tiles);
+      }
+      finish_stores();
     }
-    __syncwarp();
   }
 
   // ------------------------------------------------------------------ teardown
   tc_fence_before();
-  __syncthreads();
-  if (*abort_flag) {
+  // one outcome for the whole CTA: the pair's other CTA may raise the flag at any moment
+  if (__syncthreads_or(*abort_flag != 0)) {
     // A wait expired, here or in the pair's other CTA.  Every role has left its loop and issues nothing more; what was issued
     // completes by itself and is waited for: the leader's producer waits for the last load of every stage (its barriers
     // count both CTAs' bytes), a commit behind the leader's products reaches both CTAs' drain barriers, the epilogue warps
@@ -500,7 +661,7 @@ gated_pair_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Pro
     if (warp == 0 && lane == 0 && rank == 0) drain_ring<true>(full, STAGES, loads_issued);
     if (warp == 1) {
       if (elect_one()) {
-        if (rank == 0) umma_commit_both(drain_bar);
+        if (rank == 0) umma_commit_both(drain_bar, leader);
         mbar_wait_drain<true>(drain_bar, 0);
       }
       __syncwarp();
@@ -549,30 +710,22 @@ bool box_map(CUtensorMap* tm, const void* base, int64_t rows, int64_t cols, int6
   return make_tensor_map_2d(tm, base, rows, cols, ld * 2, 32, 32, 2, CU_TENSOR_MAP_SWIZZLE_64B);
 }
 
+int64_t tiles_of(int64_t M, int64_t N, int tile_cols) { return ((M + 2 * BM - 1) / (2 * BM)) * ((N + tile_cols - 1) / tile_cols); }
+
+// Pairs the device runs at once (SMs pair up inside a GPC, so this can be below SMs / 2).
 template <int MODE, int GATE>
-cudaError_t launch(const Maps& maps, Problem p, cudaStream_t s) {
-  using L = Smem<MODE>;
-  auto kern = gated_pair_kernel<MODE, GATE>;
-  static PerDeviceOnce configured;
-  cudaError_t e = once_per_device(configured, [&] {
-    return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kDynamic);
-  });
-  if (e != cudaSuccess) return e;
-  constexpr int tile_cols = MODE == MODE_GATE ? BN / 2 : BN;
-  const int64_t tiles = (int64_t)((p.M + 2 * BM - 1) / (2 * BM)) * ((p.N + tile_cols - 1) / tile_cols);
-  if (tiles > 0x3fffffff) return cudaErrorInvalidValue;
-  // pairs that can be resident at once on this device (SMs pair up inside a GPC, so this can be below SMs / 2)
-  static PerDeviceInt resident;
+cudaError_t resident_pairs(int* out) {
+  static PerDeviceInt cache;
   int dev = 0;
   cudaGetDevice(&dev);
   const int slot = dev >= 0 && dev < 64 ? dev : 0;
-  int max_pairs = resident.v[slot].load(std::memory_order_relaxed);
-  if (max_pairs == 0 || slot != dev) {
+  int n = cache.v[slot].load(std::memory_order_relaxed);
+  if (n == 0 || slot != dev) {
     const int sms = device_sm_count();
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(sms / 2 * 2);
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = L::kDynamic;
+    cfg.dynamicSmemBytes = Smem<MODE>::kDynamic;
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeClusterDimension;
     attr.val.clusterDim.x = 2;
@@ -580,18 +733,73 @@ cudaError_t launch(const Maps& maps, Problem p, cudaStream_t s) {
     attr.val.clusterDim.z = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess || n <= 0) {
+    if (cudaOccupancyMaxActiveClusters(&n, gated_pair_kernel<MODE, GATE, false>, &cfg) != cudaSuccess || n <= 0) {
       (void)cudaGetLastError();
       n = sms / 2;
     }
-    max_pairs = n < sms / 2 ? n : sms / 2;
-    if (slot == dev) resident.v[slot].store(max_pairs, std::memory_order_relaxed);
+    n = n < sms / 2 ? n : sms / 2;
+    if (slot == dev) cache.v[slot].store(n, std::memory_order_relaxed);
   }
-  const int avail = limited_sms(2 * max_pairs) / 2 > 0 ? limited_sms(2 * max_pairs) / 2 : 1;
-  const int pairs = tiles < avail ? (int)tiles : avail;
+  *out = n;
+  return cudaSuccess;
+}
+
+template <int MODE, int GATE, bool SPLIT>
+cudaError_t launch(Problem& p, cudaStream_t s) {
+  using L = Smem<MODE>;
+  auto kern = gated_pair_kernel<MODE, GATE, SPLIT>;
+  static PerDeviceOnce configured;
+  cudaError_t e = once_per_device(configured, [&] {
+    return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kDynamic);
+  });
+  if (e != cudaSuccess) return e;
+  const int cluster = 2 * p.split;
   p.wait_limit = wait_limit_cycles();
-  return launch_pdl(kern, dim3(2 * pairs), dim3(kThreads), L::kDynamic, s, maps, p);
+  cudaLaunchConfig_t cfg = {};
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = L::kDynamic;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cluster;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  if constexpr (!SPLIT) {
+    int pairs = 0;
+    e = resident_pairs<MODE, GATE>(&pairs);
+    if (e != cudaSuccess) return e;
+    const int avail = limited_sms(2 * pairs) / 2 > 0 ? limited_sms(2 * pairs) / 2 : 1;
+    cfg.gridDim = dim3(2 * (p.tiles < avail ? p.tiles : avail));
+    return cudaLaunchKernelEx(&cfg, kern, p);
+  }
+  // one cluster per tile; under an SM budget as many launches as keep to it
+  const int most = sm_limit() > 0 ? (sm_limit() / cluster > 0 ? sm_limit() / cluster : 1) : p.tiles;
+  for (p.tile0 = 0; p.tile0 < p.tiles; p.tile0 += most) {
+    const int now = p.tiles - p.tile0 < most ? p.tiles - p.tile0 : most;
+    cfg.gridDim = dim3(now * cluster);
+    e = cudaLaunchKernelEx(&cfg, kern, p);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+
+// Parts of the contraction for a launch of `tiles` tiles whose shortest contraction has `blocks` blocks.  All clusters are to
+// be resident at once: 33 of 4 CTAs, 15 of 8 on a device of 148 SMs (its GPCs do not all hold a multiple of 8).  Adding up
+// the parts costs about as much as 14 to 16 blocks.  The choice goes by sizes alone (not by an SM budget): the same call
+// gives the same bits.
+int choose_split(int64_t tiles, int blocks) {
+  if (tiles <= 15 && blocks / 4 + 16 < blocks / 2 + 14 && blocks / 4 + 16 < blocks) return 4;
+  if (tiles <= 33 && blocks / 2 + 14 < blocks) return 2;
+  return 1;
+}
+
+template <int MODE, int GATE>
+cudaError_t launch_either(Problem& p, cudaStream_t s) {
+  return p.split > 1 ? launch<MODE, GATE, true>(p, s) : launch<MODE, GATE, false>(p, s);
 }
 
 bool matrix_ok(const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; }
@@ -607,54 +815,140 @@ bool gated_tc_supported(std::initializer_list<MatrixArg> matrices, std::initiali
 }
 
 cudaError_t gated_tc_forward(const void* x, int64_t ldx, const void* w, int64_t ldw, const void* bias, void* out, int64_t ldo,
-                             void* pre, int64_t ldp, int64_t M, int64_t N, int64_t K, int gate, int* status,
-                             cudaStream_t s) {
-  Maps m = {};
-  if (!operand_map(&m.a, x, M, K, ldx, false) || !operand_map(&m.b, w, 2 * N, K, ldw, false) ||
-      !box_map(&m.o0, out, M, N, ldo))
+                             void* pre, int64_t ldp, int64_t M, int64_t N, int64_t K, int gate, cudaStream_t s) {
+  Problem p = {};
+  Sub& u = p.sub[0];
+  if (!operand_map(&u.a, x, M, K, ldx, false) || !operand_map(&u.b, w, 2 * N, K, ldw, false) ||
+      !box_map(&u.out, out, M, N, ldo))
     return cudaErrorInvalidValue;
   if (pre) {
     __nv_bfloat16* g = static_cast<__nv_bfloat16*>(pre);
-    if (!box_map(&m.o1, g, M, N, ldp) || !box_map(&m.o2, g + N, M, N, ldp)) return cudaErrorInvalidValue;
+    if (!box_map(&p.o1, g, M, N, ldp) || !box_map(&p.o2, g + N, M, N, ldp)) return cudaErrorInvalidValue;
   }
-  Problem p = {};
-  p.M = (int)M; p.N = (int)N; p.K = (int)K;
+  u.M = (int)M; u.N = (int)N; u.K = (int)K;
+  u.order = choose_order(M, 2 * N, K, 2 * BM, BN);
+  p.subs = 1;
+  const int64_t tiles = tiles_of(M, N, BN / 2);
+  if (tiles > (1 << 28)) return cudaErrorInvalidValue;
+  p.tiles = (int)tiles;
+  p.split = choose_split(tiles, (int)((K + BK - 1) / BK));
   p.save_pre = pre != nullptr;
   p.bias = static_cast<const __nv_bfloat16*>(bias);
-  p.order = choose_order(M, 2 * N, K, 2 * BM, BN);
-  p.status = status;
-  if (gate == EPD_GATE_SILU) return launch<MODE_GATE, EPD_GATE_SILU>(m, p, s);
-  if (gate == EPD_GATE_GELU_TANH) return launch<MODE_GATE, EPD_GATE_GELU_TANH>(m, p, s);
-  return launch<MODE_GATE, EPD_GATE_GELU_ERF>(m, p, s);
+  if (gate == EPD_GATE_SILU) return launch_either<MODE_GATE, EPD_GATE_SILU>(p, s);
+  if (gate == EPD_GATE_GELU_TANH) return launch_either<MODE_GATE, EPD_GATE_GELU_TANH>(p, s);
+  return launch_either<MODE_GATE, EPD_GATE_GELU_ERF>(p, s);
 }
 
 cudaError_t gated_tc_gradient(const void* dout, int64_t lddo, const void* w_out, int64_t ldw, const void* pre, int64_t ldp,
-                              void* dpre, int64_t lddp, int64_t M, int64_t N, int64_t D, int gate, cudaStream_t s) {
-  Maps m = {};
+                              void* dpre, int64_t lddp, float* sums, int64_t M, int64_t N, int64_t D, int gate,
+                              cudaStream_t s) {
+  Problem p = {};
+  Sub& u = p.sub[0];
   const __nv_bfloat16* g = static_cast<const __nv_bfloat16*>(pre);
   __nv_bfloat16* dg = static_cast<__nv_bfloat16*>(dpre);
-  if (!operand_map(&m.a, dout, M, D, lddo, false) || !operand_map(&m.b, w_out, N, D, ldw, true) ||
-      !box_map(&m.l0, g, M, N, ldp) || !box_map(&m.l1, g + N, M, N, ldp) || !box_map(&m.o0, dg, M, N, lddp) ||
-      !box_map(&m.o1, dg + N, M, N, lddp))
+  if (!operand_map(&u.a, dout, M, D, lddo, false) || !operand_map(&u.b, w_out, N, D, ldw, true) ||
+      !box_map(&p.l0, g, M, N, ldp) || !box_map(&p.l1, g + N, M, N, ldp) || !box_map(&u.out, dg, M, N, lddp) ||
+      !box_map(&p.o1, dg + N, M, N, lddp))
     return cudaErrorInvalidValue;
-  Problem p = {};
-  p.M = (int)M; p.N = (int)N; p.K = (int)D;
-  p.order = choose_order(M, N, D, 2 * BM, BN);
-  if (gate == EPD_GATE_SILU) return launch<MODE_GATE_GRAD, EPD_GATE_SILU>(m, p, s);
-  if (gate == EPD_GATE_GELU_TANH) return launch<MODE_GATE_GRAD, EPD_GATE_GELU_TANH>(m, p, s);
-  return launch<MODE_GATE_GRAD, EPD_GATE_GELU_ERF>(m, p, s);
+  u.M = (int)M; u.N = (int)N; u.K = (int)D;
+  u.order = choose_order(M, N, D, 2 * BM, BN);
+  p.subs = 1;
+  const int64_t tiles = tiles_of(M, N, BN);
+  if (tiles > (1 << 28)) return cudaErrorInvalidValue;
+  p.tiles = (int)tiles;
+  p.split = choose_split(tiles, (int)((D + BK - 1) / BK));
+  p.sums = sums;
+  if (gate == EPD_GATE_SILU) return launch_either<MODE_GATE_GRAD, EPD_GATE_SILU>(p, s);
+  if (gate == EPD_GATE_GELU_TANH) return launch_either<MODE_GATE_GRAD, EPD_GATE_GELU_TANH>(p, s);
+  return launch_either<MODE_GATE_GRAD, EPD_GATE_GELU_ERF>(p, s);
 }
 
-// out[M, N] = A . B with A [M, K] (or, a_mn, [K, M]) and B [K, N].
-cudaError_t matmul_tc(bool a_mn, const void* a, int64_t lda, const void* b, int64_t ldb, void* out, int64_t ldo, int64_t M,
-                      int64_t N, int64_t K, cudaStream_t s) {
-  Maps m = {};
-  if (!operand_map(&m.a, a, M, K, lda, a_mn) || !operand_map(&m.b, b, N, K, ldb, true) || !box_map(&m.o0, out, M, N, ldo))
-    return cudaErrorInvalidValue;
+bool linear_tc_split_pays(int64_t M, int64_t N, int64_t K) {
+  return choose_split(tiles_of(M, N, BN), (int)((K + BK - 1) / BK)) > 1;
+}
+
+cudaError_t linear_tc_split(const void* x, int64_t ldx, const void* w, int64_t ldw, const void* bias, void* out, int64_t ldo,
+                            int64_t M, int64_t N, int64_t K, int flags, cudaStream_t s) {
   Problem p = {};
-  p.M = (int)M; p.N = (int)N; p.K = (int)K;
-  p.order = choose_order(M, N, K, 2 * BM, BN);
-  return a_mn ? launch<MODE_TN, 0>(m, p, s) : launch<MODE_NN, 0>(m, p, s);
+  Sub& u = p.sub[0];
+  p.out_f32 = (flags & (EPD_LINEAR_ACCUMULATE | EPD_LINEAR_OUT_F32)) != 0;
+  p.accumulate = (flags & EPD_LINEAR_ACCUMULATE) != 0;
+  if (!operand_map(&u.a, x, M, K, ldx, false) || !operand_map(&u.b, w, N, K, ldw, false)) return cudaErrorInvalidValue;
+  if (!(p.out_f32 ? make_tensor_map_2d(&u.out, out, M, N, ldo * 4, 32, 32, 4, CU_TENSOR_MAP_SWIZZLE_128B)
+                  : box_map(&u.out, out, M, N, ldo)))
+    return cudaErrorInvalidValue;
+  u.M = (int)M; u.N = (int)N; u.K = (int)K;
+  u.order = choose_order(M, N, K, 2 * BM, BN);
+  p.subs = 1;
+  p.tiles = (int)tiles_of(M, N, BN);
+  p.split = choose_split(p.tiles, (int)((K + BK - 1) / BK));
+  if (p.split < 2) return cudaErrorInvalidValue;
+  p.bias = static_cast<const __nv_bfloat16*>(bias);
+  return launch<MODE_LINEAR, 0, true>(p, s);
+}
+
+// Time of a launch of whole tiles in contraction blocks, with the products in the given order: the pair that starts with tile 0
+// has the most.  A tile costs its blocks and about 3 more (the first loads, the epilogue's exposed part).
+static int64_t rounds_cost(const ProductArg* const* list, int n, int pairs) {
+  int64_t cost = 0, tile = 0;
+  for (int i = 0; i < n; ++i) {
+    const int64_t tiles = tiles_of(list[i]->M, list[i]->N, BN), len = (list[i]->K + BK - 1) / BK + 3;
+    const int64_t from = (pairs - tile % pairs) % pairs;      // its first tile that falls to the first pair
+    if (from < tiles) cost += ((tiles - from + pairs - 1) / pairs) * len;
+    else if (i + 1 == n && cost == 0) cost = len;
+    tile += tiles;
+  }
+  return cost;
+}
+
+cudaError_t matmul_tc_group(const ProductArg* list, int n, cudaStream_t s) {
+  // longest contraction first: what is left over at the end is short
+  const ProductArg* sorted[kSubs];
+  int m = 0;
+  for (int i = 0; i < n && m < kSubs; ++i) sorted[m++] = &list[i];
+  for (int i = 1; i < m; ++i)
+    for (int j = i; j > 0 && sorted[j]->K > sorted[j - 1]->K; --j) { const ProductArg* t = sorted[j]; sorted[j] = sorted[j - 1]; sorted[j - 1] = t; }
+  const int pairs = device_sm_count() / 2;
+  // One launch for all, or one launch each, which may share tiles among pairs (about 12 blocks' time for a launch).  Products
+  // that are not asked for count as well: a result's bits do not depend on what else is formed.
+  int64_t apart = 0;
+  for (int i = 0; i < m; ++i) {
+    const int64_t tiles = tiles_of(sorted[i]->M, sorted[i]->N, BN);
+    const int blocks = (int)((sorted[i]->K + BK - 1) / BK), split = choose_split(tiles, blocks);
+    apart += split > 1 ? blocks / split + 6 : rounds_cost(&sorted[i], 1, pairs);
+    if (i > 0) apart += 12;
+  }
+  const bool together = rounds_cost(sorted, m, pairs) <= apart;
+  for (int first = 0; first < m;) {
+    const int count = together ? m : 1;
+    Problem p = {};
+    int64_t tiles = 0, all_tiles = 0;
+    int shortest = 1 << 30;
+    for (int i = 0; i < count; ++i) {
+      const ProductArg& a = *sorted[first + i];
+      const int blocks = (int)((a.K + BK - 1) / BK);
+      shortest = blocks < shortest ? blocks : shortest;
+      all_tiles += tiles_of(a.M, a.N, BN);
+      if (!a.out) continue;
+      Sub& u = p.sub[p.subs++];
+      if (!operand_map(&u.a, a.a, a.M, a.K, a.lda, a.a_mn) || !operand_map(&u.b, a.b, a.N, a.K, a.ldb, true) ||
+          !box_map(&u.out, a.out, a.M, a.N, a.ldo))
+        return cudaErrorInvalidValue;
+      u.M = (int)a.M; u.N = (int)a.N; u.K = (int)a.K;
+      u.a_mn = a.a_mn;
+      u.first = (int)tiles;
+      u.order = choose_order(a.M, a.N, a.K, 2 * BM, BN);
+      tiles += tiles_of(a.M, a.N, BN);
+      if (tiles > (1 << 28)) return cudaErrorInvalidValue;
+    }
+    first += count;
+    if (p.subs == 0) continue;
+    p.tiles = (int)tiles;
+    p.split = choose_split(all_tiles, shortest);
+    const cudaError_t e = launch_either<MODE_GROUP, 0>(p, s);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
 }
 
 }  // namespace epd
