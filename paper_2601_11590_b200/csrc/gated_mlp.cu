@@ -11,11 +11,14 @@ namespace {
 
 // =============================================================================================
 // Matrix product with plain FMAs: out[m, n] = sum_k A(m, k) B(n, k), every operand either contraction-contiguous
-// ("K-major": element (r, k) at r * ld + k) or row-contiguous ("MN-major": at k * ld + r).  128 x 128 tile,
-// 256 threads with 8 x 8 outputs each (two groups of 4 rows by two groups of 4 columns), the next block of the
-// contraction fetched into registers while the present one is multiplied.
+// ("K-major": element (r, k) at r * ld + k) or row-contiguous ("MN-major": at k * ld + r).  TM x TN tile, RM x RN outputs per
+// thread in two groups of rows by two groups of columns (the gated product keeps a column's gate in the first group and its
+// up projection in the second), two outputs per instruction (fma.rn.f32x2), the next block of the contraction fetched into
+// registers while the present one is multiplied out of one of two buffers.  Bound by the FMA pipe.
+// Where the tiles are fewer than the SMs, the 2, 4 or 8 CTAs of a cluster share a tile, each with a part of the contraction;
+// each then adds up some of the rows from all parts, in order, out of the others' shared memory.
 // =============================================================================================
-constexpr int FT = 128, FK = 8;
+constexpr int FK = 16;
 
 enum { EPI_PLAIN = 0, EPI_GATE = 1, EPI_GATE_GRAD = 2 };
 
@@ -25,6 +28,7 @@ struct FmaArgs {
   int64_t M, N, K;
   void* out;                 // PLAIN: [M, N]; GATE: a [M, N]; GATE_GRAD: unused
   int64_t ldo;
+  int accumulate;            // PLAIN: out +=
   void* pre;                 // GATE: g|u [M, 2N] to write, or NULL; GATE_GRAD: g|u to read
   int64_t ldp;
   void* dpre;                // GATE_GRAD: dg|du [M, 2N]
@@ -32,77 +36,159 @@ struct FmaArgs {
   int gate;
 };
 
-template <typename T, bool A_MN, bool B_MN, int EPI>
-__global__ void __launch_bounds__(256)
-matmul_fma_kernel(const FmaArgs p) {
-  __shared__ float sa[FK][FT + 4];
-  __shared__ float sb[FK][FT + 4];
-  constexpr int COLS = EPI == EPI_GATE ? FT / 2 : FT;     // output columns of a tile
+__device__ __forceinline__ uint64_t pair_of(float a) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %1};" : "=l"(r) : "f"(a));
+  return r;
+}
+__device__ __forceinline__ void fma_pair(uint64_t& c, uint64_t a, uint64_t b) {
+  asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(c) : "l"(a), "l"(b));
+}
+
+template <int TM, int TN>
+struct FmaTile {
+  static constexpr int kPadM = TM + 4, kPadN = TN + 4;
+  static constexpr int kFloats = 2 * FK * (kPadM + kPadN);
+  static_assert(kFloats >= TM * TN || TM > 64, "a shared tile's sums take the place of its buffers");
+};
+
+template <typename T, int TM, int TN, int RM, int RN, bool A_MN, bool B_MN, int EPI>
+__global__ void __launch_bounds__((TM / RM) * (TN / RN))
+matmul_fma_kernel(const FmaArgs p, const int split) {
+  using L = FmaTile<TM, TN>;
+  constexpr int kThreads = (TM / RM) * (TN / RN);
+  constexpr int LA = TM * FK / kThreads, LB = TN * FK / kThreads;
+  constexpr int COLS = EPI == EPI_GATE ? TN / 2 : TN;     // output columns of a tile
+  __shared__ __align__(16) float smem[L::kFloats];
+  float* const sa = smem;
+  float* const sb = smem + 2 * FK * L::kPadM;
   const T* A = static_cast<const T*>(p.a);
   const T* B = static_cast<const T*>(p.b);
-  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-  const int64_t m0 = (int64_t)blockIdx.x * FT, n0 = (int64_t)blockIdx.y * COLS;
-  float ra[4], rb[4];
+  const int tx = threadIdx.x % (TN / RN), ty = threadIdx.x / (TN / RN);
+  const int part = blockIdx.x % split;
+  const int64_t m0 = (int64_t)(blockIdx.x / split) * TM, n0 = (int64_t)blockIdx.y * COLS;
+  const int64_t blocks = (p.K + FK - 1) / FK;
+  const int64_t b0 = part * blocks / split, b1 = (part + 1) * blocks / split;
+  float ra[LA], rb[LB];
   auto fetch = [&](int64_t k0) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int e = threadIdx.x + 256 * i;
-      {
-        const int r = A_MN ? e % FT : e / FK, kk = A_MN ? e / FT : e % FK;
-        const int64_t m = m0 + r, k = k0 + kk;
-        ra[i] = (m < p.M && k < p.K) ? to_float<T>(A_MN ? A[k * p.lda + m] : A[m * p.lda + k]) : 0.0f;
-      }
-      {
-        const int r = B_MN ? e % FT : e / FK, kk = B_MN ? e / FT : e % FK;
-        // gated: the tile's second half of columns is the up projection of the first half's
-        const int64_t c = n0 + (EPI == EPI_GATE ? r % COLS : r), k = k0 + kk;
-        const int64_t n = EPI == EPI_GATE && r >= COLS ? p.N + c : c;
-        rb[i] = (c < p.N && k < p.K) ? to_float<T>(B_MN ? B[k * p.ldb + n] : B[n * p.ldb + k]) : 0.0f;
-      }
+    for (int i = 0; i < LA; ++i) {
+      const int e = threadIdx.x + kThreads * i;
+      const int r = A_MN ? e % TM : e / FK, kk = A_MN ? e / TM : e % FK;
+      const int64_t m = m0 + r, k = k0 + kk;
+      ra[i] = (m < p.M && k < p.K) ? to_float<T>(A_MN ? A[k * p.lda + m] : A[m * p.lda + k]) : 0.0f;
     }
-  };
-  auto put = [&] {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int e = threadIdx.x + 256 * i;
-      sa[A_MN ? e / FT : e % FK][A_MN ? e % FT : e / FK] = ra[i];
-      sb[B_MN ? e / FT : e % FK][B_MN ? e % FT : e / FK] = rb[i];
+    for (int i = 0; i < LB; ++i) {
+      const int e = threadIdx.x + kThreads * i;
+      const int r = B_MN ? e % TN : e / FK, kk = B_MN ? e / TN : e % FK;
+      // gated: the tile's second half of columns is the up projection of the first half's
+      const int64_t c = n0 + (EPI == EPI_GATE ? r % COLS : r), k = k0 + kk;
+      const int64_t n = EPI == EPI_GATE && r >= COLS ? p.N + c : c;
+      rb[i] = (c < p.N && k < p.K) ? to_float<T>(B_MN ? B[k * p.ldb + n] : B[n * p.ldb + k]) : 0.0f;
     }
   };
-  float acc[8][8] = {};
-  fetch(0);
-  for (int64_t k0 = 0; k0 < p.K; k0 += FK) {
-    put();
-    __syncthreads();
-    if (k0 + FK < p.K) fetch(k0 + FK);
+  auto put = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < LA; ++i) {
+      const int e = threadIdx.x + kThreads * i;
+      sa[(buf * FK + (A_MN ? e / TM : e % FK)) * L::kPadM + (A_MN ? e % TM : e / FK)] = ra[i];
+    }
+#pragma unroll
+    for (int i = 0; i < LB; ++i) {
+      const int e = threadIdx.x + kThreads * i;
+      sb[(buf * FK + (B_MN ? e / TN : e % FK)) * L::kPadN + (B_MN ? e % TN : e / FK)] = rb[i];
+    }
+  };
+  uint64_t acc2[RM][RN / 2] = {};
+  if (b0 < b1) {
+    fetch(b0 * FK);
+    put(0);
+  }
+  __syncthreads();
+  int buf = 0;
+  for (int64_t b = b0; b < b1; ++b, buf ^= 1) {
+    if (b + 1 < b1) fetch((b + 1) * FK);
 #pragma unroll
     for (int kk = 0; kk < FK; ++kk) {
-      float a[8], b[8];
-      *reinterpret_cast<float4*>(a) = *reinterpret_cast<const float4*>(&sa[kk][ty * 4]);
-      *reinterpret_cast<float4*>(a + 4) = *reinterpret_cast<const float4*>(&sa[kk][64 + ty * 4]);
-      *reinterpret_cast<float4*>(b) = *reinterpret_cast<const float4*>(&sb[kk][tx * 4]);
-      *reinterpret_cast<float4*>(b + 4) = *reinterpret_cast<const float4*>(&sb[kk][64 + tx * 4]);
+      const float* ka = sa + (buf * FK + kk) * L::kPadM + ty * (RM / 2);
+      const float* kb = sb + (buf * FK + kk) * L::kPadN + tx * (RN / 2);
+      alignas(16) float a[RM];
+      alignas(16) uint64_t bv[RN / 2];
+      static_assert(RM == 8, "rows in two groups of four");
+      *reinterpret_cast<float4*>(a) = *reinterpret_cast<const float4*>(ka);
+      *reinterpret_cast<float4*>(a + 4) = *reinterpret_cast<const float4*>(ka + TM / 2);
+      if constexpr (RN == 8) {
+        *reinterpret_cast<float4*>(bv) = *reinterpret_cast<const float4*>(kb);
+        *reinterpret_cast<float4*>(bv + 2) = *reinterpret_cast<const float4*>(kb + TN / 2);
+      } else {
+        bv[0] = *reinterpret_cast<const uint64_t*>(kb);
+        bv[1] = *reinterpret_cast<const uint64_t*>(kb + TN / 2);
+      }
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
+      for (int i = 0; i < RM; ++i) {
+        const uint64_t av = pair_of(a[i]);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc[i][j] = fmaf(a[i], b[j], acc[i][j]);
+        for (int j = 0; j < RN / 2; ++j) fma_pair(acc2[i][j], av, bv[j]);
+      }
     }
+    if (b + 1 < b1) put(buf ^ 1);
     __syncthreads();
+  }
+  float acc[RM][RN];
+#pragma unroll
+  for (int i = 0; i < RM; ++i)
+#pragma unroll
+    for (int j = 0; j < RN / 2; ++j)
+      asm("mov.b64 {%0, %1}, %2;" : "=f"(acc[i][2 * j]), "=f"(acc[i][2 * j + 1]) : "l"(acc2[i][j]));
+  int i0 = 0, i1 = RM;          // rows of acc this CTA finishes
+  if constexpr (TM <= 64) {
+    if (split > 1) {
+      // sums by (row, column) of the thread, then by thread
+#pragma unroll
+      for (int i = 0; i < RM; ++i)
+#pragma unroll
+        for (int j = 0; j < RN; ++j) smem[(i * RN + j) * kThreads + threadIdx.x] = acc[i][j];
+      asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+      i0 = part * RM / split;
+      i1 = (part + 1) * RM / split;
+      const uint32_t own = (uint32_t)__cvta_generic_to_shared(smem + threadIdx.x);
+#pragma unroll
+      for (int i = 0; i < RM; ++i) {
+        if (i < i0 || i >= i1) continue;
+#pragma unroll
+        for (int j = 0; j < RN; ++j) acc[i][j] = 0.0f;
+        for (int o = 0; o < split; ++o) {
+          uint32_t at;
+          asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(own), "r"(o));
+#pragma unroll
+          for (int j = 0; j < RN; ++j) {
+            float v;
+            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at + (uint32_t)((i * RN + j) * kThreads * 4)));
+            acc[i][j] += v;
+          }
+        }
+      }
+      // nobody's shared memory goes away while another may still read it
+      asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    }
   }
   const T* bias = static_cast<const T*>(p.bias);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int64_t m = m0 + (i < 4 ? ty * 4 + i : 64 + ty * 4 + i - 4);
-    if (m >= p.M) continue;
+  for (int i = 0; i < RM; ++i) {
+    const int64_t m = m0 + (i < RM / 2 ? ty * (RM / 2) + i : TM / 2 + ty * (RM / 2) + i - RM / 2);
+    if (i < i0 || i >= i1 || m >= p.M) continue;
 #pragma unroll
-    for (int j = 0; j < (EPI == EPI_GATE ? 4 : 8); ++j) {
-      const int64_t n = n0 + (j < 4 ? tx * 4 + j : 64 + tx * 4 + j - 4);
+    for (int j = 0; j < (EPI == EPI_GATE ? RN / 2 : RN); ++j) {
+      const int64_t n = n0 + (j < RN / 2 ? tx * (RN / 2) + j : TN / 2 + tx * (RN / 2) + j - RN / 2);
       if (n >= p.N) continue;
       if constexpr (EPI == EPI_PLAIN) {
-        static_cast<T*>(p.out)[m * p.ldo + n] = from_float<T>(acc[i][j] + (bias ? to_float<T>(bias[n]) : 0.0f));
+        T* o = static_cast<T*>(p.out) + m * p.ldo + n;
+        const float v = acc[i][j] + (bias ? to_float<T>(bias[n]) : 0.0f);
+        *o = from_float<T>(p.accumulate ? to_float<T>(*o) + v : v);
       } else if constexpr (EPI == EPI_GATE) {
         const float g = acc[i][j] + (bias ? to_float<T>(bias[n]) : 0.0f);
-        const float u = acc[i][j + 4] + (bias ? to_float<T>(bias[p.N + n]) : 0.0f);
+        const float u = acc[i][j + RN / 2] + (bias ? to_float<T>(bias[p.N + n]) : 0.0f);
         static_cast<T*>(p.out)[m * p.ldo + n] = from_float<T>(gate_act(p.gate, g) * u);
         if (p.pre) {
           static_cast<T*>(p.pre)[m * p.ldp + n] = from_float<T>(g);
@@ -120,18 +206,35 @@ matmul_fma_kernel(const FmaArgs p) {
   }
 }
 
-template <typename T, bool A_MN, bool B_MN, int EPI>
-cudaError_t matmul_fma_t(const FmaArgs& p, cudaStream_t s) {
-  const int64_t cols = EPI == EPI_GATE ? FT / 2 : FT;
-  const int64_t gx = (p.M + FT - 1) / FT, gy = (p.N + cols - 1) / cols;
+template <typename T, int TILE, int RN, bool A_MN, bool B_MN, int EPI>
+cudaError_t matmul_fma_t(const FmaArgs& p, int split, cudaStream_t s) {
+  const int64_t cols = EPI == EPI_GATE ? TILE / 2 : TILE;
+  const int64_t gx = (p.M + TILE - 1) / TILE * split, gy = (p.N + cols - 1) / cols;
   if (gx > 0x7fffffff || gy > 65535) return cudaErrorInvalidValue;
-  matmul_fma_kernel<T, A_MN, B_MN, EPI><<<dim3((unsigned)gx, (unsigned)gy), 256, 0, s>>>(p);
-  return cudaGetLastError();
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)gx, (unsigned)gy);
+  cfg.blockDim = dim3((TILE / 8) * (TILE / RN));
+  cfg.stream = s;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = split;
+  attr.val.clusterDim.y = 1;
+  attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = split > 1 ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, matmul_fma_kernel<T, TILE, TILE, 8, RN, A_MN, B_MN, EPI>, p, split);
 }
+// 128 x 128 tiles where they fill the SMs, else 64 x 64, and as many CTAs per tile as fill the SMs twice and leave each at least
+// 4 blocks of the contraction.
 template <bool A_MN, bool B_MN, int EPI>
 cudaError_t matmul_fma(int dtype, const FmaArgs& p, cudaStream_t s) {
-  return dtype == EPD_DTYPE_F32 ? matmul_fma_t<float, A_MN, B_MN, EPI>(p, s)
-                                : matmul_fma_t<__nv_bfloat16, A_MN, B_MN, EPI>(p, s);
+  const int64_t n = EPI == EPI_GATE ? 2 * p.N : p.N;
+  const int64_t large = ((p.M + 127) / 128) * ((n + 127) / 128), small = ((p.M + 63) / 64) * ((n + 63) / 64);
+  if (large >= 148 && dtype == EPD_DTYPE_F32) return matmul_fma_t<float, 128, 8, A_MN, B_MN, EPI>(p, 1, s);
+  int split = 1;
+  while (split < 8 && small * split * 2 <= 2 * 148 && (p.K + FK - 1) / FK >= 8 * split) split *= 2;
+  return dtype == EPD_DTYPE_F32 ? matmul_fma_t<float, 64, 4, A_MN, B_MN, EPI>(p, split, s)
+                                : matmul_fma_t<__nv_bfloat16, 64, 4, A_MN, B_MN, EPI>(p, split, s);
 }
 
 // =============================================================================================
@@ -378,6 +481,16 @@ int epd_op_gated_mlp(int32_t dtype, const void* x, int64_t ldx, const void* w_in
   if (dtype == EPD_DTYPE_BF16 && ldo % 8 == 0 && linear_tc_split_pays(M, D, N) &&
       gated_tc_supported({{hidden, ldh}, {w_out, ldw_out}, {out, ldo}}, {D, N}))
     return finish(linear_tc_split(hidden, ldh, w_out, ldw_out, b_out, out, ldo, M, D, N, flags, s));
+  if (dtype == EPD_DTYPE_F32) {
+    FmaArgs p = {};
+    p.a = hidden; p.lda = ldh;
+    p.b = w_out; p.ldb = ldw_out;
+    p.bias = b_out;
+    p.out = out; p.ldo = ldo;
+    p.accumulate = (flags & EPD_LINEAR_ACCUMULATE) != 0;
+    p.M = M; p.N = D; p.K = N;
+    return finish(matmul_fma<false, false, EPI_PLAIN>(dtype, p, s));
+  }
   return epd_op_linear(dtype, hidden, ldh, w_out, ldw_out, b_out, out, ldo, M, D, N, flags, stream);
 }
 
