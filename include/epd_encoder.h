@@ -413,10 +413,15 @@ enum { EPD_GATE_SILU = 0, EPD_GATE_GELU_TANH = 1, EPD_GATE_GELU_ERF = 2 };   /* 
  * x, w, bias, out, pre: element type per dtype; sums are held in float.  Leading dimensions in elements.  Outputs must
  * not overlap inputs or each other.  In bf16 the tensor-core kernels run when N, K and every leading dimension are
  * multiples of 8 and every matrix starts on a 16-byte boundary; other shapes run on a plain-FMA kernel.
+ * workspace: device memory, 256-byte aligned, of epd_gated_mlp_workspace_bytes(dtype, M, N, K, D) bytes (D = 0 for this call
+ * alone), free again once the call's work has run; calls that may overlap on the device need one each.  It is used for large
+ * float blocks, whose products then run on the tensor cores with the precision of float (a float as the sum of three bf16
+ * numbers; an infinity in an operand gives NaN there); the size is 0 otherwise.  NULL: plain FMAs, with the same precision.
  * M == 0 is valid and launches nothing.  Extents up to 2^28; EPD_EINVAL otherwise. */
+size_t epd_gated_mlp_workspace_bytes(int32_t dtype, int64_t M, int64_t N, int64_t K, int64_t D);
 int epd_op_gated_linear(int32_t dtype, const void* x, int64_t ldx, const void* w, int64_t ldw, const void* bias, void* out,
-                        int64_t ldo, void* pre, int64_t ldp, int64_t M, int64_t N, int64_t K, int32_t gate,
-                        void* stream);
+                        int64_t ldo, void* pre, int64_t ldp, void* workspace, size_t workspace_bytes, int64_t M, int64_t N,
+                        int64_t K, int32_t gate, void* stream);
 
 /* The whole block: hidden[M,N] as epd_op_gated_linear(x, w_in, b_in), then out[M,D] = hidden . w_out[D,N]^T + b_out.
  * hidden is caller memory (scratch for inference; the gradient reads it), pre as above.  flags: EPD_LINEAR_ACCUMULATE
@@ -424,8 +429,8 @@ int epd_op_gated_linear(int32_t dtype, const void* x, int64_t ldx, const void* w
  * run on kernels that stream the weights. */
 int epd_op_gated_mlp(int32_t dtype, const void* x, int64_t ldx, const void* w_in, int64_t ldw_in, const void* b_in,
                      const void* w_out, int64_t ldw_out, const void* b_out, void* hidden, int64_t ldh, void* pre,
-                     int64_t ldp, void* out, int64_t ldo, int64_t M, int64_t N, int64_t K, int64_t D, int32_t gate,
-                     int32_t flags, void* stream);
+                     int64_t ldp, void* out, int64_t ldo, void* workspace, size_t workspace_bytes, int64_t M, int64_t N,
+                     int64_t K, int64_t D, int32_t gate, int32_t flags, void* stream);
 
 /* Gradient of epd_op_gated_mlp: from dout[M,D], x, the weights, and hidden and pre as the forward call left them,
  *   dx[M,K], dw_in[2N,K], db_in[2N], dw_out[D,N], db_out[D]   (any may be NULL: not formed),
@@ -433,7 +438,7 @@ int epd_op_gated_mlp(int32_t dtype, const void* x, int64_t ldx, const void* w_in
  * products.  workspace: device memory, 256-byte aligned, epd_gated_mlp_backward_workspace_bytes() bytes, free again
  * once the call's work has run; calls that may overlap on the device need one each.  The same inputs give the same bits on
  * every call (no atomics).  M == 0 zeroes dw_in, db_in, dw_out and db_out. */
-size_t epd_gated_mlp_backward_workspace_bytes(int32_t dtype, int64_t M, int64_t N, int64_t D);
+size_t epd_gated_mlp_backward_workspace_bytes(int32_t dtype, int64_t M, int64_t N, int64_t K, int64_t D);
 int epd_op_gated_mlp_backward(int32_t dtype, const void* dout, int64_t lddo, const void* x, int64_t ldx, const void* w_in,
                               int64_t ldw_in, const void* w_out, int64_t ldw_out, const void* hidden, int64_t ldh,
                               const void* pre, int64_t ldp, void* dx, int64_t lddx, void* dw_in, int64_t lddw_in,
@@ -443,8 +448,8 @@ int epd_op_gated_mlp_backward(int32_t dtype, const void* dout, int64_t lddo, con
 
 /* Gradient of a linear layer out[M,N] = x[M,K] . w[N,K]^T + bias (epd_op_linear without activation):
  *   dx[M,K] = dout . w,  dw[N,K] = dout^T . x,  db[N] = column sums of dout   (any may be NULL),
- * overwritten, element type per dtype.  workspace (needed for db only) as above. */
-size_t epd_linear_backward_workspace_bytes(int32_t dtype, int64_t M, int64_t N);
+ * overwritten, element type per dtype.  workspace as above; in bf16 it is needed for db only. */
+size_t epd_linear_backward_workspace_bytes(int32_t dtype, int64_t M, int64_t N, int64_t K);
 int epd_op_linear_backward(int32_t dtype, const void* dout, int64_t lddo, const void* x, int64_t ldx, const void* w,
                            int64_t ldw, void* dx, int64_t lddx, void* dw, int64_t lddw, void* db, void* workspace,
                            size_t workspace_bytes, int64_t M, int64_t N, int64_t K, void* stream);

@@ -40,7 +40,7 @@ EXPORTED_SYMBOLS = [
     "epd_feature_cache_lookup", "epd_feature_cache_insert", "epd_feature_cache_stats",
     "epd_encode_frames_cached", "epd_debug_set_wait_limit", "epd_encode_frames_fmt", "epd_op_patchify_fmt",
     "epd_op_quantize_e4m3", "epd_op_linear_e4m3",
-    "epd_op_gated_linear", "epd_op_gated_mlp", "epd_op_gated_mlp_backward", "epd_gated_mlp_backward_workspace_bytes",
+    "epd_gated_mlp_workspace_bytes", "epd_op_gated_linear", "epd_op_gated_mlp", "epd_op_gated_mlp_backward", "epd_gated_mlp_backward_workspace_bytes",
     "epd_op_linear_backward", "epd_linear_backward_workspace_bytes", "epd_op_rope_axes", "epd_op_rope_axes_split",
     "epd_op_rope_axes_split_backward",
 ]
@@ -193,17 +193,20 @@ def load_library() -> ctypes.CDLL:
     lib.epd_static_scratch_bytes.restype = ctypes.c_size_t
     lib.epd_static_scratch_bytes.argtypes = []
     lib.epd_op_gated_linear.restype = ctypes.c_int
-    lib.epd_op_gated_linear.argtypes = [i32, vp, i64, vp, i64, vp, vp, i64, vp, i64, i64, i64, i64, i32, vp]
+    lib.epd_gated_mlp_workspace_bytes.restype = ctypes.c_size_t
+    lib.epd_gated_mlp_workspace_bytes.argtypes = [i32, i64, i64, i64, i64]
+    lib.epd_op_gated_linear.argtypes = [i32, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, ctypes.c_size_t, i64, i64, i64, i32,
+                                        vp]
     lib.epd_op_gated_mlp.restype = ctypes.c_int
-    lib.epd_op_gated_mlp.argtypes = [i32, vp, i64, vp, i64, vp, vp, i64, vp, vp, i64, vp, i64, vp, i64, i64, i64, i64, i64,
-                                     i32, i32, vp]
+    lib.epd_op_gated_mlp.argtypes = [i32, vp, i64, vp, i64, vp, vp, i64, vp, vp, i64, vp, i64, vp, i64, vp, ctypes.c_size_t,
+                                     i64, i64, i64, i64, i32, i32, vp]
     lib.epd_gated_mlp_backward_workspace_bytes.restype = ctypes.c_size_t
-    lib.epd_gated_mlp_backward_workspace_bytes.argtypes = [i32, i64, i64, i64]
+    lib.epd_gated_mlp_backward_workspace_bytes.argtypes = [i32, i64, i64, i64, i64]
     lib.epd_op_gated_mlp_backward.restype = ctypes.c_int
     lib.epd_op_gated_mlp_backward.argtypes = [i32, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64,
                                               vp, vp, i64, vp, vp, ctypes.c_size_t, i64, i64, i64, i64, i32, vp]
     lib.epd_linear_backward_workspace_bytes.restype = ctypes.c_size_t
-    lib.epd_linear_backward_workspace_bytes.argtypes = [i32, i64, i64]
+    lib.epd_linear_backward_workspace_bytes.argtypes = [i32, i64, i64, i64]
     lib.epd_op_linear_backward.restype = ctypes.c_int
     lib.epd_op_linear_backward.argtypes = [i32, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, ctypes.c_size_t, i64,
                                            i64, i64, vp]
@@ -683,7 +686,7 @@ def _ld(t, cols) -> int:
     return cols if t is None or t.shape[0] <= 1 else t.stride(0)
 
 
-def op_gated_linear(dtype, x, w, bias, gate, out=None, pre=None, stream=None):
+def op_gated_linear(dtype, x, w, bias, gate, out=None, pre=None, workspace=None, stream=None):
     """act(x . w[:N]^T + bias[:N]) * (x . w[N:]^T + bias[N:]) for w [2N, K]; `pre` [M, 2N] receives both projections."""
     M, K = x.shape
     N = w.shape[0] // 2
@@ -699,13 +702,17 @@ def op_gated_linear(dtype, x, w, bias, gate, out=None, pre=None, stream=None):
         out = torch.empty((M, N), dtype=want, device=dev)
     else:
         _expect("out", out, want, dev, (M, N))
-    _launch(torch, dev, stream, load_library().epd_op_gated_linear, "epd_op_gated_linear", dtype, _ptr(x), _ld(x, K), _ptr(w),
-            _ld(w, K), _ptr(bias), _ptr(out), _ld(out, N), _ptr(pre), _ld(pre, 2 * N), M, N, K, gate)
+    lib = load_library()
+    if dtype == DTYPE_F32:
+        workspace = _workspace(torch, workspace, lib.epd_gated_mlp_workspace_bytes(dtype, M, N, K, 0), dev)
+    _launch(torch, dev, stream, lib.epd_op_gated_linear, "epd_op_gated_linear", dtype, _ptr(x), _ld(x, K), _ptr(w),
+            _ld(w, K), _ptr(bias), _ptr(out), _ld(out, N), _ptr(pre), _ld(pre, 2 * N), _ptr(workspace), _bytes(workspace), M,
+            N, K, gate)
     return out
 
 
 def op_gated_mlp(dtype, x, w_in, b_in, w_out, b_out, gate, out=None, hidden=None, pre=None, save=False, flags=0,
-                 stream=None):
+                 workspace=None, stream=None):
     """The gated feed-forward block (epd_op_gated_mlp).  Returns out, or with save=True (out, hidden, pre), which
     op_gated_mlp_backward takes.  flags: LINEAR_ACCUMULATE adds into a float `out` (which has to be given)."""
     M, K = x.shape
@@ -734,9 +741,12 @@ def op_gated_mlp(dtype, x, w_in, b_in, w_out, b_out, gate, out=None, hidden=None
         _expect("pre", pre, want, dev, (M, 2 * N))
     elif save:
         pre = torch.empty((M, 2 * N), dtype=want, device=dev)
-    _launch(torch, dev, stream, load_library().epd_op_gated_mlp, "epd_op_gated_mlp", dtype, _ptr(x), _ld(x, K), _ptr(w_in),
+    lib = load_library()
+    if dtype == DTYPE_F32:
+        workspace = _workspace(torch, workspace, lib.epd_gated_mlp_workspace_bytes(dtype, M, N, K, D), dev)
+    _launch(torch, dev, stream, lib.epd_op_gated_mlp, "epd_op_gated_mlp", dtype, _ptr(x), _ld(x, K), _ptr(w_in),
             _ld(w_in, K), _ptr(b_in), _ptr(w_out), _ld(w_out, N), _ptr(b_out), _ptr(hidden), _ld(hidden, N), _ptr(pre),
-            _ld(pre, 2 * N), _ptr(out), _ld(out, D), M, N, K, D, gate, flags)
+            _ld(pre, 2 * N), _ptr(out), _ld(out, D), _ptr(workspace), _bytes(workspace), M, N, K, D, gate, flags)
     return (out, hidden, pre) if save else out
 
 
@@ -759,22 +769,27 @@ def op_gated_mlp_backward(dtype, dout, x, w_in, w_out, hidden, pre, gate, bias=T
         g["db_in"] = torch.empty(2 * N, dtype=want, device=x.device)
         g["db_out"] = torch.empty(D, dtype=want, device=x.device)
     lib = load_library()
-    nbytes = lib.epd_gated_mlp_backward_workspace_bytes(dtype, M, N, D)
+    nbytes = lib.epd_gated_mlp_backward_workspace_bytes(dtype, M, N, K, D)
     workspace = _workspace(torch, workspace, nbytes, x.device)
     _launch(torch, x.device, stream, lib.epd_op_gated_mlp_backward, "epd_op_gated_mlp_backward", dtype, _ptr(dout),
             _ld(dout, D), _ptr(x), _ld(x, K), _ptr(w_in), _ld(w_in, K), _ptr(w_out), _ld(w_out, N), _ptr(hidden),
             _ld(hidden, N), _ptr(pre), _ld(pre, 2 * N), _ptr(g.get("dx")), K, _ptr(g.get("dw_in")), K, _ptr(g.get("db_in")),
-            _ptr(g.get("dw_out")), N, _ptr(g.get("db_out")), _ptr(workspace), workspace.numel() * workspace.element_size(), M,
-            N, K, D, gate)
+            _ptr(g.get("dw_out")), N, _ptr(g.get("db_out")), _ptr(workspace), _bytes(workspace), M, N, K, D,
+            gate)
     return g
 
 
 def _workspace(torch, given, nbytes, device):
+    """The caller's workspace, or one from the allocator; None where the call needs none."""
     if given is None:
-        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+        return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
     if given.device != device or not given.is_contiguous():
         raise ValueError(f"workspace: expected contiguous memory on {device}")
     return given
+
+
+def _bytes(t) -> int:
+    return 0 if t is None else t.numel() * t.element_size()
 
 
 def op_linear_backward(dtype, dout, x, w, bias=True, need_dx=True, need_dw=True, workspace=None, stream=None) -> Dict:
@@ -792,10 +807,10 @@ def op_linear_backward(dtype, dout, x, w, bias=True, need_dx=True, need_dw=True,
     if bias:
         g["db"] = torch.empty(N, dtype=want, device=x.device)
     lib = load_library()
-    workspace = _workspace(torch, workspace, lib.epd_linear_backward_workspace_bytes(dtype, M, N), x.device)
+    workspace = _workspace(torch, workspace, lib.epd_linear_backward_workspace_bytes(dtype, M, N, K), x.device)
     _launch(torch, x.device, stream, lib.epd_op_linear_backward, "epd_op_linear_backward", dtype, _ptr(dout), _ld(dout, N),
             _ptr(x), _ld(x, K), _ptr(w), _ld(w, K), _ptr(g.get("dx")), K, _ptr(g.get("dw")), K, _ptr(g.get("db")),
-            _ptr(workspace), workspace.numel() * workspace.element_size(), M, N, K)
+            _ptr(workspace), _bytes(workspace), M, N, K)
     return g
 
 

@@ -103,7 +103,27 @@ cudaError_t gated_tc_forward(const void* x, int64_t ldx, const void* w, int64_t 
 cudaError_t gated_tc_gradient(const void* dout, int64_t lddo, const void* w_out, int64_t ldw, const void* pre, int64_t ldp,
                               void* dpre, int64_t lddp, float* sums, int64_t M, int64_t N, int64_t D, int gate,
                               cudaStream_t s);
-// out[M, N] = A . B with A [M, K] (or, a_mn, [K, M]) and B [K, N], all bf16; out NULL: not formed, but planned for.
+// A float matrix [rows, cols] as three bf16 planes of plane_rows rows (a multiple of 64, zeros behind the last row), one below
+// the other, leading dimension ld (a multiple of 8).
+struct Planes {
+  __nv_bfloat16* p;
+  int64_t plane_rows, cols, ld;
+};
+struct PlaneArg {
+  const float* src;          // NULL: left out
+  int64_t ld, rows;
+  Planes planes;
+};
+cudaError_t split_planes(std::initializer_list<PlaneArg> list, cudaStream_t s);     // up to five
+// The products of float matrices given as planes.  out_planes: the planes of `out` are written too.
+cudaError_t gated_f32_forward(const Planes& x, const Planes& w, const void* bias, float* out, int64_t ldo, float* pre,
+                              int64_t ldp, const Planes* out_planes, int64_t M, int64_t N, int64_t K, int gate,
+                              cudaStream_t s);
+cudaError_t gated_f32_gradient(const Planes& dout, const Planes& w_out, const float* pre, int64_t ldp, const Planes& dpre,
+                               float* sums, int64_t M, int64_t N, int64_t D, int gate, cudaStream_t s);
+cudaError_t linear_f32(const Planes& x, const Planes& w, const void* bias, float* out, int64_t ldo, int64_t M, int64_t N,
+                       int64_t K, bool accumulate, cudaStream_t s);
+// out[M, N] = A . B with A [M, K] (or, a_mn, [K, M]) and B [K, N], all bf16 or all float; out NULL: not formed, but planned for.
 struct ProductArg {
   const void* a;
   int64_t lda;
@@ -113,6 +133,7 @@ struct ProductArg {
   void* out;
   int64_t ldo;
   int64_t M, N, K;
+  const Planes *planes_a, *planes_b;   // float matrices (out too): in place of a and b
 };
 // Up to three products that do not depend on one another.
 cudaError_t matmul_tc_group(const ProductArg* list, int n, cudaStream_t s);

@@ -20,6 +20,9 @@ namespace {
 // =============================================================================================
 constexpr int FK = 16;
 
+// Multiply-adds of one projection from which a float block runs on the tensor cores.
+constexpr double kFloatTensorCoreWork = 256.0 * 1024 * 1024;
+
 enum { EPI_PLAIN = 0, EPI_GATE = 1, EPI_GATE_GRAD = 2 };
 
 struct FmaArgs {
@@ -340,6 +343,21 @@ cudaError_t column_sum_final(int dtype, const FinalSum& a, const FinalSum& b, cu
 // =============================================================================================
 // The products of the block, each on the kernel that takes its shape
 // =============================================================================================
+// ---- float matrices as planes ------------------------------------------------------------------
+int64_t up(int64_t v, int64_t a) { return (v + a - 1) / a * a; }
+size_t planes_bytes(int64_t rows, int64_t cols) { return align256((size_t)3 * up(rows, 64) * up(cols, 8) * 2); }
+// Takes the next planes out of a workspace.
+Planes take_planes(char** ws, int64_t rows, int64_t cols) {
+  Planes p{reinterpret_cast<__nv_bfloat16*>(*ws), up(rows, 64), cols, up(cols, 8)};
+  *ws += planes_bytes(rows, cols);
+  return p;
+}
+// The tensor cores take a float product where it is large enough to pay for writing the planes (about 6 bytes and a launch a
+// matrix) and for the unused part of a 256-row tile.
+bool float_tc_pays(int64_t M, int64_t N, int64_t K) {
+  return M >= 64 && (double)M * (double)N * (double)K >= kFloatTensorCoreWork && tensor_core_path_available();
+}
+
 // Few rows: what the kernels that stream the weights can load in 16-byte pieces.
 bool few_rows(int dtype, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t M, int64_t K) {
   return dtype == EPD_DTYPE_BF16 && M <= kFewRows && K % 8 == 0 && ldx % 8 == 0 && ldw % 8 == 0 &&
@@ -386,12 +404,20 @@ cudaError_t gate_gradient(int dtype, const void* dout, int64_t lddo, const void*
 // dx[M, K] = dout[M, N] . w[N, K]
 ProductArg input_gradient(const void* dout, int64_t lddo, const void* w, int64_t ldw, void* dx, int64_t lddx, int64_t M,
                           int64_t N, int64_t K) {
-  return ProductArg{dout, lddo, false, w, ldw, dx, lddx, M, K, N};
+  return ProductArg{dout, lddo, false, w, ldw, dx, lddx, M, K, N, nullptr, nullptr};
 }
 // dw[N, K] = dout[M, N]^T . x[M, K]
 ProductArg weight_gradient(const void* dout, int64_t lddo, const void* x, int64_t ldx, void* dw, int64_t lddw, int64_t M,
                            int64_t N, int64_t K) {
-  return ProductArg{dout, lddo, true, x, ldx, dw, lddw, N, K, M};
+  return ProductArg{dout, lddo, true, x, ldx, dw, lddw, N, K, M, nullptr, nullptr};
+}
+
+// The same of float matrices in planes.
+ProductArg input_gradient(const Planes& dout, const Planes& w, void* dx, int64_t lddx, int64_t M, int64_t N, int64_t K) {
+  return ProductArg{nullptr, 0, false, nullptr, 0, dx, lddx, M, K, N, &dout, &w};
+}
+ProductArg weight_gradient(const Planes& dout, const Planes& x, void* dw, int64_t lddw, int64_t M, int64_t N, int64_t K) {
+  return ProductArg{nullptr, 0, true, nullptr, 0, dw, lddw, N, K, M, &dout, &x};
 }
 
 // The products of the list (those with an output): together on the tensor cores where they can take them, else on FMAs.
@@ -447,22 +473,41 @@ cudaError_t zero_rows(int dtype, void* p, int64_t ld, int64_t rows, int64_t cols
 
 extern "C" {
 
+size_t epd_gated_mlp_workspace_bytes(int32_t dtype, int64_t M, int64_t N, int64_t K, int64_t D) {
+  using namespace epd;
+  if (dtype != EPD_DTYPE_F32 || M < 0 || M > (1 << 28) || !extent_ok(N) || !extent_ok(K) || D < 0 || D > (1 << 28)) return 0;
+  if (!float_tc_pays(M, N, K)) return 0;
+  size_t bytes = planes_bytes(M, K) + planes_bytes(2 * N, K);
+  if (D > 0) bytes += planes_bytes(M, N) + planes_bytes(D, N);
+  return bytes;
+}
+
 int epd_op_gated_linear(int32_t dtype, const void* x, int64_t ldx, const void* w, int64_t ldw, const void* bias, void* out,
-                        int64_t ldo, void* pre, int64_t ldp, int64_t M, int64_t N, int64_t K, int32_t gate,
-                        void* stream) {
+                        int64_t ldo, void* pre, int64_t ldp, void* workspace, size_t workspace_bytes, int64_t M, int64_t N,
+                        int64_t K, int32_t gate, void* stream) {
   using namespace epd;
   if (!dtype_ok(dtype) || !gate_ok(gate) || M < 0 || M > (1 << 28) || !extent_ok(N) || !extent_ok(K)) return EPD_EINVAL;
   if (ldx < K || ldw < K || ldo < N || (pre && ldp < 2 * N)) return EPD_EINVAL;
   if (M == 0) return EPD_OK;
-  if (!x || !w || !out || !aligned_to(dtype == EPD_DTYPE_F32 ? 4 : 2, x, w, bias, out, pre)) return EPD_EINVAL;
-  return finish(gated_linear(dtype, x, ldx, w, ldw, bias, out, ldo, pre, ldp, M, N, K, gate,
-                             static_cast<cudaStream_t>(stream)));
+  if (!x || !w || !out || !aligned_to(dtype == EPD_DTYPE_F32 ? 4 : 2, x, w, bias, out, pre) || (uintptr_t)workspace % 256)
+    return EPD_EINVAL;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const size_t need = epd_gated_mlp_workspace_bytes(dtype, M, N, K, 0);
+  if (workspace && need > 0) {
+    if (workspace_bytes < need) return EPD_ENOMEM;
+    char* ws = static_cast<char*>(workspace);
+    const Planes px = take_planes(&ws, M, K), pw = take_planes(&ws, 2 * N, K);
+    EPD_TRY(split_planes({{static_cast<const float*>(x), ldx, M, px}, {static_cast<const float*>(w), ldw, 2 * N, pw}}, s));
+    return finish(gated_f32_forward(px, pw, bias, static_cast<float*>(out), ldo, static_cast<float*>(pre), ldp, nullptr, M, N,
+                                    K, gate, s));
+  }
+  return finish(gated_linear(dtype, x, ldx, w, ldw, bias, out, ldo, pre, ldp, M, N, K, gate, s));
 }
 
 int epd_op_gated_mlp(int32_t dtype, const void* x, int64_t ldx, const void* w_in, int64_t ldw_in, const void* b_in,
                      const void* w_out, int64_t ldw_out, const void* b_out, void* hidden, int64_t ldh, void* pre,
-                     int64_t ldp, void* out, int64_t ldo, int64_t M, int64_t N, int64_t K, int64_t D, int32_t gate,
-                     int32_t flags, void* stream) {
+                     int64_t ldp, void* out, int64_t ldo, void* workspace, size_t workspace_bytes, int64_t M, int64_t N,
+                     int64_t K, int64_t D, int32_t gate, int32_t flags, void* stream) {
   using namespace epd;
   if (!dtype_ok(dtype) || !gate_ok(gate) || M < 0 || M > (1 << 28) || !extent_ok(N) || !extent_ok(K) || !extent_ok(D))
     return EPD_EINVAL;
@@ -471,9 +516,22 @@ int epd_op_gated_mlp(int32_t dtype, const void* x, int64_t ldx, const void* w_in
   if (M == 0) return EPD_OK;
   const size_t es = dtype == EPD_DTYPE_F32 ? 4 : 2;
   if (!x || !w_in || !w_out || !hidden || !out || !aligned_to(es, x, w_in, b_in, w_out, b_out, hidden, pre, out) ||
-      ((flags != 0) && !aligned_to(4, out)))
+      ((flags != 0) && !aligned_to(4, out)) || (uintptr_t)workspace % 256)
     return EPD_EINVAL;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const size_t need = epd_gated_mlp_workspace_bytes(dtype, M, N, K, D);
+  if (workspace && need > 0) {
+    if (workspace_bytes < need) return EPD_ENOMEM;
+    char* ws = static_cast<char*>(workspace);
+    const Planes px = take_planes(&ws, M, K), pw = take_planes(&ws, 2 * N, K), ph = take_planes(&ws, M, N),
+                 po = take_planes(&ws, D, N);
+    EPD_TRY(split_planes({{static_cast<const float*>(x), ldx, M, px},
+                          {static_cast<const float*>(w_in), ldw_in, 2 * N, pw},
+                          {static_cast<const float*>(w_out), ldw_out, D, po}}, s));
+    EPD_TRY(gated_f32_forward(px, pw, b_in, static_cast<float*>(hidden), ldh, static_cast<float*>(pre), ldp, &ph, M, N, K, gate,
+                              s));
+    return finish(linear_f32(ph, po, b_out, static_cast<float*>(out), ldo, M, D, N, (flags & EPD_LINEAR_ACCUMULATE) != 0, s));
+  }
   EPD_TRY(gated_linear(dtype, x, ldx, w_in, ldw_in, b_in, hidden, ldh, pre, ldp, M, N, K, gate, s));
   if (few_rows(dtype, hidden, ldh, w_out, ldw_out, M, N))
     return finish(linear_few_rows(hidden, ldh, w_out, ldw_out, b_out, out, ldo, M, D, N, flags,
@@ -494,12 +552,16 @@ int epd_op_gated_mlp(int32_t dtype, const void* x, int64_t ldx, const void* w_in
   return epd_op_linear(dtype, hidden, ldh, w_out, ldw_out, b_out, out, ldo, M, D, N, flags, stream);
 }
 
-size_t epd_gated_mlp_backward_workspace_bytes(int32_t dtype, int64_t M, int64_t N, int64_t D) {
+size_t epd_gated_mlp_backward_workspace_bytes(int32_t dtype, int64_t M, int64_t N, int64_t K, int64_t D) {
   using namespace epd;
-  if (!dtype_ok(dtype) || M < 0 || M > (1 << 28) || !extent_ok(N) || !extent_ok(D)) return 0;
+  if (!dtype_ok(dtype) || M < 0 || M > (1 << 28) || !extent_ok(N) || !extent_ok(K) || !extent_ok(D)) return 0;
   const size_t es = dtype == EPD_DTYPE_F32 ? 4 : 2;
-  // dpre, then the partial sums of its columns (a group per 32 rows at most), then those of dout's
-  return align256((size_t)M * 2 * N * es) + align256((size_t)((M + 31) / 32) * 2 * N * 4) + column_sum_bytes(M, D) + 256;
+  // partial sums of dpre's columns (a group per 32 rows at most) and of dout's, then dpre; float on the tensor cores: planes
+  size_t bytes = align256((size_t)((M + 31) / 32) * 2 * N * 4) + column_sum_bytes(M, D) + 256;
+  if (dtype == EPD_DTYPE_F32 && float_tc_pays(M, N, K))
+    return bytes + planes_bytes(M, 2 * N) + planes_bytes(M, D) + planes_bytes(M, K) + planes_bytes(2 * N, K) +
+           planes_bytes(D, N) + planes_bytes(M, N);
+  return bytes + align256((size_t)M * 2 * N * es);
 }
 
 int epd_op_gated_mlp_backward(int32_t dtype, const void* dout, int64_t lddo, const void* x, int64_t ldx, const void* w_in,
@@ -527,18 +589,39 @@ int epd_op_gated_mlp_backward(int32_t dtype, const void* dout, int64_t lddo, con
   const bool inner = dx || dw_in || db_in;        // anything in front of the product
   if (!dout || (inner && (!pre || !w_out)) || (dx && !w_in) || (dw_in && !x) || (dw_out && !hidden)) return EPD_EINVAL;
   if (!workspace || (uintptr_t)workspace % 256) return EPD_EINVAL;
-  if (workspace_bytes < epd_gated_mlp_backward_workspace_bytes(dtype, M, N, D)) return EPD_ENOMEM;
+  if (workspace_bytes < epd_gated_mlp_backward_workspace_bytes(dtype, M, N, K, D)) return EPD_ENOMEM;
   char* ws = static_cast<char*>(workspace);
-  void* dpre = ws;
-  float* part_in = reinterpret_cast<float*>(ws + align256((size_t)M * 2 * N * es));
-  float* part_out = reinterpret_cast<float*>(reinterpret_cast<char*>(part_in) + align256((size_t)((M + 31) / 32) * 2 * N * 4));
+  float* part_in = reinterpret_cast<float*>(ws);
+  ws += align256((size_t)((M + 31) / 32) * 2 * N * 4);
+  float* part_out = reinterpret_cast<float*>(ws);
+  ws += column_sum_bytes(M, D);
   FinalSum sum_in = {}, sum_out = {};
   if (db_out) {
     EPD_TRY(column_sum_partial(dtype, dout, lddo, M, D, part_out, s));
     sum_out = FinalSum{part_out, sum_groups(M), D, db_out};
   }
+  int64_t groups = 0;
+  if (dtype == EPD_DTYPE_F32 && float_tc_pays(M, N, K)) {
+    const Planes pd = take_planes(&ws, M, 2 * N), py = take_planes(&ws, M, D), px = take_planes(&ws, M, K),
+                 pw = take_planes(&ws, 2 * N, K), po = take_planes(&ws, D, N), ph = take_planes(&ws, M, N);
+    auto given = [](const void* p, bool used) { return used ? static_cast<const float*>(p) : nullptr; };
+    EPD_TRY(split_planes({{given(dout, inner || dw_out), lddo, M, py},
+                          {given(x, dw_in), ldx, M, px},
+                          {given(w_in, dx), ldw_in, 2 * N, pw},
+                          {given(w_out, inner), ldw_out, D, po},
+                          {given(hidden, dw_out), ldh, M, ph}}, s));
+    if (inner) {
+      EPD_TRY(gated_f32_gradient(py, po, static_cast<const float*>(pre), ldp, pd, db_in ? part_in : nullptr, M, N, D, gate, s));
+      if (db_in) sum_in = FinalSum{part_in, (M + 31) / 32, 2 * N, db_in};
+    }
+    EPD_TRY(column_sum_final(dtype, sum_in, sum_out, s));
+    const ProductArg list[3] = {input_gradient(pd, pw, dx, lddx, M, 2 * N, K),
+                                weight_gradient(pd, px, dw_in, lddw_in, M, 2 * N, K),
+                                weight_gradient(py, ph, dw_out, lddw_out, M, D, N)};
+    return finish(matmul_tc_group(list, 3, s));
+  }
+  void* dpre = ws;
   if (inner) {
-    int64_t groups = 0;
     EPD_TRY(gate_gradient(dtype, dout, lddo, w_out, ldw_out, pre, ldp, dpre, 2 * N, db_in ? part_in : nullptr, &groups, M, N,
                           D, gate, s));
     if (db_in) sum_in = FinalSum{part_in, groups, 2 * N, db_in};
@@ -551,10 +634,13 @@ int epd_op_gated_mlp_backward(int32_t dtype, const void* dout, int64_t lddo, con
                          s));
 }
 
-size_t epd_linear_backward_workspace_bytes(int32_t dtype, int64_t M, int64_t N) {
+size_t epd_linear_backward_workspace_bytes(int32_t dtype, int64_t M, int64_t N, int64_t K) {
   using namespace epd;
-  if (!dtype_ok(dtype) || M < 0 || M > (1 << 28) || !extent_ok(N)) return 0;
-  return column_sum_bytes(M, N) + 256;
+  if (!dtype_ok(dtype) || M < 0 || M > (1 << 28) || !extent_ok(N) || !extent_ok(K)) return 0;
+  const size_t bytes = column_sum_bytes(M, N) + 256;
+  if (dtype == EPD_DTYPE_F32 && float_tc_pays(M, N, K))
+    return bytes + planes_bytes(M, N) + planes_bytes(M, K) + planes_bytes(N, K);
+  return bytes;
 }
 
 int epd_op_linear_backward(int32_t dtype, const void* dout, int64_t lddo, const void* x, int64_t ldx, const void* w,
@@ -572,12 +658,24 @@ int epd_op_linear_backward(int32_t dtype, const void* dout, int64_t lddo, const 
     return EPD_OK;
   }
   if (!dout || (dx && !w) || (dw && !x)) return EPD_EINVAL;
-  if (db) {
+  const bool planes = dtype == EPD_DTYPE_F32 && (dx || dw) && float_tc_pays(M, N, K);
+  if (db || planes) {
     if (!workspace || (uintptr_t)workspace % 256) return EPD_EINVAL;
-    if (workspace_bytes < epd_linear_backward_workspace_bytes(dtype, M, N)) return EPD_ENOMEM;
+    if (workspace_bytes < epd_linear_backward_workspace_bytes(dtype, M, N, K)) return EPD_ENOMEM;
+  }
+  if (db) {
     float* part = static_cast<float*>(workspace);
     EPD_TRY(column_sum_partial(dtype, dout, lddo, M, N, part, s));
     EPD_TRY(column_sum_final(dtype, FinalSum{part, sum_groups(M), N, db}, FinalSum{}, s));
+  }
+  if (planes) {
+    char* ws = static_cast<char*>(workspace) + column_sum_bytes(M, N);
+    const Planes py = take_planes(&ws, M, N), px = take_planes(&ws, M, K), pw = take_planes(&ws, N, K);
+    EPD_TRY(split_planes({{static_cast<const float*>(dout), lddo, M, py},
+                          {dw ? static_cast<const float*>(x) : nullptr, ldx, M, px},
+                          {dx ? static_cast<const float*>(w) : nullptr, ldw, N, pw}}, s));
+    const ProductArg list[2] = {input_gradient(py, pw, dx, lddx, M, N, K), weight_gradient(py, px, dw, lddw, M, N, K)};
+    return finish(matmul_tc_group(list, 2, s));
   }
   return finish(products(dtype,
                          {input_gradient(dout, lddo, w, ldw, dx, lddx, M, N, K),

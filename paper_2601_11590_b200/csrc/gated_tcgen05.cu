@@ -9,7 +9,7 @@
 //              column sums over each 32 rows (the bias gradient's first half) leave with them.
 //   GROUP      up to three products with a row-contiguous B: dx = dout . w (A contraction-contiguous) and dw = dout^T . x
 //              (A row-contiguous too), which do not depend on one another and share the machine's last, half-empty round.
-//   LINEAR     x . w^T + bias, both contraction-contiguous, for few rows (SPLIT only).
+//   LINEAR     x . w^T + bias, both contraction-contiguous (bf16: for few rows, SPLIT only).
 // A row-contiguous ("MN-major") operand is staged as boxes of 64 rows x 64 contraction steps: TMA brings 128 contiguous
 // bytes of 64 rows per step, 128-byte swizzled, and the tensor core transposes on the way (descriptor: 8 KB between
 // boxes, 1 KB between groups of 8 steps), so no operand is ever transposed in memory.
@@ -18,6 +18,14 @@
 // tokens of the 6B-class block), 2 or 4 pairs of one cluster share a tile, each taking a part of the contraction.  At the
 // end every pair owns a part of the tile's columns; the others write their sums for it into the owner's shared memory
 // (the operand ring, free by then), and the owner adds them to its own in order: no atomics, no second launch.
+//
+// F32: float matrices.  A float is the sum of three bf16 numbers (8 + 8 + 8 bits of its fraction), so a float product is the
+// sum of the six products of parts that reach its precision: first x third, third x first, second x second, first x second,
+// second x first, first x first; what is left out is below 2^-26 of a product.  split_planes writes the parts of a matrix as
+// three planes, and the contraction of a tile runs six times over the blocks with the planes of the pass, small products
+// first, all into one float accumulator: 6 bf16 products for one float product, where the FMA pipe has 1/22 of the rate.
+// The epilogue reads and writes the float matrices from registers, with any leading dimension, and writes the planes of what
+// the next product takes (hidden, dpre).  An infinity takes part as infinity - infinity: its row or column of results is NaN.
 //
 // Roles per CTA (10 warps): warp 0 TMA producer, warp 1 issues the products (in the pair's first CTA) and owns tensor memory,
 // warps 2..9 epilogue, two per TMEM lane quarter, each taking half of the tile's columns in steps of 32: tcgen05.ld, the
@@ -161,7 +169,16 @@ struct Sub {                   // one product: out[M, N] = A . B over K
   int a_mn;                    // A row-contiguous
   int first;                   // number of its first tile in the launch
   Order order;
+  int passes;                  // 1, or the 6 products of parts (F32)
+  int plane_a, plane_b;        // F32: rows from plane to plane
+  float* out_f32;              // F32
+  int64_t ldo;
 };
+// Parts of a float's products, by pass: the last is first x first (the only one of a bf16 product).
+constexpr int kPasses = 6;
+constexpr int kSumBlocks = 8;  // F32: contraction blocks added up in one accumulator
+__device__ __forceinline__ int plane_a(int pass) { return (0x118 >> (2 * pass)) & 3; }    // 0, 2, 1, 0, 1, 0
+__device__ __forceinline__ int plane_b(int pass) { return (0x052 >> (2 * pass)) & 3; }    // 2, 0, 1, 1, 0, 0
 struct Problem {
   Sub sub[kSubs];              // GROUP: up to three, in the order of the launch's tiles; else the first
   CUtensorMap o1, o2;          // GATE: g, u; GATE_GRAD: out and o1 are dg, du
@@ -171,7 +188,12 @@ struct Problem {
   int split;                   // pairs that share a tile (SPLIT), else 1
   int save_pre;                // GATE: g and u are written
   int out_f32, accumulate;     // LINEAR
-  const __nv_bfloat16* bias;   // GATE: [2N] or NULL; LINEAR: [N] or NULL
+  const void* bias;            // GATE: [2N] or NULL; LINEAR: [N] or NULL
+  // F32: g|u [M, 2N] (GATE: written if save_pre; GATE_GRAD: read), and the planes of GATE's out or of dpre, or NULL
+  float* pre;
+  int64_t ldp;
+  __nv_bfloat16* planes;
+  int64_t planes_ld, planes_rows;   // leading dimension; rows of one plane
   float* sums;                 // GATE_GRAD: column sums of 32 rows each, [ceil(M / 32), 2N], or NULL
   long long wait_limit;
   int* status;
@@ -184,6 +206,73 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
 // One lane's row of a staged box: 16-byte piece j of row r lives at piece j ^ ((r / 2) % 4) (64-byte swizzle).
 __device__ __forceinline__ uint8_t* box_piece(uint8_t* buf, int lane, int j) {
   return buf + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4);
+}
+
+template <bool F32>
+__device__ __forceinline__ float bias_at(const void* bias, int64_t i) {
+  if constexpr (F32) return static_cast<const float*>(bias)[i];
+  else return __bfloat162float(static_cast<const __nv_bfloat16*>(bias)[i]);
+}
+// Up to 32 floats of a row, in 16-byte pieces where the address allows.
+__device__ __forceinline__ void store_row(float* to, const float (&v)[32], int cols) {
+  if (cols == 32 && (reinterpret_cast<uintptr_t>(to) & 15) == 0) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) reinterpret_cast<float4*>(to)[j] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+      if (i < cols) to[i] = v[i];
+  }
+}
+__device__ __forceinline__ void load_row(const float* from, float (&v)[32], int cols) {
+  if (cols == 32 && (reinterpret_cast<uintptr_t>(from) & 15) == 0) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float4 f = reinterpret_cast<const float4*>(from)[j];
+      v[4 * j] = f.x; v[4 * j + 1] = f.y; v[4 * j + 2] = f.z; v[4 * j + 3] = f.w;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = i < cols ? from[i] : 0.0f;
+  }
+}
+// The three bf16 parts of a float: rounded, the rest rounded, the rest of that.  A float just below the largest, where rounding
+// would give infinity, is cut off instead, and so are its further parts: no partial sum of the parts is larger than the
+// float.  Infinity and NaN are their own first part.
+__device__ __forceinline__ void three_parts(float x, __nv_bfloat16 (&part)[3]) {
+  const bool cut = isinf(__bfloat162float(__float2bfloat16_rn(x))) && !isinf(x);
+  float r = x;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    part[i] = cut ? __float2bfloat16_rz(r) : __float2bfloat16_rn(r);
+    r = isfinite(r) ? r - __bfloat162float(part[i]) : 0.0f;
+  }
+}
+// Up to 32 values of a row into the three planes; the rows behind the last one, up to the end of a plane, are zeros.
+__device__ __forceinline__ void store_planes(const Problem& p, int row, bool in, int col, const float (&v)[32], int cols) {
+  if (row >= p.planes_rows) return;
+  __nv_bfloat16* to = p.planes + row * p.planes_ld + col;
+  const int64_t next = p.planes_rows * p.planes_ld;
+  const bool whole = cols == 32 && (reinterpret_cast<uintptr_t>(to) & 15) == 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    __nv_bfloat16 part[8][3];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) three_parts(in ? v[8 * j + e] : 0.0f, part[e]);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      if (whole) {
+        alignas(16) __nv_bfloat16 piece[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) piece[e] = part[e][i];
+        *reinterpret_cast<uint4*>(to + i * next + 8 * j) = *reinterpret_cast<const uint4*>(piece);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (8 * j + e < cols) to[i * next + 8 * j + e] = part[e][i];
+      }
+    }
+  }
 }
 
 // Adds up 32 columns over the warp's 32 rows (one row per lane): lane l returns the sum of column l.  Always the same order.
@@ -200,7 +289,7 @@ __device__ __forceinline__ float column_sum32(float (&v)[32], int lane) {
   return v[0];
 }
 
-template <int MODE, int GATE, bool SPLIT>
+template <int MODE, int GATE, bool SPLIT, bool F32>
 __global__ void __launch_bounds__(kThreads, 1)
 gated_pair_kernel(const __grid_constant__ Problem p) {
   using L = Smem<MODE>;
@@ -208,7 +297,7 @@ gated_pair_kernel(const __grid_constant__ Problem p) {
   constexpr bool B_MN = MODE == MODE_GATE_GRAD || MODE == MODE_GROUP;
   constexpr int TILE_COLS = MODE == MODE_GATE ? BN / 2 : BN;     // output columns of a tile
   constexpr int kSteps = TILE_COLS / 32;                         // 32-column steps of a tile
-  static_assert(MODE != MODE_LINEAR || SPLIT, "whole tiles of a linear layer run on its own kernel");
+  static_assert(MODE != MODE_LINEAR || SPLIT || F32, "whole tiles of a bf16 linear layer run on its own kernel");
 
   pdl_launch_dependents();
   extern __shared__ uint8_t smem_raw[];
@@ -240,7 +329,7 @@ gated_pair_kernel(const __grid_constant__ Problem p) {
     }
     const Sub& u = p.sub[i];
     tile_coords(tile - u.first, (u.M + 2 * BM - 1) / (2 * BM), (u.N + TILE_COLS - 1) / TILE_COLS, u.order, mt, nt);
-    const int blocks = (u.K + BK - 1) / BK;
+    const int blocks = (u.K + BK - 1) / BK * (F32 ? u.passes : 1);
     kb0 = SPLIT ? slice * blocks / split : 0;
     kb1 = SPLIT ? (slice + 1) * blocks / split : blocks;
     return u;
@@ -296,6 +385,120 @@ gated_pair_kernel(const __grid_constant__ Problem p) {
   auto partial_at = [&](int part, int local_step, int col) {     // in floats
     return ((part * (kSteps / split) + local_step) * kPer + col) * BM;
   };
+  // F32: the tensor core adds with truncation, so a long contraction in one accumulator drifts (8608 steps of 16: 1e-5 of the
+  // result).  Every kSumBlocks blocks the accumulator is handed over and added, rounded to nearest, to sums in registers: 128
+  // columns of this warp's row per lane, as kParts groups of the steps it finishes (SPLIT: of all owners').
+  constexpr int kGroups = kPer / 32, kParts = 4 / kGroups;
+  float sum[F32 ? 128 : 1];
+  auto part_step = [&](int k) {                    // the step behind group k
+    if (!SPLIT) return half * (kSteps / 2) + k;
+    const int per = kSteps / (2 * split);
+    return (k / per) * (2 * per) + 2 * (k % per) + half;
+  };
+  auto gather = [&](int kb0, int kb1, uint32_t& acc_phase) -> bool {
+#pragma unroll
+    for (int i = 0; i < 128; ++i) sum[F32 ? i : 0] = 0.0f;
+#pragma unroll 1
+    for (int c0 = kb0; c0 < kb1; c0 += kSumBlocks) {
+      if (!mbar_wait_warp<true>(&tmem_full[acc], acc_phase, wc)) return false;
+      tc_fence_after();
+#pragma unroll
+      for (int k = 0; k < kParts; ++k) {
+#pragma unroll
+        for (int which = 0; which < kGroups; ++which) {
+          uint32_t v[32];
+          tmem_ld32(tmem_base + acc * BN + ((uint32_t)(q * 32) << 16) + which * (BN / 2) + part_step(k) * 32, v);
+          tmem_ld_wait();
+#pragma unroll
+          for (int i = 0; i < 32; ++i) sum[F32 ? (k * kGroups + which) * 32 + i : 0] += __uint_as_float(v[i]);
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(map_to_rank(smem_u32(&tmem_empty[acc]), leader));
+      if (++acc == 2) { acc = 0; acc_phase ^= 1; }
+    }
+    return true;
+  };
+  auto take_sum = [&](int ls, int which, uint32_t (&v)[32]) {
+    const int k = SPLIT ? slice * (kSteps / (2 * split)) + ls : ls;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = 0;
+#pragma unroll
+    for (int n = 0; n < kParts; ++n) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (n == k) v[i] = __float_as_uint(sum[F32 ? (n * kGroups + which) * 32 + i : 0]);
+    }
+  };
+  // F32: one step, this lane's row of 32 columns, between tensor memory and the float matrices.
+  auto finish_f32 = [&](const Sub& u, int st, int ls, int row, int col, auto& add_parts) {
+    const int cols = min(32, u.N - col);
+    const bool in = row < u.M;
+    float v[32];
+    if constexpr (MODE == MODE_GATE) {
+      uint32_t g[32], w[32];
+      take_sum(ls, 0, g);
+      take_sum(ls, 1, w);
+      add_parts(g, st, 0);
+      add_parts(w, st, 1);
+      float a[32], b[32];
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        a[i] = __uint_as_float(g[i]) + bs[ls * 32 + i];
+        b[i] = __uint_as_float(w[i]) + bs[64 + ls * 32 + i];
+        v[i] = gate_act(GATE, a[i]) * b[i];
+      }
+      if (in) {
+        store_row(u.out_f32 + row * u.ldo + col, v, cols);
+        if (p.save_pre) {
+          store_row(p.pre + row * p.ldp + col, a, cols);
+          store_row(p.pre + row * p.ldp + u.N + col, b, cols);
+        }
+      }
+      if (p.planes != nullptr) store_planes(p, row, in, col, v, cols);
+    } else if constexpr (MODE == MODE_GATE_GRAD) {
+      uint32_t da[32];
+      take_sum(ls, 0, da);
+      add_parts(da, st, 0);
+      float g[32], w[32];
+      load_row(p.pre + row * p.ldp + col, g, in ? cols : 0);
+      load_row(p.pre + row * p.ldp + u.N + col, w, in ? cols : 0);
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        float act, slope;
+        gate_act_slope(GATE, g[i], &act, &slope);
+        const float d = __uint_as_float(da[i]);
+        g[i] = in ? d * w[i] * slope : 0.0f;
+        w[i] = in ? d * act : 0.0f;
+      }
+      store_planes(p, row, in, col, g, cols);
+      store_planes(p, row, in, u.N + col, w, cols);
+      if (p.sums != nullptr && row - lane < u.M) {
+        const float sg = column_sum32(g, lane), su = column_sum32(w, lane);
+        if (lane < cols) {
+          float* to = p.sums + (int64_t)(row / 32) * (2 * (int64_t)u.N) + col + lane;
+          to[0] = sg;
+          to[u.N] = su;
+        }
+      }
+    } else {
+      uint32_t w[32];
+      take_sum(ls, 0, w);
+      add_parts(w, st, 0);
+      float* to = u.out_f32 + row * u.ldo + col;
+      float old[32];
+      const bool add = MODE == MODE_LINEAR && p.accumulate;
+      if (add) load_row(to, old, in ? cols : 0);
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        v[i] = __uint_as_float(w[i]);
+        if constexpr (MODE == MODE_LINEAR) v[i] += bs[ls * 32 + i];
+        if (add) v[i] += old[i];
+      }
+      if (in) store_row(to, v, cols);
+    }
+  };
   // The steps of one tile, from tensor memory (and, SPLIT, the other parts' sums) to the output.  False: a wait expired.
   auto finish_tile = [&](const Sub& u, int mt, int nt, int next_tile) -> bool {
     const int row0 = mt * (2 * BM) + (int)rank * BM + q * 32, n0 = nt * TILE_COLS;
@@ -318,8 +521,8 @@ gated_pair_kernel(const __grid_constant__ Problem p) {
       for (int st = step0; st < step_end; st += kStepBy, ++ls) {
         const int col = n0 + st * 32 + lane;
         const bool in = p.bias != nullptr && col < u.N;
-        bs[ls * 32 + lane] = in ? __bfloat162float(p.bias[col]) : 0.0f;
-        if (MODE == MODE_GATE) bs[64 + ls * 32 + lane] = in ? __bfloat162float(p.bias[u.N + (int64_t)col]) : 0.0f;
+        bs[ls * 32 + lane] = in ? bias_at<F32>(p.bias, col) : 0.0f;
+        if (MODE == MODE_GATE) bs[64 + ls * 32 + lane] = in ? bias_at<F32>(p.bias, u.N + (int64_t)col) : 0.0f;
       }
       __syncwarp();
     }
@@ -336,6 +539,10 @@ gated_pair_kernel(const __grid_constant__ Problem p) {
     for (int st = step0; st < step_end; st += kStepBy, ++ls, ++step) {
       const int col = n0 + st * 32;
       const bool inside = row0 < u.M && col < u.N;
+      if constexpr (F32) {
+        finish_f32(u, st, ls, row0 + lane, col, add_parts);
+        continue;
+      }
       if constexpr (MODE == MODE_GATE) {
         uint32_t g[32], w[32];
         tmem_ld32(taddr + st * 32, g);
@@ -526,7 +733,16 @@ gated_pair_kernel(const __grid_constant__ Problem p) {
       // this CTA's half of the B tile; GATE: gate rows in the first CTA, up rows in the second
       const int n0 = MODE == MODE_GATE ? nt * TILE_COLS + (int)rank * u.N : nt * BN + (int)rank * (BN / 2);
       const bool a_mn = MODE == MODE_GROUP && u.a_mn;
-      for (int kb = kb0; kb < kb1; ++kb) {
+      const int k_blocks = (u.K + BK - 1) / BK;
+      int pass = F32 ? kPasses - u.passes + kb0 / k_blocks : kPasses - 1, kb = F32 ? kb0 % k_blocks : kb0;
+      int ya = F32 ? plane_a(pass) * u.plane_a : 0, yb = F32 ? plane_b(pass) * u.plane_b : 0;   // the planes' first rows
+      for (int it = kb0; it < kb1; ++it, ++kb) {
+        if (F32 && kb == k_blocks) {
+          kb = 0;
+          ++pass;
+          ya = plane_a(pass) * u.plane_a;
+          yb = plane_b(pass) * u.plane_b;
+        }
         if (!mbar_wait_warp<true>(&empty[stage], phase ^ 1, wc)) { ok = false; break; }
         uint8_t* sa = smem + stage * kStageBytes;
         uint8_t* sb = sa + kTileBytes;
@@ -534,16 +750,16 @@ gated_pair_kernel(const __grid_constant__ Problem p) {
         if (elect_one()) {
           if (rank == 0) mbar_expect_tx(&full[stage], 2 * kStageBytes);   // both CTAs' bytes
           if (a_mn) {
-            tma_load_pair(sa, &u.a, m0, kb * BK, bar, pol_a);
-            tma_load_pair(sa + kBoxBytes, &u.a, m0 + 64, kb * BK, bar, pol_a);
+            tma_load_pair(sa, &u.a, m0, ya + kb * BK, bar, pol_a);
+            tma_load_pair(sa + kBoxBytes, &u.a, m0 + 64, ya + kb * BK, bar, pol_a);
           } else {
-            tma_load_pair(sa, &u.a, kb * BK, m0, bar, pol_a);
+            tma_load_pair(sa, &u.a, kb * BK, ya + m0, bar, pol_a);
           }
           if constexpr (B_MN) {
-            tma_load_pair(sb, &u.b, n0, kb * BK, bar, pol_b);
-            tma_load_pair(sb + kBoxBytes, &u.b, n0 + 64, kb * BK, bar, pol_b);
+            tma_load_pair(sb, &u.b, n0, yb + kb * BK, bar, pol_b);
+            tma_load_pair(sb + kBoxBytes, &u.b, n0 + 64, yb + kb * BK, bar, pol_b);
           } else {
-            tma_load_pair(sb, &u.b, kb * BK, n0, bar, pol_b);
+            tma_load_pair(sb, &u.b, kb * BK, yb + n0, bar, pol_b);
           }
         }
         __syncwarp();
@@ -567,35 +783,39 @@ gated_pair_kernel(const __grid_constant__ Problem p) {
         // 16 contraction steps: 32 bytes inside a swizzled row, or two groups of 8 steps of 1024 bytes (units of 16 bytes)
         const uint32_t a_step = a_mn ? 2048 / 16 : 2;
         constexpr uint32_t b_step = B_MN ? 2048 / 16 : 2;
-        if (!mbar_wait_warp<true>(&tmem_empty[acc], acc_phase ^ 1, wc)) break;
-        tc_fence_after();
-        const uint32_t d_tmem = tmem_base + acc * BN;
-        for (int kb = kb0; kb < kb1; ++kb) {
-          if (!mbar_wait_warp<true>(&full[stage], phase, wc)) { ok = false; break; }
+        const int chunk = F32 ? kSumBlocks : kb1 - kb0;     // blocks to an accumulator
+        for (int c0 = kb0; c0 < kb1; c0 += chunk) {
+          if (!mbar_wait_warp<true>(&tmem_empty[acc], acc_phase ^ 1, wc)) { ok = false; break; }
           tc_fence_after();
-          const uint32_t sa = smem_u32(smem + stage * kStageBytes);
-          const uint64_t da = a_mn ? smem_desc_mn_sw128(sa) : smem_desc_k_sw128(sa);
-          const uint64_t db = B_MN ? smem_desc_mn_sw128(sa + kTileBytes) : smem_desc_k_sw128(sa + kTileBytes);
-          if (elect_one()) {
+          const uint32_t d_tmem = tmem_base + acc * BN;
+          const int c1 = min(c0 + chunk, kb1);
+          for (int kb = c0; kb < c1; ++kb) {
+            if (!mbar_wait_warp<true>(&full[stage], phase, wc)) { ok = false; break; }
+            tc_fence_after();
+            const uint32_t sa = smem_u32(smem + stage * kStageBytes);
+            const uint64_t da = a_mn ? smem_desc_mn_sw128(sa) : smem_desc_k_sw128(sa);
+            const uint64_t db = B_MN ? smem_desc_mn_sw128(sa + kTileBytes) : smem_desc_k_sw128(sa + kTileBytes);
+            if (elect_one()) {
 #pragma unroll
-            for (int k = 0; k < BK / 16; ++k) umma_pair(d_tmem, da + a_step * k, db + b_step * k, idesc, kb > kb0 || k != 0);
-            umma_commit_both(&empty[stage], leader);
+              for (int k = 0; k < BK / 16; ++k) umma_pair(d_tmem, da + a_step * k, db + b_step * k, idesc, kb > c0 || k != 0);
+              umma_commit_both(&empty[stage], leader);
+            }
+            __syncwarp();
+            if (++stage == STAGES) { stage = 0; phase ^= 1; }
           }
+          if (!ok) break;
+          if (elect_one()) umma_commit_both(&tmem_full[acc], leader);
           __syncwarp();
-          if (++stage == STAGES) { stage = 0; phase ^= 1; }
+          if (++acc == 2) { acc = 0; acc_phase ^= 1; }
         }
-        if (!ok) break;
-        if (elect_one()) umma_commit_both(&tmem_full[acc], leader);
-        __syncwarp();
-        if (++acc == 2) { acc = 0; acc_phase ^= 1; }
       }
     }
     __syncwarp();
   } else {
     // ------------------------------------------------------------------ epilogue (both CTAs)
-    if (lane == 0) prefetch_map(&p.sub[0].out);
+    if (!F32 && lane == 0) prefetch_map(&p.sub[0].out);
     uint32_t acc_phase = 0;
-    if constexpr (MODE == MODE_GATE_GRAD) {
+    if constexpr (MODE == MODE_GATE_GRAD && !F32) {
       if (first_tile < p.tiles && step0 < step_end) {
         int mt, nt, kb0, kb1;
         locate(first_tile, mt, nt, kb0, kb1);
@@ -603,15 +823,26 @@ gated_pair_kernel(const __grid_constant__ Problem p) {
       }
     }
     if constexpr (SPLIT) {
-      tile_ready = mbar_wait_warp<true>(&tmem_full[0], 0, wc);
+      if constexpr (F32) {
+        int mt, nt, kb0, kb1;
+        locate(first_tile, mt, nt, kb0, kb1);
+        tile_ready = gather(kb0, kb1, acc_phase);
+      } else {
+        tile_ready = mbar_wait_warp<true>(&tmem_full[0], 0, wc);
+      }
     } else {
       for (int tile = first_tile; tile < p.tiles; tile += tile_step) {
-        if (!mbar_wait_warp<true>(&tmem_full[acc], acc_phase, wc)) break;
-        tc_fence_after();
         int mt, nt, kb0, kb1;
         const Sub& u = locate(tile, mt, nt, kb0, kb1);
-        if (!finish_tile(u, mt, nt, tile + tile_step)) break;
-        if (++acc == 2) { acc = 0; acc_phase ^= 1; }
+        if constexpr (F32) {
+          if (!gather(kb0, kb1, acc_phase)) break;
+          finish_tile(u, mt, nt, tile + tile_step);
+        } else {
+          if (!mbar_wait_warp<true>(&tmem_full[acc], acc_phase, wc)) break;
+          tc_fence_after();
+          if (!finish_tile(u, mt, nt, tile + tile_step)) break;
+          if (++acc == 2) { acc = 0; acc_phase ^= 1; }
+        }
       }
       finish_stores();
     }
@@ -623,18 +854,26 @@ gated_pair_kernel(const __grid_constant__ Problem p) {
     tc_fence_after();
     const uint32_t ring = smem_u32(smem);
     if (warp >= 2 && tile_ready) {
-      for (int st = 0; st < kSteps; ++st) {
+#pragma unroll
+      for (int k = 0; k < kSteps; ++k) {
+        // F32: group k of the sums in registers, a number known to the compiler; else every step of the tile in turn
+        if (F32 && k >= kParts) break;
+        const int st = F32 ? part_step(k) : k;
         const int owner = st * split / kSteps, ls = st - owner * kSteps / split;
         if (owner == slice || (ls & 1) != half) continue;
         const int part = slice < owner ? slice : slice - 1;
         const uint32_t to = map_to_rank(ring, (uint32_t)owner * 2 + rank) + (q * 32 + lane) * 4;
 #pragma unroll
-        for (int which = 0; which < kPer / 32; ++which) {
+        for (int which = 0; which < kGroups; ++which) {
           uint32_t v[32];
-          tmem_ld32(tmem_base + ((uint32_t)(q * 32) << 16) + which * (BN / 2) + st * 32, v);
-          tmem_ld_wait();
+          if constexpr (!F32) {
+            tmem_ld32(tmem_base + ((uint32_t)(q * 32) << 16) + which * (BN / 2) + st * 32, v);
+            tmem_ld_wait();
+          }
 #pragma unroll
-          for (int i = 0; i < 32; ++i) store_cluster(to + partial_at(part, ls, which * 32 + i) * 4, v[i]);
+          for (int i = 0; i < 32; ++i)
+            store_cluster(to + partial_at(part, ls, which * 32 + i) * 4,
+                          F32 ? __float_as_uint(sum[F32 ? ((k < kParts ? k : 0) * kGroups + which) * 32 + i : 0]) : v[i]);
         }
       }
     }
@@ -705,6 +944,11 @@ bool operand_map(CUtensorMap* tm, const void* base, int64_t rows, int64_t K, int
   return mn ? make_tensor_map_2d(tm, base, K, rows, ld * 2, BK, 64, 2, CU_TENSOR_MAP_SWIZZLE_128B)
             : make_tensor_map_2d(tm, base, rows, K, ld * 2, BM, BK, 2, CU_TENSOR_MAP_SWIZZLE_128B);
 }
+// The same of the three planes of a float matrix [rows, cols] (planes of plane_rows rows): rows from plane to plane, so that the
+// map has them one below the other.
+bool plane_map(CUtensorMap* tm, const Planes& x, bool mn) {
+  return make_tensor_map_2d(tm, x.p, 3 * x.plane_rows, x.cols, x.ld * 2, mn ? BK : BM, 64, 2, CU_TENSOR_MAP_SWIZZLE_128B);
+}
 // 32 x 32 boxes of a bf16 matrix [rows, cols], staged with the 64-byte swizzle.
 bool box_map(CUtensorMap* tm, const void* base, int64_t rows, int64_t cols, int64_t ld) {
   return make_tensor_map_2d(tm, base, rows, cols, ld * 2, 32, 32, 2, CU_TENSOR_MAP_SWIZZLE_64B);
@@ -713,7 +957,7 @@ bool box_map(CUtensorMap* tm, const void* base, int64_t rows, int64_t cols, int6
 int64_t tiles_of(int64_t M, int64_t N, int tile_cols) { return ((M + 2 * BM - 1) / (2 * BM)) * ((N + tile_cols - 1) / tile_cols); }
 
 // Pairs the device runs at once (SMs pair up inside a GPC, so this can be below SMs / 2).
-template <int MODE, int GATE>
+template <int MODE, int GATE, bool F32>
 cudaError_t resident_pairs(int* out) {
   static PerDeviceInt cache;
   int dev = 0;
@@ -733,7 +977,7 @@ cudaError_t resident_pairs(int* out) {
     attr.val.clusterDim.z = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    if (cudaOccupancyMaxActiveClusters(&n, gated_pair_kernel<MODE, GATE, false>, &cfg) != cudaSuccess || n <= 0) {
+    if (cudaOccupancyMaxActiveClusters(&n, gated_pair_kernel<MODE, GATE, false, F32>, &cfg) != cudaSuccess || n <= 0) {
       (void)cudaGetLastError();
       n = sms / 2;
     }
@@ -744,10 +988,10 @@ cudaError_t resident_pairs(int* out) {
   return cudaSuccess;
 }
 
-template <int MODE, int GATE, bool SPLIT>
+template <int MODE, int GATE, bool SPLIT, bool F32>
 cudaError_t launch(Problem& p, cudaStream_t s) {
   using L = Smem<MODE>;
-  auto kern = gated_pair_kernel<MODE, GATE, SPLIT>;
+  auto kern = gated_pair_kernel<MODE, GATE, SPLIT, F32>;
   static PerDeviceOnce configured;
   cudaError_t e = once_per_device(configured, [&] {
     return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kDynamic);
@@ -770,7 +1014,7 @@ cudaError_t launch(Problem& p, cudaStream_t s) {
   cfg.numAttrs = 2;
   if constexpr (!SPLIT) {
     int pairs = 0;
-    e = resident_pairs<MODE, GATE>(&pairs);
+    e = resident_pairs<MODE, GATE, F32>(&pairs);
     if (e != cudaSuccess) return e;
     const int avail = limited_sms(2 * pairs) / 2 > 0 ? limited_sms(2 * pairs) / 2 : 1;
     cfg.gridDim = dim3(2 * (p.tiles < avail ? p.tiles : avail));
@@ -797,9 +1041,9 @@ int choose_split(int64_t tiles, int blocks) {
   return 1;
 }
 
-template <int MODE, int GATE>
+template <int MODE, int GATE, bool F32 = false>
 cudaError_t launch_either(Problem& p, cudaStream_t s) {
-  return p.split > 1 ? launch<MODE, GATE, true>(p, s) : launch<MODE, GATE, false>(p, s);
+  return p.split > 1 ? launch<MODE, GATE, true, F32>(p, s) : launch<MODE, GATE, false, F32>(p, s);
 }
 
 bool matrix_ok(const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; }
@@ -833,7 +1077,7 @@ cudaError_t gated_tc_forward(const void* x, int64_t ldx, const void* w, int64_t 
   p.tiles = (int)tiles;
   p.split = choose_split(tiles, (int)((K + BK - 1) / BK));
   p.save_pre = pre != nullptr;
-  p.bias = static_cast<const __nv_bfloat16*>(bias);
+  p.bias = bias;
   if (gate == EPD_GATE_SILU) return launch_either<MODE_GATE, EPD_GATE_SILU>(p, s);
   if (gate == EPD_GATE_GELU_TANH) return launch_either<MODE_GATE, EPD_GATE_GELU_TANH>(p, s);
   return launch_either<MODE_GATE, EPD_GATE_GELU_ERF>(p, s);
@@ -883,16 +1127,147 @@ cudaError_t linear_tc_split(const void* x, int64_t ldx, const void* w, int64_t l
   p.tiles = (int)tiles_of(M, N, BN);
   p.split = choose_split(p.tiles, (int)((K + BK - 1) / BK));
   if (p.split < 2) return cudaErrorInvalidValue;
-  p.bias = static_cast<const __nv_bfloat16*>(bias);
-  return launch<MODE_LINEAR, 0, true>(p, s);
+  p.bias = bias;
+  return launch<MODE_LINEAR, 0, true, false>(p, s);
 }
+
+// ---- float matrices -----------------------------------------------------------------------
+namespace {
+
+// Planes of up to kSplitLists matrices in one launch: a thread takes 8 columns of a row.  HBM bound: 4 bytes read and 6 written
+// per value.
+constexpr int kSplitLists = 5;
+struct SplitList {
+  PlaneArg m[kSplitLists];
+  int64_t first[kSplitLists + 1];   // pieces in front of a matrix
+  int n;
+};
+__global__ void __launch_bounds__(256) split_planes_kernel(const __grid_constant__ SplitList list) {
+  pdl_launch_dependents();
+  pdl_wait();
+  const int64_t piece = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (piece >= list.first[list.n]) return;
+  int i = 0;
+  while (piece >= list.first[i + 1]) ++i;
+  const PlaneArg& m = list.m[i];
+  const int64_t per_row = m.planes.ld / 8, at = piece - list.first[i], row = at / per_row, col = (at - row * per_row) * 8;
+  const float* src = m.src + row * m.ld + col;
+  float v[8];
+  const bool in = row < m.rows;
+  if (in && col + 8 <= m.planes.cols && (reinterpret_cast<uintptr_t>(src) & 15) == 0) {
+    *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(src);
+    *reinterpret_cast<float4*>(v + 4) = *reinterpret_cast<const float4*>(src + 4);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = in && col + e < m.planes.cols ? src[e] : 0.0f;
+  }
+  alignas(16) __nv_bfloat16 out[3][8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    __nv_bfloat16 part[3];
+    three_parts(v[e], part);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) out[k][e] = part[k];
+  }
+#pragma unroll
+  for (int k = 0; k < 3; ++k)
+    *reinterpret_cast<uint4*>(m.planes.p + (k * m.planes.plane_rows + row) * m.planes.ld + col) = *reinterpret_cast<const uint4*>(out[k]);
+}
+
+}  // namespace
+
+cudaError_t split_planes(std::initializer_list<PlaneArg> list, cudaStream_t s) {
+  SplitList l = {};
+  for (const PlaneArg& m : list) {
+    if (!m.src || l.n == kSplitLists) continue;
+    l.m[l.n] = m;
+    l.first[l.n + 1] = l.first[l.n] + m.planes.plane_rows * (m.planes.ld / 8);
+    ++l.n;
+  }
+  if (l.n == 0) return cudaSuccess;
+  const int64_t blocks = (l.first[l.n] + 255) / 256;
+  if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
+  return launch_pdl(split_planes_kernel, dim3((unsigned)blocks), dim3(256), 0, s, l);
+}
+
+namespace {
+// What the float products have in common: sizes, planes, tiles.
+bool float_sub(Sub* u, const Planes& a, bool a_mn, const Planes& b, bool b_mn, int64_t M, int64_t N, int64_t K, int tile_n) {
+  if (!plane_map(&u->a, a, a_mn) || !plane_map(&u->b, b, b_mn)) return false;
+  u->M = (int)M; u->N = (int)N; u->K = (int)K;
+  u->a_mn = a_mn;
+  u->passes = kPasses;
+  u->plane_a = (int)a.plane_rows;
+  u->plane_b = (int)b.plane_rows;
+  u->order = choose_order(M, N, 3 * K, 2 * BM, tile_n);
+  return true;
+}
+}  // namespace
+
+cudaError_t gated_f32_forward(const Planes& x, const Planes& w, const void* bias, float* out, int64_t ldo, float* pre,
+                              int64_t ldp, const Planes* out_planes, int64_t M, int64_t N, int64_t K, int gate,
+                              cudaStream_t s) {
+  Problem p = {};
+  if (!float_sub(&p.sub[0], x, false, w, false, M, 2 * N, K, BN)) return cudaErrorInvalidValue;
+  p.sub[0].N = (int)N;
+  p.sub[0].out_f32 = out;
+  p.sub[0].ldo = ldo;
+  p.subs = 1;
+  p.tiles = (int)tiles_of(M, N, BN / 2);
+  // the sums of a warp's steps lie in registers: two pairs a tile at most (four would leave two projections of four steps each)
+  p.split = choose_split(p.tiles, kPasses * (int)((K + BK - 1) / BK)) > 1 ? 2 : 1;
+  p.bias = bias;
+  p.pre = pre;
+  p.ldp = ldp;
+  p.save_pre = pre != nullptr;
+  if (out_planes) { p.planes = out_planes->p; p.planes_ld = out_planes->ld; p.planes_rows = out_planes->plane_rows; }
+  if (gate == EPD_GATE_SILU) return launch_either<MODE_GATE, EPD_GATE_SILU, true>(p, s);
+  if (gate == EPD_GATE_GELU_TANH) return launch_either<MODE_GATE, EPD_GATE_GELU_TANH, true>(p, s);
+  return launch_either<MODE_GATE, EPD_GATE_GELU_ERF, true>(p, s);
+}
+
+cudaError_t gated_f32_gradient(const Planes& dout, const Planes& w_out, const float* pre, int64_t ldp, const Planes& dpre,
+                               float* sums, int64_t M, int64_t N, int64_t D, int gate, cudaStream_t s) {
+  Problem p = {};
+  if (!float_sub(&p.sub[0], dout, false, w_out, true, M, N, D, BN)) return cudaErrorInvalidValue;
+  p.subs = 1;
+  p.tiles = (int)tiles_of(M, N, BN);
+  p.split = choose_split(p.tiles, kPasses * (int)((D + BK - 1) / BK));
+  p.pre = const_cast<float*>(pre);
+  p.ldp = ldp;
+  p.planes = dpre.p;
+  p.planes_ld = dpre.ld;
+  p.planes_rows = dpre.plane_rows;
+  p.sums = sums;
+  if (gate == EPD_GATE_SILU) return launch_either<MODE_GATE_GRAD, EPD_GATE_SILU, true>(p, s);
+  if (gate == EPD_GATE_GELU_TANH) return launch_either<MODE_GATE_GRAD, EPD_GATE_GELU_TANH, true>(p, s);
+  return launch_either<MODE_GATE_GRAD, EPD_GATE_GELU_ERF, true>(p, s);
+}
+
+cudaError_t linear_f32(const Planes& x, const Planes& w, const void* bias, float* out, int64_t ldo, int64_t M, int64_t N,
+                       int64_t K, bool accumulate, cudaStream_t s) {
+  Problem p = {};
+  if (!float_sub(&p.sub[0], x, false, w, false, M, N, K, BN)) return cudaErrorInvalidValue;
+  p.sub[0].out_f32 = out;
+  p.sub[0].ldo = ldo;
+  p.subs = 1;
+  p.tiles = (int)tiles_of(M, N, BN);
+  p.split = choose_split(p.tiles, kPasses * (int)((K + BK - 1) / BK));
+  p.bias = bias;
+  p.accumulate = accumulate;
+  return launch_either<MODE_LINEAR, 0, true>(p, s);
+}
+
+namespace {
+
+int blocks_of(const ProductArg& a) { return (int)((a.K + BK - 1) / BK) * (a.planes_a ? kPasses : 1); }
 
 // Time of a launch of whole tiles in contraction blocks, with the products in the given order: the pair that starts with tile 0
 // has the most.  A tile costs its blocks and about 3 more (the first loads, the epilogue's exposed part).
-static int64_t rounds_cost(const ProductArg* const* list, int n, int pairs) {
+int64_t rounds_cost(const ProductArg* const* list, int n, int pairs) {
   int64_t cost = 0, tile = 0;
   for (int i = 0; i < n; ++i) {
-    const int64_t tiles = tiles_of(list[i]->M, list[i]->N, BN), len = (list[i]->K + BK - 1) / BK + 3;
+    const int64_t tiles = tiles_of(list[i]->M, list[i]->N, BN), len = blocks_of(*list[i]) + 3;
     const int64_t from = (pairs - tile % pairs) % pairs;      // its first tile that falls to the first pair
     if (from < tiles) cost += ((tiles - from + pairs - 1) / pairs) * len;
     else if (i + 1 == n && cost == 0) cost = len;
@@ -901,20 +1276,22 @@ static int64_t rounds_cost(const ProductArg* const* list, int n, int pairs) {
   return cost;
 }
 
+}  // namespace
+
 cudaError_t matmul_tc_group(const ProductArg* list, int n, cudaStream_t s) {
   // longest contraction first: what is left over at the end is short
   const ProductArg* sorted[kSubs];
   int m = 0;
   for (int i = 0; i < n && m < kSubs; ++i) sorted[m++] = &list[i];
   for (int i = 1; i < m; ++i)
-    for (int j = i; j > 0 && sorted[j]->K > sorted[j - 1]->K; --j) { const ProductArg* t = sorted[j]; sorted[j] = sorted[j - 1]; sorted[j - 1] = t; }
+    for (int j = i; j > 0 && blocks_of(*sorted[j]) > blocks_of(*sorted[j - 1]); --j) { const ProductArg* t = sorted[j]; sorted[j] = sorted[j - 1]; sorted[j - 1] = t; }
   const int pairs = device_sm_count() / 2;
   // One launch for all, or one launch each, which may share tiles among pairs (about 12 blocks' time for a launch).  Products
   // that are not asked for count as well: a result's bits do not depend on what else is formed.
   int64_t apart = 0;
   for (int i = 0; i < m; ++i) {
     const int64_t tiles = tiles_of(sorted[i]->M, sorted[i]->N, BN);
-    const int blocks = (int)((sorted[i]->K + BK - 1) / BK), split = choose_split(tiles, blocks);
+    const int blocks = blocks_of(*sorted[i]), split = choose_split(tiles, blocks);
     apart += split > 1 ? blocks / split + 6 : rounds_cost(&sorted[i], 1, pairs);
     if (i > 0) apart += 12;
   }
@@ -926,18 +1303,24 @@ cudaError_t matmul_tc_group(const ProductArg* list, int n, cudaStream_t s) {
     int shortest = 1 << 30;
     for (int i = 0; i < count; ++i) {
       const ProductArg& a = *sorted[first + i];
-      const int blocks = (int)((a.K + BK - 1) / BK);
+      const int blocks = blocks_of(a);
       shortest = blocks < shortest ? blocks : shortest;
       all_tiles += tiles_of(a.M, a.N, BN);
       if (!a.out) continue;
       Sub& u = p.sub[p.subs++];
-      if (!operand_map(&u.a, a.a, a.M, a.K, a.lda, a.a_mn) || !operand_map(&u.b, a.b, a.N, a.K, a.ldb, true) ||
-          !box_map(&u.out, a.out, a.M, a.N, a.ldo))
-        return cudaErrorInvalidValue;
-      u.M = (int)a.M; u.N = (int)a.N; u.K = (int)a.K;
-      u.a_mn = a.a_mn;
+      if (a.planes_a) {
+        if (!float_sub(&u, *a.planes_a, a.a_mn, *a.planes_b, true, a.M, a.N, a.K, BN)) return cudaErrorInvalidValue;
+        u.out_f32 = static_cast<float*>(a.out);
+        u.ldo = a.ldo;
+      } else {
+        if (!operand_map(&u.a, a.a, a.M, a.K, a.lda, a.a_mn) || !operand_map(&u.b, a.b, a.N, a.K, a.ldb, true) ||
+            !box_map(&u.out, a.out, a.M, a.N, a.ldo))
+          return cudaErrorInvalidValue;
+        u.M = (int)a.M; u.N = (int)a.N; u.K = (int)a.K;
+        u.a_mn = a.a_mn;
+        u.order = choose_order(a.M, a.N, a.K, 2 * BM, BN);
+      }
       u.first = (int)tiles;
-      u.order = choose_order(a.M, a.N, a.K, 2 * BM, BN);
       tiles += tiles_of(a.M, a.N, BN);
       if (tiles > (1 << 28)) return cudaErrorInvalidValue;
     }
@@ -945,7 +1328,7 @@ cudaError_t matmul_tc_group(const ProductArg* list, int n, cudaStream_t s) {
     if (p.subs == 0) continue;
     p.tiles = (int)tiles;
     p.split = choose_split(all_tiles, shortest);
-    const cudaError_t e = launch_either<MODE_GROUP, 0>(p, s);
+    const cudaError_t e = list[0].planes_a ? launch_either<MODE_GROUP, 0, true>(p, s) : launch_either<MODE_GROUP, 0>(p, s);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;

@@ -164,6 +164,50 @@ def test_block_odd_widths(dtype, M, N, K, D):
         assert bool(((g[name].double() - r).abs() <= bound).all()), name
 
 
+@pytest.mark.parametrize("M,N,K,D", [
+    (2000, 520, 264, 264),     # several tiles, whole contraction per tile
+    (671, 1031, 391, 397),     # odd in every direction
+    (64, 4304, 1024, 512),     # few rows: contraction shared among pairs
+    (193, 1301, 1103, 77),     # just over three blocks of rows, few output columns
+    (4099, 200, 352, 360),     # many rows, narrow
+    (257, 1152, 1152, 1152),
+])
+@pytest.mark.parametrize("gate", GATES)
+def test_large_float_block_on_the_tensor_cores(M, N, K, D, gate):
+    """A float as three bf16 parts, six products of parts: what is left out is 2^-26 of a product, the float sums are those of
+    the plain path, so the same 1e-5 holds."""
+    assert epd.load_library().epd_gated_mlp_workspace_bytes(F32, M, N, K, D) > 0
+    b = block(M, F32, M, N, K, D, bias=gate != epd.GATE_SILU)
+    out, hidden, pre, g = check_block(F32, b, gate)
+    # the plain-FMA path of the same call: no workspace.  Two results within 1e-5 of the definition each.
+    lib = epd.load_library()
+    out2, hid2 = torch.empty_like(out), torch.empty_like(hidden)
+    p = lambda t: None if t is None else t.data_ptr()   # noqa: E731
+    assert lib.epd_op_gated_mlp(F32, p(b["x"]), K, p(b["w_in"]), K, p(b["b_in"]), p(b["w_out"]), N, p(b["b_out"]), p(hid2), N, None,
+                                0, p(out2), D, None, 0, M, N, K, D, gate, 0, torch.cuda.current_stream().cuda_stream) == 0
+    parity(out2, out.double(), 2e-5, "the two paths")
+    n = Draw(M, F32)
+    lin = epd.op_linear_backward(F32, n(1.0, M, N), b["x"], b["w_in"][:N])
+    parity(lin["dw"], f64(Draw(M, F32)(1.0, M, N)).T @ f64(b["x"]), ONE[F32], "dw")
+    parity(lin["dx"], f64(Draw(M, F32)(1.0, M, N)) @ f64(b["w_in"][:N]), ONE[F32], "dx")
+
+
+def test_float_parts_over_the_whole_range():
+    """Values over the whole range of float, the largest ones among them: every operand value is the exact sum of its parts (24
+    bits, above 2^-110), products and sums stay finite.  A diagonal weight leaves one product per result: relative error
+    2^-24 of the final rounding and 2^-25 of the parts left out, element by element."""
+    M = K = 1024
+    x = torch.zeros(M, K, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(1)
+    e = torch.randint(-100, 127, (M, K), generator=g, device="cuda").double()
+    x = ((1 + torch.rand(M, K, generator=g, device="cuda", dtype=torch.float64)) * 2.0 ** e).float()
+    x[0, :8] = torch.tensor([3.4028235e38, -3.4028235e38, 3.39e38, 3.3961775e38, 0.0, -0.0, 1.0, 1e-30], device="cuda")
+    eye = torch.eye(K, device="cuda") * 0.75
+    dw = epd.op_linear_backward(F32, x, torch.eye(M, device="cuda"), eye, bias=False)
+    assert torch.allclose(dw["dx"].double(), x.double() * 0.75, rtol=2.0 ** -22, atol=0)
+    assert torch.allclose(dw["dw"].double(), x.double().T, rtol=2.0 ** -22, atol=0)
+
+
 def test_block_at_the_encoder_widths():
     for M, N, K, gate in ((777, 4304, 1152, epd.GATE_GELU_TANH), (30, 12800, 3200, epd.GATE_GELU_ERF),
                           (1, 12800, 3200, epd.GATE_SILU)):

@@ -21,27 +21,28 @@ def replace(args, **kw):
 
 
 def test_gated_linear_refusals(lib):
-    ok = dict(dtype=1, x=P, ldx=64, w=P, ldw=64, bias=None, out=P, ldo=32, pre=None, ldp=0, M=4, N=32, K=64, gate=0, stream=None)
+    ok = dict(dtype=1, x=P, ldx=64, w=P, ldw=64, bias=None, out=P, ldo=32, pre=None, ldp=0, ws=None, bytes=0,
+              M=4, N=32, K=64, gate=0, stream=None)
     for bad in (dict(dtype=2), dict(x=None), dict(w=None), dict(out=None), dict(ldx=63), dict(ldw=63), dict(ldo=31),
                 dict(pre=P, ldp=63), dict(M=-1), dict(N=0), dict(K=0), dict(gate=3), dict(gate=-1), dict(x=P + 1),
-                dict(M=(1 << 28) + 1), dict(N=1 << 29, ldo=1 << 29)):
+                dict(M=(1 << 28) + 1), dict(N=1 << 29, ldo=1 << 29), dict(ws=P + 16)):
         assert lib.epd_op_gated_linear(*replace(ok, **bad)) == epd.EPD_EINVAL, bad
     assert lib.epd_op_gated_linear(*replace(ok, M=0, x=None, w=None, out=None)) == epd.EPD_OK
 
 
 def test_gated_mlp_refusals(lib):
     ok = dict(dtype=1, x=P, ldx=64, w_in=P, ldw_in=64, b_in=None, w_out=P, ldw_out=32, b_out=None, hidden=P, ldh=32,
-              pre=None, ldp=0, out=P, ldo=48, M=4, N=32, K=64, D=48, gate=0, flags=0, stream=None)
+              pre=None, ldp=0, out=P, ldo=48, ws=None, bytes=0, M=4, N=32, K=64, D=48, gate=0, flags=0, stream=None)
     for bad in (dict(dtype=-1), dict(x=None), dict(w_in=None), dict(w_out=None), dict(hidden=None), dict(out=None),
                 dict(ldx=60), dict(ldw_in=60), dict(ldw_out=31), dict(ldh=31), dict(ldo=47), dict(pre=P, ldp=60), dict(M=-4),
                 dict(N=-1), dict(D=0), dict(gate=9), dict(flags=1), dict(flags=16), dict(hidden=P + 1),
-                dict(flags=8, out=P + 2)):
+                dict(flags=8, out=P + 2), dict(ws=P + 128)):
         assert lib.epd_op_gated_mlp(*replace(ok, **bad)) == epd.EPD_EINVAL, bad
     assert lib.epd_op_gated_mlp(*replace(ok, M=0, hidden=None)) == epd.EPD_OK
 
 
 def test_gated_mlp_backward_refusals(lib):
-    need = lib.epd_gated_mlp_backward_workspace_bytes(1, 4, 32, 48)
+    need = lib.epd_gated_mlp_backward_workspace_bytes(1, 4, 32, 64, 48)
     assert need >= 4 * 64 * 2
     ok = dict(dtype=1, dout=P, lddo=48, x=P, ldx=64, w_in=P, ldw_in=64, w_out=P, ldw_out=32, hidden=P, ldh=32, pre=P, ldp=64,
               dx=P, lddx=64, dw_in=P, lddw_in=64, db_in=P, dw_out=P, lddw_out=32, db_out=P, ws=P, bytes=need, M=4, N=32,
@@ -52,12 +53,13 @@ def test_gated_mlp_backward_refusals(lib):
                 dict(N=0), dict(K=0), dict(D=0), dict(dx=P + 1)):
         assert lib.epd_op_gated_mlp_backward(*replace(ok, **bad)) == epd.EPD_EINVAL, bad
     assert lib.epd_op_gated_mlp_backward(*replace(ok, bytes=need - 1)) == epd.EPD_ENOMEM
-    for bad in ((2, 4, 32, 48), (1, -1, 32, 48), (1, 4, 0, 48), (1, 4, 32, 0), (1, 1 << 29, 32, 48)):
+    for bad in ((2, 4, 32, 64, 48), (1, -1, 32, 64, 48), (1, 4, 0, 64, 48), (1, 4, 32, 0, 48), (1, 4, 32, 64, 0),
+                (1, 1 << 29, 32, 64, 48)):
         assert lib.epd_gated_mlp_backward_workspace_bytes(*bad) == 0
 
 
 def test_linear_backward_refusals(lib):
-    need = lib.epd_linear_backward_workspace_bytes(1, 4, 32)
+    need = lib.epd_linear_backward_workspace_bytes(1, 4, 32, 64)
     ok = dict(dtype=1, dout=P, lddo=32, x=P, ldx=64, w=P, ldw=64, dx=P, lddx=64, dw=P, lddw=64, db=P, ws=P, bytes=need, M=4,
               N=32, K=64, stream=None)
     for bad in (dict(dtype=3), dict(dout=None), dict(x=None), dict(w=None), dict(lddo=31), dict(ldx=1), dict(ldw=1),
