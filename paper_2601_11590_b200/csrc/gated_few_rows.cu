@@ -1,23 +1,26 @@
 // The gated block for one token and a handful of tokens (bf16): bound by reading the weights once.
 //
-// A block owns 8 output columns of the gated product (8 gate rows and the 8 up rows of the same columns: one 16-row
+// A column group is 8 output columns of the gated product (8 gate rows and the 8 up rows of the same columns: one 16-row
 // operand tile, so a thread ends up holding both projections of its columns), or 8 or 16 output columns of the projection
-// behind it.  Its warps share the contraction: warp w takes every kWarps-th chunk of 32 steps, so that the block reads
-// contiguous pieces of its weight rows, and the warps' sums are added in shared memory, always in the same order.
-// Weights go from global memory straight into matrix fragments: the contraction may be taken in any order as long as both
-// operands share it, so a thread loads 16 contiguous bytes of a weight row and of a token's row and uses them as the
-// fragments of two products (mma.sync, tokens as the 8-wide side).  tcgen05 has nothing to add here: its products would
-// have to be staged through shared memory, and the matrix pipe is idle most of the time either way.
+// behind it.  A block walks column groups; its 8 warps share the contraction: warp w takes every eighth piece of 32 steps, so
+// that the block reads contiguous stretches of its weight rows, and the warps' sums are added in shared memory, always in
+// the same order.  The contraction may be taken in any order as long as both operands share it, so a thread takes 16
+// contiguous bytes of a weight row and of a token's row as the fragments of two products (mma.sync, tokens as the 8-wide
+// side).  Those pieces come by asynchronous copies into slots of shared memory that belong to the thread alone, several
+// pieces ahead and across column groups: nothing has to be synchronised for them, and two or three blocks keep 48 to
+// 120 KB of weights on their way to every SM (with the pieces in registers, 24 to 32 KB, 16 tokens of the 6B-class block took 46 + 32 us).
+// tcgen05 has nothing to add here: the matrix pipe is idle most of the time either way.
 // Token rows beyond the last and weight rows beyond the last are read from the last valid row; their results are not stored.
 #include "gated.cuh"
+#include "tcgen05_common.cuh"
 
 namespace epd {
 namespace {
 
 constexpr int kWarps = 8;
-constexpr int kChunk = 32;          // contraction steps of a warp's chunk: 64 bytes of a row
+constexpr int kChunk = 32;          // contraction steps of a warp's piece: 64 bytes of a row
 
-enum { KIND_GATED = 0, KIND_16 = 1, KIND_8 = 2 };
+enum { KIND_GATED = 0, KIND_16 = 1, KIND_8 = 2 };     // a 16-row tile: 8 gate + 8 up rows; 16 rows; 8 rows and nothing
 
 struct FewRows {
   const __nv_bfloat16 *x, *w, *bias;
@@ -40,114 +43,203 @@ __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ uint4 load_stream(const __nv_bfloat16* p) {
+// 16 bytes to a slot of shared memory, zeros where `in` is false (nothing is read then).
+__device__ __forceinline__ void copy16(uint32_t slot, const __nv_bfloat16* p, bool in) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(slot), "l"(p), "r"(in ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ uint4 load_slot(uint32_t slot) {
   uint4 v;
-  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
-               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(slot) : "memory");
   return v;
 }
 
-template <int KIND, int NT>
-__global__ void __launch_bounds__(32 * kWarps, NT >= 2 ? 2 : 3)
+// TILES 16-row tiles of weights and NT groups of 8 tokens to a step.
+template <int KIND, int NT, int TILES>
+struct Ring {
+  static constexpr int kWeights = KIND == KIND_8 ? 1 : 2 * TILES;           // pieces of weights per step and thread
+  static constexpr int kPieces = kWeights + NT;
+  static constexpr int kBlocksPerSm = NT * TILES >= 8 ? 1 : NT * TILES >= 4 ? 2 : 3;
+  static constexpr int kPieceBytes = 32 * kWarps * 16;
+  static constexpr int kRows = 16 * TILES + 1;
+  static constexpr int kPartBytes = 2 * kWarps * NT * 8 * kRows * 4;        // two sets of the warps' sums
+  static constexpr int kDepth = (233472 / kBlocksPerSm - 1024 - kPartBytes) / (kPieces * kPieceBytes);
+  static constexpr int kRingBytes = kDepth * kPieces * kPieceBytes;
+  static constexpr int kBytes = kRingBytes + kPartBytes;
+  static_assert(kDepth >= 3 && kBlocksPerSm * (kBytes + 1024) <= 233472, "the blocks of an SM");
+  static_assert(KIND != KIND_8 || TILES == 1, "half a tile");
+};
+
+template <int KIND, int NT, int TILES>
+__global__ void __launch_bounds__(32 * kWarps, Ring<KIND, NT, TILES>::kBlocksPerSm)
 few_rows_kernel(const FewRows p) {
-  constexpr int COLS = KIND == KIND_16 ? 16 : 8;       // output columns of a block
-  constexpr int kAhead = NT >= 4 ? 2 : 4;              // chunks loaded ahead of their products
-  __shared__ float part[kWarps][NT * 8][17];
+  using R = Ring<KIND, NT, TILES>;
+  constexpr int COLS = KIND == KIND_16 ? 16 * TILES : 8 * TILES;       // output columns of a group
+  extern __shared__ __align__(16) uint8_t smem[];
+  float* part = reinterpret_cast<float*>(smem + R::kRingBytes);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int g = lane >> 2, t = lane & 3;
-  const int n0 = blockIdx.x * COLS;
-  const int64_t r0 = min(n0 + g, p.N - 1);
-  const int64_t r1 = KIND == KIND_GATED ? p.N + r0 : min(n0 + g + 8, p.N - 1);
-  const __nv_bfloat16* w0 = p.w + r0 * p.ldw + 8 * t;
-  const __nv_bfloat16* w1 = p.w + r1 * p.ldw + 8 * t;
+  const int groups = (p.N + COLS - 1) / COLS;
+  const int steps = (p.K + kWarps * kChunk - 1) / (kWarps * kChunk);       // of a column group
+  const int mine = ((int)blockIdx.x < groups ? (groups - 1 - (int)blockIdx.x) / (int)gridDim.x + 1 : 0) * steps;
+  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + threadIdx.x * 16;
+  auto slot = [&](int depth, int piece) { return ring + (depth * R::kPieces + piece) * R::kPieceBytes; };
+  // Tokens beyond the last one: their slots hold zeros and nothing is copied (copies of the last token's row by eight lanes
+  // at once made one token slower than eight: 87 against 51 us).
   const __nv_bfloat16* xr[NT];
+  bool token[NT];
 #pragma unroll
-  for (int j = 0; j < NT; ++j) xr[j] = p.x + (int64_t)min(8 * j + g, p.M - 1) * p.ldx + 8 * t;
-
-  float acc[NT][4] = {};
-  const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-  uint4 a0[kAhead], a1[kAhead];
-  auto load_weights = [&](int k, uint4& u, uint4& v) {
-    const bool in = k + 8 * t < p.K;                   // K is a multiple of 8: a 16-byte piece is whole or beyond the end
-    u = in ? load_stream(w0 + k) : zero;
-    v = in && KIND != KIND_8 ? load_stream(w1 + k) : zero;
-  };
-  constexpr int kStride = kWarps * kChunk;
-  int k = warp * kChunk;
-  // Behind the block's own gated kernel the weights may be fetched before that kernel has finished.
-  if (p.weights_settled) {
+  for (int j = 0; j < NT; ++j) {
+    token[j] = 8 * j + g < p.M;
+    xr[j] = p.x + (token[j] ? (int64_t)(8 * j + g) * p.ldx + 8 * t : 0);
+    if (!token[j]) {
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) load_weights(k + i * kStride, a0[i], a1[i]);
-    pdl_wait();
-  } else {
-    pdl_wait();
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) load_weights(k + i * kStride, a0[i], a1[i]);
+      for (int d = 0; d < R::kDepth; ++d)
+        asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(slot(d, R::kWeights + j)), "r"(0u) : "memory");
+    }
   }
+
+  // The next pieces to ask for.  K is a multiple of 8: a 16-byte piece is whole or beyond the end.
+  struct Cursor { int group, k; };
+  auto advance = [&](Cursor& c) {
+    c.k += kWarps * kChunk;
+    if (c.k >= steps * kWarps * kChunk) { c.k -= steps * kWarps * kChunk; c.group += gridDim.x; }
+  };
+  auto ask_weights = [&](const Cursor& c, int depth) {
+    const bool in = c.k + 8 * t < p.K;
+    const __nv_bfloat16* w = p.w + (in ? c.k + 8 * t : 0);
+#pragma unroll
+    for (int i = 0; i < (KIND == KIND_8 ? 1 : TILES); ++i) {
+      const int n0 = c.group * COLS + i * (KIND == KIND_16 ? 16 : 8);
+      const int64_t r0 = min(n0 + g, p.N - 1);
+      copy16(slot(depth, 2 * i), w + r0 * p.ldw, in);
+      if constexpr (KIND != KIND_8) {
+        const int64_t r1 = KIND == KIND_GATED ? p.N + r0 : min(n0 + g + 8, p.N - 1);
+        copy16(slot(depth, 2 * i + 1), w + r1 * p.ldw, in);
+      }
+    }
+  };
+  auto ask_tokens = [&](const Cursor& c, int depth) {
+    const bool in = c.k + 8 * t < p.K;
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+      if (token[j]) copy16(slot(depth, R::kWeights + j), xr[j] + (in ? c.k : -8 * t), in);
+  };
+  Cursor weights{(int)blockIdx.x, warp * kChunk}, tokens = weights;
+  // Behind the block's own gated kernel the weights may be fetched before that kernel has finished.
+  if (!p.weights_settled) pdl_wait();
+#pragma unroll
+  for (int d = 0; d < R::kDepth; ++d) {
+    if (d < mine) ask_weights(weights, d);
+    advance(weights);
+  }
+  if (p.weights_settled) pdl_wait();
   // From here on whatever ran in front of this kernel has completed: the next one may start and fetch its weights.
   pdl_launch_dependents();
-  for (; k < p.K; k += kAhead * kStride) {
-    uint4 b[kAhead][NT];
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      const bool in = k + i * kStride + 8 * t < p.K;
-#pragma unroll
-      for (int j = 0; j < NT; ++j) b[i][j] = in ? *reinterpret_cast<const uint4*>(xr[j] + k + i * kStride) : zero;
-    }
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      const uint4 u = a0[i], v = a1[i];
-      load_weights(k + (kAhead + i) * kStride, a0[i], a1[i]);
-#pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        mma_16816(acc[j], u.x, v.x, u.y, v.y, b[i][j].x, b[i][j].y);
-        mma_16816(acc[j], u.z, v.z, u.w, v.w, b[i][j].z, b[i][j].w);
-      }
-    }
+  for (int d = 0; d < R::kDepth; ++d) {
+    if (d < mine) ask_tokens(tokens, d);
+    advance(tokens);
+    asm volatile("cp.async.commit_group;" ::: "memory");
   }
-  // fragment: acc[j][0..1] = (weight row g, tokens 8j + 2t, + 1), acc[j][2..3] = (weight row g + 8, same tokens)
+  int done = 0, depth = 0, set = 0;
+  for (int group = blockIdx.x; group < groups; group += gridDim.x, set ^= 1) {
+    float acc[TILES][NT][4] = {};
+    for (int s = 0; s < steps; ++s) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(R::kDepth - 1) : "memory");
+      uint4 b[NT];
 #pragma unroll
-  for (int j = 0; j < NT; ++j)
+      for (int j = 0; j < NT; ++j) b[j] = load_slot(slot(depth, R::kWeights + j));
 #pragma unroll
-    for (int e = 0; e < 4; ++e) part[warp][8 * j + 2 * t + (e & 1)][g + (e >> 1) * 8] = acc[j][e];
-  __syncthreads();
-  constexpr int ROWS = KIND == KIND_8 ? 8 : 16;
-  for (int i = threadIdx.x; i < NT * 8 * COLS; i += 32 * kWarps) {
-    const int m = i / COLS, c = i % COLS, n = n0 + c;
-    if (m >= p.M || n >= p.N) continue;
-    float s = 0.0f, s2 = 0.0f;
+      for (int i = 0; i < TILES; ++i) {
+        const uint4 u = load_slot(slot(depth, 2 * i));
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if constexpr (KIND != KIND_8) v = load_slot(slot(depth, 2 * i + 1));
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-      s += part[w][m][c];
-      if (KIND == KIND_GATED) s2 += part[w][m][(c + 8) % ROWS];
-    }
-    if (p.bias) s += __bfloat162float(p.bias[n]);
-    if constexpr (KIND == KIND_GATED) {
-      if (p.bias) s2 += __bfloat162float(p.bias[p.N + n]);
-      const float a = p.gate == EPD_GATE_SILU        ? gate_act_fast<EPD_GATE_SILU>(s)
-                      : p.gate == EPD_GATE_GELU_TANH ? gate_act_fast<EPD_GATE_GELU_TANH>(s)
-                                                     : gate_act_fast<EPD_GATE_GELU_ERF>(s);
-      p.out[m * p.ldo + n] = __float2bfloat16_rn(a * s2);
-      if (p.pre) {
-        p.pre[m * p.ldp + n] = __float2bfloat16_rn(s);
-        p.pre[m * p.ldp + p.N + n] = __float2bfloat16_rn(s2);
+        for (int j = 0; j < NT; ++j) {
+          mma_16816(acc[i][j], u.x, v.x, u.y, v.y, b[j].x, b[j].y);
+          mma_16816(acc[i][j], u.z, v.z, u.w, v.w, b[j].z, b[j].w);
+        }
       }
-    } else if (p.out_f32) {
-      float* o = p.out_f32 + m * p.ldo + n;
-      *o = p.accumulate ? *o + s : s;
-    } else {
-      p.out[m * p.ldo + n] = __float2bfloat16_rn(s);
+      // the slots have been read (the products above needed them): the piece kDepth steps on takes their place
+      if (++done + R::kDepth <= mine) {
+        ask_weights(weights, depth);
+        ask_tokens(weights, depth);
+        advance(weights);
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      if (++depth == R::kDepth) depth = 0;
+    }
+    // fragment: acc[i][j][0..1] = (weight row g of tile i, tokens 8j + 2t, + 1), acc[i][j][2..3] = (weight row g + 8, same)
+    float* sums = part + set * (kWarps * NT * 8 * R::kRows);
+#pragma unroll
+    for (int i = 0; i < TILES; ++i)
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          sums[(warp * NT * 8 + 8 * j + 2 * t + (e & 1)) * R::kRows + 16 * i + g + (e >> 1) * 8] = acc[i][j][e];
+    __syncthreads();      // the other set is read by no one any more once every thread has come here
+    const int n0 = group * COLS;
+    for (int i = threadIdx.x; i < NT * 8 * COLS; i += 32 * kWarps) {
+      const int m = i / COLS, c = i % COLS, n = n0 + c;
+      if (m >= p.M || n >= p.N) continue;
+      const int row = KIND == KIND_GATED ? c / 8 * 16 + c % 8 : c;
+      float s = 0.0f, s2 = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        s += sums[(w * NT * 8 + m) * R::kRows + row];
+        if (KIND == KIND_GATED) s2 += sums[(w * NT * 8 + m) * R::kRows + row + 8];
+      }
+      if (p.bias) s += __bfloat162float(p.bias[n]);
+      if constexpr (KIND == KIND_GATED) {
+        if (p.bias) s2 += __bfloat162float(p.bias[p.N + n]);
+        const float a = p.gate == EPD_GATE_SILU        ? gate_act_fast<EPD_GATE_SILU>(s)
+                        : p.gate == EPD_GATE_GELU_TANH ? gate_act_fast<EPD_GATE_GELU_TANH>(s)
+                                                       : gate_act_fast<EPD_GATE_GELU_ERF>(s);
+        p.out[m * p.ldo + n] = __float2bfloat16_rn(a * s2);
+        if (p.pre) {
+          p.pre[m * p.ldp + n] = __float2bfloat16_rn(s);
+          p.pre[m * p.ldp + p.N + n] = __float2bfloat16_rn(s2);
+        }
+      } else if (p.out_f32) {
+        float* o = p.out_f32 + m * p.ldo + n;
+        *o = p.accumulate ? *o + s : s;
+      } else {
+        p.out[m * p.ldo + n] = __float2bfloat16_rn(s);
+      }
     }
   }
 }
 
-template <int KIND>
-cudaError_t launch(const FewRows& p, cudaStream_t s) {
-  constexpr int COLS = KIND == KIND_16 ? 16 : 8;
-  const dim3 grid((unsigned)((p.N + COLS - 1) / COLS)), block(32 * kWarps);
-  if (p.M <= 8) return launch_pdl(few_rows_kernel<KIND, 1>, grid, block, 0, s, p);
-  if (p.M <= 16) return launch_pdl(few_rows_kernel<KIND, 2>, grid, block, 0, s, p);
-  return launch_pdl(few_rows_kernel<KIND, 4>, grid, block, 0, s, p);
+template <int KIND, int NT, int TILES>
+cudaError_t launch_tokens(const FewRows& p, cudaStream_t s) {
+  using R = Ring<KIND, NT, TILES>;
+  auto kern = few_rows_kernel<KIND, NT, TILES>;
+  static PerDeviceOnce configured;
+  cudaError_t e = once_per_device(configured, [&] {
+    return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, R::kBytes);
+  });
+  if (e != cudaSuccess) return e;
+  constexpr int COLS = KIND == KIND_16 ? 16 * TILES : 8 * TILES;
+  const int groups = (p.N + COLS - 1) / COLS, most = R::kBlocksPerSm * limited_sms(device_sm_count());
+  return launch_pdl(kern, dim3((unsigned)(groups < most ? groups : most)), dim3(32 * kWarps), R::kBytes, s, p);
+}
+
+// Every token row is read once per column group, so wide groups save that traffic and narrow ones fill the SMs.  Measured on
+// 148 SMs: the gated product of 16 tokens with 16 columns a group against 8: 6.7 / 9.4 us with 269 groups (1152 x 4304), 31.9
+// / 36.9 us with 800 (3200 x 12800); the projection behind it (12800 -> 3200) for 32 tokens with 32 / 16 / 8 columns a group:
+// 25 / 32 / 53 us (100, 200, 400 groups), for one token with 16 / 8: 20 / 17 us.
+cudaError_t launch_gated(const FewRows& p, cudaStream_t s) {
+  if (p.M <= 8) return launch_tokens<KIND_GATED, 1, 1>(p, s);
+  const bool wide = p.N / 16 >= 148;
+  if (p.M <= 16) return wide ? launch_tokens<KIND_GATED, 2, 2>(p, s) : launch_tokens<KIND_GATED, 2, 1>(p, s);
+  return wide ? launch_tokens<KIND_GATED, 4, 2>(p, s) : launch_tokens<KIND_GATED, 4, 1>(p, s);
+}
+cudaError_t launch_linear(const FewRows& p, cudaStream_t s) {
+  if (p.M <= 8) return p.N / 16 >= 296 ? launch_tokens<KIND_16, 1, 1>(p, s) : launch_tokens<KIND_8, 1, 1>(p, s);
+  if (p.N / 32 >= 100) return p.M <= 16 ? launch_tokens<KIND_16, 2, 2>(p, s) : launch_tokens<KIND_16, 4, 2>(p, s);
+  if (p.N / 16 >= 148) return p.M <= 16 ? launch_tokens<KIND_16, 2, 1>(p, s) : launch_tokens<KIND_16, 4, 1>(p, s);
+  return p.M <= 16 ? launch_tokens<KIND_8, 2, 1>(p, s) : launch_tokens<KIND_8, 4, 1>(p, s);
 }
 
 }  // namespace
@@ -162,7 +254,7 @@ cudaError_t gated_few_rows(const void* x, int64_t ldx, const void* w, int64_t ld
   p.out = static_cast<__nv_bfloat16*>(out); p.ldo = ldo;
   p.pre = static_cast<__nv_bfloat16*>(pre); p.ldp = ldp;
   p.gate = gate;
-  return launch<KIND_GATED>(p, s);
+  return launch_gated(p, s);
 }
 
 cudaError_t linear_few_rows(const void* x, int64_t ldx, const void* w, int64_t ldw, const void* bias, void* out, int64_t ldo,
@@ -177,8 +269,7 @@ cudaError_t linear_few_rows(const void* x, int64_t ldx, const void* w, int64_t l
   else p.out = static_cast<__nv_bfloat16*>(out);
   p.accumulate = (flags & EPD_LINEAR_ACCUMULATE) != 0;
   p.weights_settled = behind_gated;
-  // 8 columns a block where 16 would leave SMs without one
-  return (N + 15) / 16 >= 2 * 148 ? launch<KIND_16>(p, s) : launch<KIND_8>(p, s);
+  return launch_linear(p, s);
 }
 
 }  // namespace epd
