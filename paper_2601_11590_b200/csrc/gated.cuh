@@ -60,33 +60,87 @@ __device__ __forceinline__ float normal_cdf_fast(float x, float* gauss) {
   return x < 0.0f ? tail : 1.0f - tail;
 }
 
+// Two float operations in one instruction.
+__device__ __forceinline__ uint64_t bits2(float2 v) { return reinterpret_cast<uint64_t&>(v); }
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t&>(r)) : "l"(bits2(a)), "l"(bits2(b)));
+  return r;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(reinterpret_cast<uint64_t&>(r)) : "l"(bits2(a)), "l"(bits2(b)), "l"(bits2(c)));
+  return r;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t&>(r)) : "l"(bits2(a)), "l"(bits2(b)));
+  return r;
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+__device__ __forceinline__ float2 ex2_2(float2 x) {
+  float2 e;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.x) : "f"(x.x));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.y) : "f"(x.y));
+  return e;
+}
+__device__ __forceinline__ float2 rcp_2(float2 x) {
+  float2 r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.x) : "f"(x.x));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.y) : "f"(x.y));
+  return r;
+}
+__device__ __forceinline__ float2 sigmoid2(float2 x) { return rcp_2(add2(ex2_2(mul2(x, both(-1.4426950408889634f))), both(1.0f))); }
+__device__ __forceinline__ float2 normal_cdf2(float2 x, float2* gauss) {
+  const float2 z = mul2(make_float2(fabsf(x.x), fabsf(x.y)), both(0.70710678118654752f));
+  const float2 t = rcp_2(fma2(z, both(0.3275911f), both(1.0f)));
+  float2 poly = fma2(both(1.061405429f), t, both(-1.453152027f));
+  poly = fma2(poly, t, both(1.421413741f));
+  poly = fma2(poly, t, both(-0.284496736f));
+  poly = fma2(poly, t, both(0.254829592f));
+  const float2 e = ex2_2(mul2(mul2(z, z), both(-1.4426950408889634f)));
+  *gauss = e;
+  const float2 tail = mul2(mul2(mul2(poly, t), e), both(0.5f));
+  return make_float2(x.x < 0.0f ? tail.x : 1.0f - tail.x, x.y < 0.0f ? tail.y : 1.0f - tail.y);
+}
+
+// Two activations at once: what the epilogues use.
+template <int GATE>
+__device__ __forceinline__ float2 gate_act2(float2 g) {
+  if constexpr (GATE == EPD_GATE_SILU) return mul2(g, sigmoid2(g));
+  if constexpr (GATE == EPD_GATE_GELU_TANH)
+    return mul2(g, sigmoid2(mul2(fma2(mul2(mul2(g, g), g), both(0.044715f), g), both(1.5957691216057308f))));
+  float2 e;
+  return mul2(g, normal_cdf2(g, &e));
+}
+// And their slopes.  The correction term is formed from g held to a range outside of which it is zero: see gate_act_slope().
+template <int GATE>
+__device__ __forceinline__ void gate_act_slope2(float2 g, float2* act, float2* slope) {
+  if constexpr (GATE == EPD_GATE_SILU) {
+    const float2 s = sigmoid2(g);
+    *act = mul2(g, s);
+    *slope = fma2(*act, fma2(s, both(-1.0f), both(1.0f)), s);
+  } else if constexpr (GATE == EPD_GATE_GELU_TANH) {
+    const float2 c = make_float2(fminf(fmaxf(g.x, -10.0f), 10.0f), fminf(fmaxf(g.y, -10.0f), 10.0f));
+    const float2 s = sigmoid2(mul2(fma2(mul2(mul2(g, g), g), both(0.044715f), g), both(1.5957691216057308f)));
+    *act = mul2(g, s);
+    const float2 rest = mul2(mul2(c, s), fma2(s, both(-1.0f), both(1.0f)));
+    *slope = fma2(rest, mul2(fma2(mul2(c, c), both(0.134145f), both(1.0f)), both(1.5957691216057308f)), s);
+  } else {
+    const float2 c = make_float2(fminf(fmaxf(g.x, -20.0f), 20.0f), fminf(fmaxf(g.y, -20.0f), 20.0f));
+    float2 e;
+    const float2 phi = normal_cdf2(g, &e);
+    *act = mul2(g, phi);
+    *slope = fma2(mul2(c, both(0.3989422804014327f)), e, phi);
+  }
+}
+
 template <int GATE>
 __device__ __forceinline__ float gate_act_fast(float g) {
   if constexpr (GATE == EPD_GATE_SILU) return g * sigmoid_fast(g);
   if constexpr (GATE == EPD_GATE_GELU_TANH) return g * sigmoid_fast(1.5957691216057308f * (g + 0.044715f * g * g * g));
   float e;
   return g * normal_cdf_fast(g, &e);
-}
-
-// The correction term is formed from g held to a range outside of which it is zero: see gate_act_slope().
-template <int GATE>
-__device__ __forceinline__ void gate_act_slope_fast(float g, float* act, float* slope) {
-  if constexpr (GATE == EPD_GATE_SILU) {
-    const float s = sigmoid_fast(g);
-    *act = g * s;
-    *slope = fmaf(*act, 1.0f - s, s);
-  } else if constexpr (GATE == EPD_GATE_GELU_TANH) {
-    const float c = fminf(fmaxf(g, -10.0f), 10.0f);
-    const float s = sigmoid_fast(1.5957691216057308f * (g + 0.044715f * g * g * g));
-    *act = g * s;
-    *slope = fmaf(c * s * (1.0f - s), 1.5957691216057308f * fmaf(0.134145f * c, c, 1.0f), s);
-  } else {
-    const float c = fminf(fmaxf(g, -20.0f), 20.0f);
-    float e;
-    const float phi = normal_cdf_fast(g, &e);
-    *act = g * phi;
-    *slope = fmaf(c * 0.3989422804014327f, e, phi);
-  }
 }
 
 // ---- tensor-core kernels (gated_tcgen05.cu) ---------------------------------------------------

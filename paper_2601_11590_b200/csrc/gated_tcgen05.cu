@@ -27,8 +27,8 @@
 // The epilogue reads and writes the float matrices from registers, with any leading dimension, and writes the planes of what
 // the next product takes (hidden, dpre).  An infinity takes part as infinity - infinity: its row or column of results is NaN.
 //
-// Roles per CTA (10 warps): warp 0 TMA producer, warp 1 issues the products (in the pair's first CTA) and owns tensor memory,
-// warps 2..9 epilogue, two per TMEM lane quarter, each taking half of the tile's columns in steps of 32: tcgen05.ld, the
+// Roles per CTA: warp 0 TMA producer, warp 1 issues the products (in the pair's first CTA) and owns tensor memory, 8 or 16
+// epilogue warps, two or four per TMEM lane quarter, which share the tile's columns in steps of 32: tcgen05.ld, the
 // arithmetic in float, one rounding to bf16, a 32-row x 64-byte box in 64-byte-swizzled shared memory, TMA store.  Two
 // accumulators in tensor memory: a tile's epilogue runs under the next tile's products.  Ragged extents: TMA fills loads
 // with zeros and clips stores.  Every wait is bounded; on expiry the kernel drains and returns.  No load is a multicast load.
@@ -45,24 +45,28 @@ enum { MODE_GATE = 0, MODE_GATE_GRAD = 1, MODE_GROUP = 2, MODE_LINEAR = 3 };
 constexpr int BM = 128;            // rows of A per CTA (256 per pair)
 constexpr int BN = 256;            // accumulator columns
 constexpr int BK = 64;             // contraction steps per stage: 128 bytes
-constexpr int kEpiWarps = 8;
-constexpr int kThreads = 32 * (2 + kEpiWarps);
+// Epilogue warps: 8, or 16 for the activation's gradient, whose epilogue has most to do: reads, products, writes and column sums
+// of two matrices (2.5 MB through shared memory a tile, the operands of its 18 blocks 1.2 MB; 139 against 148 thousand clocks
+// for dout . w_out of 6272 x 4304 x 1152, 86 thousand without an epilogue).  The forward tile is better off with the shared
+// memory for a fifth stage (138 against 152 thousand).  Float tiles keep a row's sums in registers.
+constexpr int epi_warps(int mode, bool f32) { return !f32 && mode == MODE_GATE_GRAD ? 16 : 8; }
 constexpr int kTileBytes = BM * BK * 2;            // one operand of one CTA: 16 KB
 constexpr int kStageBytes = 2 * kTileBytes;
 constexpr int kBoxBytes = 8192;                    // 64 rows x 64 steps of a row-contiguous operand
 constexpr int kBufBytes = 32 * 64;                 // staged output box: 32 rows x 32 bf16
 
-// 5 stages and 3 staged boxes per epilogue warp; GATE_GRAD, which also fetches g and u through the staged boxes ahead of
-// time, has 4 stages and 3 pairs of boxes.
-template <int MODE> struct Smem {
-  static constexpr int kStages = MODE == MODE_GATE_GRAD ? 4 : 5;
-  static constexpr int kBufs = MODE == MODE_GATE_GRAD ? 6 : 3;
+// Stages of the operand ring, staged boxes per epilogue warp.
+template <int MODE, bool F32> struct Smem {
+  static constexpr int kEpiWarps = epi_warps(MODE, F32);
+  static constexpr int kThreads = 32 * (2 + kEpiWarps);
+  static constexpr int kStages = 5;
+  static constexpr int kBufs = kEpiWarps == 16 ? 2 : 3;
   static constexpr int kBufOffset = kStages * kStageBytes;
   static constexpr int kBarOffset = kBufOffset + kEpiWarps * kBufs * kBufBytes;
-  // full[S], empty[S], tmem_full[2], tmem_empty[2], drain, spare; per epilogue warp 3 fetch barriers; TMEM base, abort flag
-  static constexpr int kFetchOffset = kBarOffset + (2 * kStages + 6) * 8;
-  static constexpr int kBiasOffset = kFetchOffset + kEpiWarps * 3 * 8 + 16;
-  static constexpr int kTotal = kBiasOffset + (MODE == MODE_GATE || MODE == MODE_LINEAR ? kEpiWarps * 128 * 4 : 0);
+  // full[S], empty[S], tmem_full[2], tmem_empty[2], drain, spare, TMEM base, abort flag
+  static constexpr int kBiasOffset = kBarOffset + (2 * kStages + 6) * 8 + 16;
+  static constexpr int kBias = kEpiWarps == 16 ? 64 : 128;       // floats per warp
+  static constexpr int kTotal = kBiasOffset + (MODE == MODE_GATE || MODE == MODE_LINEAR ? kEpiWarps * kBias * 4 : 0);
   static constexpr int kDynamic = kTotal + 1024;
   static_assert(kDynamic <= 232448, "exceeds the shared memory of one CTA");
   static_assert(kDynamic > 116 * 1024, "one CTA per SM is assumed by the TMEM allocation");
@@ -81,6 +85,20 @@ __device__ __forceinline__ uint32_t map_to_rank(uint32_t smem_addr, uint32_t ran
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// 32 lanes x 16 consecutive 32-bit columns of tensor memory.
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr)
+      : "memory");
+}
+// 16 bytes to shared memory, zeros where `in` is false (nothing is read then).
+__device__ __forceinline__ void copy16(uint32_t to, const void* from, bool in) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(in ? 16 : 0) : "memory");
 }
 // Relaxed: says only that this warp's tcgen05.ld of the accumulator have completed.
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
@@ -182,17 +200,16 @@ __device__ __forceinline__ int plane_b(int pass) { return (0x052 >> (2 * pass)) 
 struct Problem {
   Sub sub[kSubs];              // GROUP: up to three, in the order of the launch's tiles; else the first
   CUtensorMap o1, o2;          // GATE: g, u; GATE_GRAD: out and o1 are dg, du
-  CUtensorMap l0, l1;          // GATE_GRAD: g, u
   int subs, tiles;
   int tile0;                   // SPLIT: the launch's first tile
   int split;                   // pairs that share a tile (SPLIT), else 1
   int save_pre;                // GATE: g and u are written
   int out_f32, accumulate;     // LINEAR
   const void* bias;            // GATE: [2N] or NULL; LINEAR: [N] or NULL
-  // F32: g|u [M, 2N] (GATE: written if save_pre; GATE_GRAD: read), and the planes of GATE's out or of dpre, or NULL
-  float* pre;
+  // g|u [M, 2N] (GATE: written if save_pre, F32 from registers; GATE_GRAD: read)
+  void* pre;
   int64_t ldp;
-  __nv_bfloat16* planes;
+  __nv_bfloat16* planes;       // F32: the planes of GATE's out or of dpre, or NULL
   int64_t planes_ld, planes_rows;   // leading dimension; rows of one plane
   float* sums;                 // GATE_GRAD: column sums of 32 rows each, [ceil(M / 32), 2N], or NULL
   long long wait_limit;
@@ -289,10 +306,28 @@ __device__ __forceinline__ float column_sum32(float (&v)[32], int lane) {
   return v[0];
 }
 
+// Column sums of 8 columns (16-byte piece j) of a staged 32 x 32 box of bf16, as a product with a matrix of ones (mma.sync, the
+// box transposed on the way by ldmatrix): lane l < 4 returns those of columns 2l, 2l + 1.  3 instructions for 8 columns, where
+// adding over the lanes by shuffles takes about 30.
+__device__ __forceinline__ float2 box_column_sums(uint8_t* buf, int lane, int j) {
+  uint32_t b[4];
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(b[0]), "=r"(b[1]), "=r"(b[2]), "=r"(b[3]) : "r"(smem_u32(box_piece(buf, lane, j))) : "memory");
+  constexpr uint32_t ones = 0x3F803F80u;
+  float c[4] = {};
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %4, %4, %4}, {%5, %6}, {%0, %1, %2, %3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(ones), "r"(b[2 * k]), "r"(b[2 * k + 1]));
+  return make_float2(c[0], c[1]);
+}
+
 template <int MODE, int GATE, bool SPLIT, bool F32>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(Smem<MODE, F32>::kThreads, 1)
 gated_pair_kernel(const __grid_constant__ Problem p) {
-  using L = Smem<MODE>;
+  using L = Smem<MODE, F32>;
+  constexpr int kEpiWarps = L::kEpiWarps, kCols = kEpiWarps / 4;   // groups of columns: warps that share a lane quarter
   constexpr int STAGES = L::kStages;
   constexpr bool B_MN = MODE == MODE_GATE_GRAD || MODE == MODE_GROUP;
   constexpr int TILE_COLS = MODE == MODE_GATE ? BN / 2 : BN;     // output columns of a tile
@@ -307,8 +342,7 @@ gated_pair_kernel(const __grid_constant__ Problem p) {
   uint64_t* tmem_full = empty + STAGES;                                 // one set per CTA
   uint64_t* tmem_empty = tmem_full + 2;                                 // used in the leader only
   uint64_t* drain_bar = tmem_empty + 2;
-  uint64_t* fetch = reinterpret_cast<uint64_t*>(smem + L::kFetchOffset);
-  uint32_t* tmem_base_slot = reinterpret_cast<uint32_t*>(fetch + kEpiWarps * 3);
+  uint32_t* tmem_base_slot = reinterpret_cast<uint32_t*>(drain_bar + 2);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_base_slot + 1);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -338,7 +372,6 @@ gated_pair_kernel(const __grid_constant__ Problem p) {
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
     for (int a = 0; a < 2; ++a) { mbar_init(&tmem_full[a], 1); mbar_init(&tmem_empty[a], 2 * kEpiWarps); }
-    for (int i = 0; i < kEpiWarps * 3; ++i) mbar_init(&fetch[i], 1);
     mbar_init(drain_bar, 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -357,29 +390,32 @@ gated_pair_kernel(const __grid_constant__ Problem p) {
 
   // Epilogue state that lives on past the role's loop in a split launch
   const int q = warp & 3;                          // TMEM lane quarter this warp may read
-  const int half = (warp - 2) >> 2;                // which half of the columns (warps 2..9)
+  const int grp = (warp - 2) >> 2;                 // which group of the columns
   uint8_t* bufs = smem + L::kBufOffset + (warp - 2) * L::kBufs * kBufBytes;
-  uint64_t* fbar = fetch + (warp - 2) * 3;
-  float* bs = reinterpret_cast<float*>(smem + L::kBiasOffset) + (warp - 2) * 128;   // biases of up to 2 steps: 64, 64 (up)
-  // 32-column steps this warp finishes: half of the tile's, or half of those its pair owns
-  const int step0 = SPLIT ? slice * kSteps / split + half : half * (kSteps / 2);
-  const int step_end = SPLIT ? (slice + 1) * kSteps / split : step0 + kSteps / 2;
-  constexpr int kStepBy = SPLIT ? 2 : 1;
+  float* bs = reinterpret_cast<float*>(smem + L::kBiasOffset) + (warp - 2) * L::kBias;   // of the steps; up: second half
+  // 32-column steps this warp finishes: its share of the tile's, or of those its pair owns
+  const int step0 = SPLIT ? slice * kSteps / split + grp : grp * (kSteps / kCols);
+  const int step_end = SPLIT ? (slice + 1) * kSteps / split : step0 + kSteps / kCols;
+  constexpr int kStepBy = SPLIT ? kCols : 1;
   uint32_t step = 0;                               // steps done by this warp over all its tiles
-  uint32_t fetched = 0;                            // GATE_GRAD: steps whose g and u have been asked for
   int acc = 0;
-  // GATE_GRAD: asks for g and u of the step at (row, column)
+  // GATE_GRAD: asks for g and u of the step at (row, column): 4 lanes to a row of 64 bytes, zeros beyond the matrix.  Not with
+  // TMA: it takes these boxes row by row, and its rows are what bounds the kernel (operands 4608 rows of 128 bytes a tile,
+  // results 2048 of 64; with another 2048 of 64 for g and u 74 us, against 46 us without an epilogue).
   auto fetch_pre = [&](int row, int col) {
-    if (lane == 0) {
-      uint64_t* b = &fbar[fetched % 3];
-      uint8_t* to = bufs + (fetched % 3) * 2 * kBufBytes;
-      mbar_expect_tx(b, 2 * kBufBytes);
-      tma_load_2d(to, &p.l0, col, row, b);
-      tma_load_2d(to + kBufBytes, &p.l1, col, row, b);
+    const __nv_bfloat16* pre = static_cast<const __nv_bfloat16*>(p.pre);
+    uint8_t* to = bufs;
+    const int piece = lane & 3, c = col + 8 * piece;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = 8 * i + (lane >> 2);
+      const bool in = row + r < p.sub[0].M && c < p.sub[0].N;
+      const __nv_bfloat16* from = pre + (in ? (int64_t)(row + r) * p.ldp + c : 0);
+      copy16(smem_u32(box_piece(to, r, piece)), from, in);
+      copy16(smem_u32(box_piece(to + kBufBytes, r, piece)), from + (in ? p.sub[0].N : 0), in);
     }
-    __syncwarp();
-    ++fetched;
   };
+  auto fetch_commit = [&] { asm volatile("cp.async.commit_group;" ::: "memory"); };
   // Where the sums of the other parts lie in an owner's ring: [part before it, parts after it][step][g | u][column][128 rows]
   constexpr int kPer = MODE == MODE_GATE ? 64 : 32;              // columns of accumulators per step
   auto partial_at = [&](int part, int local_step, int col) {     // in floats
@@ -391,9 +427,9 @@ gated_pair_kernel(const __grid_constant__ Problem p) {
   constexpr int kGroups = kPer / 32, kParts = 4 / kGroups;
   float sum[F32 ? 128 : 1];
   auto part_step = [&](int k) {                    // the step behind group k
-    if (!SPLIT) return half * (kSteps / 2) + k;
+    if (!SPLIT) return grp * (kSteps / kCols) + k;
     const int per = kSteps / (2 * split);
-    return (k / per) * (2 * per) + 2 * (k % per) + half;
+    return (k / per) * (2 * per) + 2 * (k % per) + grp;
   };
   auto gather = [&](int kb0, int kb1, uint32_t& acc_phase) -> bool {
 #pragma unroll
@@ -446,14 +482,15 @@ gated_pair_kernel(const __grid_constant__ Problem p) {
 #pragma unroll
       for (int i = 0; i < 32; ++i) {
         a[i] = __uint_as_float(g[i]) + bs[ls * 32 + i];
-        b[i] = __uint_as_float(w[i]) + bs[64 + ls * 32 + i];
+        b[i] = __uint_as_float(w[i]) + bs[L::kBias / 2 + ls * 32 + i];
         v[i] = gate_act(GATE, a[i]) * b[i];
       }
       if (in) {
         store_row(u.out_f32 + row * u.ldo + col, v, cols);
         if (p.save_pre) {
-          store_row(p.pre + row * p.ldp + col, a, cols);
-          store_row(p.pre + row * p.ldp + u.N + col, b, cols);
+          float* pre = static_cast<float*>(p.pre) + row * p.ldp + col;
+          store_row(pre, a, cols);
+          store_row(pre + u.N, b, cols);
         }
       }
       if (p.planes != nullptr) store_planes(p, row, in, col, v, cols);
@@ -462,8 +499,9 @@ gated_pair_kernel(const __grid_constant__ Problem p) {
       take_sum(ls, 0, da);
       add_parts(da, st, 0);
       float g[32], w[32];
-      load_row(p.pre + row * p.ldp + col, g, in ? cols : 0);
-      load_row(p.pre + row * p.ldp + u.N + col, w, in ? cols : 0);
+      const float* pre = static_cast<const float*>(p.pre) + row * p.ldp + col;
+      load_row(pre, g, in ? cols : 0);
+      load_row(pre + u.N, w, in ? cols : 0);
 #pragma unroll
       for (int i = 0; i < 32; ++i) {
         float act, slope;
@@ -499,33 +537,38 @@ gated_pair_kernel(const __grid_constant__ Problem p) {
       if (in) store_row(to, v, cols);
     }
   };
-  // The steps of one tile, from tensor memory (and, SPLIT, the other parts' sums) to the output.  False: a wait expired.
-  auto finish_tile = [&](const Sub& u, int mt, int nt, int next_tile) -> bool {
-    const int row0 = mt * (2 * BM) + (int)rank * BM + q * 32, n0 = nt * TILE_COLS;
-    const uint32_t taddr = tmem_base + acc * BN + ((uint32_t)(q * 32) << 16);
-    const float* ring = reinterpret_cast<const float*>(smem);
-    auto add_parts = [&](uint32_t (&v)[32], int st, int which) {
-      if constexpr (SPLIT) {
-        // the pair's own part, then the others in order: a column has one owner, so its sum always runs the same way
-        const float* r = ring + partial_at(0, st - slice * kSteps / split, which * 32) + q * 32 + lane;
-#pragma unroll 1
-        for (int o = 1; o < split; ++o, r += (kSteps / split) * kPer * BM) {
-#pragma unroll
-          for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + r[i * BM]);
-        }
-      }
-    };
+  // Biases of the steps this warp finishes, in front of the wait for the tile's products.
+  auto load_bias = [&](const Sub& u, int nt) {
     if constexpr (MODE == MODE_GATE || MODE == MODE_LINEAR) {
       __syncwarp();
       int ls = 0;
       for (int st = step0; st < step_end; st += kStepBy, ++ls) {
-        const int col = n0 + st * 32 + lane;
+        const int col = nt * TILE_COLS + st * 32 + lane;
         const bool in = p.bias != nullptr && col < u.N;
         bs[ls * 32 + lane] = in ? bias_at<F32>(p.bias, col) : 0.0f;
-        if (MODE == MODE_GATE) bs[64 + ls * 32 + lane] = in ? bias_at<F32>(p.bias, u.N + (int64_t)col) : 0.0f;
+        if (MODE == MODE_GATE) bs[L::kBias / 2 + ls * 32 + lane] = in ? bias_at<F32>(p.bias, u.N + (int64_t)col) : 0.0f;
       }
       __syncwarp();
     }
+  };
+  // The steps of one tile, from tensor memory (and, SPLIT, the other parts' sums) to the output.
+  auto finish_tile = [&](const Sub& u, int mt, int nt, int next_tile) {
+    const int row0 = mt * (2 * BM) + (int)rank * BM + q * 32, n0 = nt * TILE_COLS;
+    const uint32_t taddr = tmem_base + acc * BN + ((uint32_t)(q * 32) << 16);
+    const float* ring = reinterpret_cast<const float*>(smem);
+    // columns first .. of part `which` of step st
+    auto add_parts = [&](auto& v, int st, int which, int first = 0) {
+      constexpr int n = sizeof(v) / 4;
+      if constexpr (SPLIT) {
+        // the pair's own part, then the others in order: a column has one owner, so its sum always runs the same way
+        const float* r = ring + partial_at(0, st - slice * kSteps / split, which * 32 + first) + q * 32 + lane;
+#pragma unroll 1
+        for (int o = 1; o < split; ++o, r += (kSteps / split) * kPer * BM) {
+#pragma unroll
+          for (int i = 0; i < n; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + r[i * BM]);
+        }
+      }
+    };
     auto release = [&](int st) {
       if (!SPLIT && st + kStepBy >= step_end) {
         // this warp has read all of its accumulator columns
@@ -559,13 +602,14 @@ gated_pair_kernel(const __grid_constant__ Problem p) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int i = 8 * j + 2 * e;
-            const float2 bg = *reinterpret_cast<const float2*>(bs + ls * 32 + i);
-            const float2 bu = *reinterpret_cast<const float2*>(bs + 64 + ls * 32 + i);
-            const float g0 = __uint_as_float(g[i]) + bg.x, g1 = __uint_as_float(g[i + 1]) + bg.y;
-            const float u0 = __uint_as_float(w[i]) + bu.x, u1 = __uint_as_float(w[i + 1]) + bu.y;
-            o4[e] = pack2(gate_act_fast<GATE>(g0) * u0, gate_act_fast<GATE>(g1) * u1);
-            g4[e] = pack2(g0, g1);
-            u4[e] = pack2(u0, u1);
+            const float2 gv = add2(make_float2(__uint_as_float(g[i]), __uint_as_float(g[i + 1])),
+                                   *reinterpret_cast<const float2*>(bs + ls * 32 + i));
+            const float2 uv = add2(make_float2(__uint_as_float(w[i]), __uint_as_float(w[i + 1])),
+                                   *reinterpret_cast<const float2*>(bs + L::kBias / 2 + ls * 32 + i));
+            const float2 o = mul2(gate_act2<GATE>(gv), uv);
+            o4[e] = pack2(o.x, o.y);
+            g4[e] = pack2(gv.x, gv.y);
+            u4[e] = pack2(uv.x, uv.y);
           }
           *reinterpret_cast<uint4*>(box_piece(bufs, lane, j)) = make_uint4(o4[0], o4[1], o4[2], o4[3]);
           if (p.save_pre) {
@@ -586,57 +630,39 @@ gated_pair_kernel(const __grid_constant__ Problem p) {
           bulk_commit();
         }
       } else if constexpr (MODE == MODE_GATE_GRAD) {
-        // the next step's g and u: into the pair of boxes whose store was issued two steps ago
-        int next_row = row0, next_col = col + kStepBy * 32;
-        bool more = true;
-        if (st + kStepBy >= step_end) {
-          more = next_tile < p.tiles;
-          if (more) {
-            int nm, nn, k0, k1;
-            locate(next_tile, nm, nn, k0, k1);
-            next_row = nm * (2 * BM) + (int)rank * BM + q * 32;
-            next_col = nn * TILE_COLS + step0 * 32;
-          }
-        }
-        if (more) {
-          if (lane == 0) bulk_wait_read<1>();
-          __syncwarp();
-          fetch_pre(next_row, next_col);
-        }
-        uint32_t da[32];
-        tmem_ld32(taddr + st * 32, da);
-        tmem_ld_wait();
-        release(st);
-        add_parts(da, st, 0);
-        if (!mbar_wait_warp(&fbar[step % 3], (step / 3) & 1, wc)) return false;
-        uint8_t* gb = bufs + (step % 3) * 2 * kBufBytes;
-        uint8_t* ub = gb + kBufBytes;
-        float dg[32], du[32];
+        uint8_t* gb = bufs;
+        uint8_t* ub = bufs + kBufBytes;
+        asm volatile("cp.async.wait_group 0;" ::: "memory");      // this step's g and u
+        __syncwarp();
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          uint4* gp = reinterpret_cast<uint4*>(box_piece(gb, lane, j));
-          uint4* up = reinterpret_cast<uint4*>(box_piece(ub, lane, j));
-          const uint4 gv = *gp, uv = *up;
-          const uint32_t gw[4] = {gv.x, gv.y, gv.z, gv.w}, uw[4] = {uv.x, uv.y, uv.z, uv.w};
-          uint32_t dg4[4], du4[4];
+        for (int hf = 0; hf < 2; ++hf) {
+          uint32_t da[16];
+          tmem_ld16(taddr + st * 32 + hf * 16, da);
+          tmem_ld_wait();
+          if (hf == 1) release(st);
+          add_parts(da, st, 0, hf * 16);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float2 gf = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&gw[e]));
-            const float2 uf = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&uw[e]));
-            const int i = 8 * j + 2 * e;
-            const float d0 = __uint_as_float(da[i]), d1 = __uint_as_float(da[i + 1]);
-            float a0, s0, a1, s1;
-            gate_act_slope_fast<GATE>(gf.x, &a0, &s0);
-            gate_act_slope_fast<GATE>(gf.y, &a1, &s1);
-            dg[i] = d0 * uf.x * s0;
-            dg[i + 1] = d1 * uf.y * s1;
-            du[i] = d0 * a0;
-            du[i + 1] = d1 * a1;
-            dg4[e] = pack2(dg[i], dg[i + 1]);
-            du4[e] = pack2(du[i], du[i + 1]);
+          for (int j = 0; j < 2; ++j) {
+            uint4* gp = reinterpret_cast<uint4*>(box_piece(gb, lane, 2 * hf + j));
+            uint4* up = reinterpret_cast<uint4*>(box_piece(ub, lane, 2 * hf + j));
+            const uint4 gv = *gp, uv = *up;
+            const uint32_t gw[4] = {gv.x, gv.y, gv.z, gv.w}, uw[4] = {uv.x, uv.y, uv.z, uv.w};
+            uint32_t dg4[4], du4[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float2 gf = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&gw[e]));
+              const float2 uf = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&uw[e]));
+              const int i = 8 * j + 2 * e;
+              const float2 d = make_float2(__uint_as_float(da[i]), __uint_as_float(da[i + 1]));
+              float2 act, slope;
+              gate_act_slope2<GATE>(gf, &act, &slope);
+              const float2 dg = mul2(mul2(d, uf), slope), du = mul2(d, act);
+              dg4[e] = pack2(dg.x, dg.y);
+              du4[e] = pack2(du.x, du.y);
+            }
+            *gp = make_uint4(dg4[0], dg4[1], dg4[2], dg4[3]);
+            *up = make_uint4(du4[0], du4[1], du4[2], du4[3]);
           }
-          *gp = make_uint4(dg4[0], dg4[1], dg4[2], dg4[3]);
-          *up = make_uint4(du4[0], du4[1], du4[2], du4[3]);
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
@@ -649,13 +675,34 @@ gated_pair_kernel(const __grid_constant__ Problem p) {
         }
         if (p.sums != nullptr && row0 < u.M) {
           // rows beyond the last one hold zeros: their dout rows were filled with zeros
-          const float sg = column_sum32(dg, lane), su = column_sum32(du, lane);
-          if (col + lane < u.N) {
-            float* to = p.sums + (int64_t)(row0 / 32) * (2 * (int64_t)u.N) + col + lane;
-            to[0] = sg;
-            to[u.N] = su;
+          float* to = p.sums + (int64_t)(row0 / 32) * (2 * (int64_t)u.N) + col + 2 * (lane & 3);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float2 sg = box_column_sums(gb, lane, j), su = box_column_sums(ub, lane, j);
+            if (lane < 4 && col + 8 * j < u.N) {
+              *reinterpret_cast<float2*>(to + 8 * j) = sg;
+              *reinterpret_cast<float2*>(to + u.N + 8 * j) = su;
+            }
           }
         }
+        // the next step's g and u, into the same boxes: under the wait for its products, and the other warps' work
+        int next_row = row0, next_col = col + kStepBy * 32;
+        bool more = true;
+        if (st + kStepBy >= step_end) {
+          more = next_tile < p.tiles;
+          if (more) {
+            int nm, nn, k0, k1;
+            locate(next_tile, nm, nn, k0, k1);
+            next_row = nm * (2 * BM) + (int)rank * BM + q * 32;
+            next_col = nn * TILE_COLS + step0 * 32;
+          }
+        }
+        if (more) {
+          if (lane == 0) bulk_wait_read<0>();
+          __syncwarp();
+          fetch_pre(next_row, next_col);
+        }
+        fetch_commit();
       } else {
         uint32_t v[32];
         tmem_ld32(taddr + st * 32, v);
@@ -703,14 +750,10 @@ gated_pair_kernel(const __grid_constant__ Problem p) {
         }
       }
     }
-    return true;
   };
   auto finish_stores = [&] {
-    if (lane == 0) {
-      bulk_wait_all();
-      // after an abort: boxes asked for and not waited for are still on their way
-      for (uint32_t f = step; f < fetched; ++f) mbar_wait_drain(&fbar[f % 3], (f / 3) & 1);
-    }
+    if (lane == 0) bulk_wait_all();
+    asm volatile("cp.async.wait_all;" ::: "memory");     // after an abort: pieces asked for and not waited for
     __syncwarp();
   };
   bool tile_ready = false;                         // SPLIT: this warp's accumulator is complete
@@ -820,12 +863,13 @@ gated_pair_kernel(const __grid_constant__ Problem p) {
         int mt, nt, kb0, kb1;
         locate(first_tile, mt, nt, kb0, kb1);
         fetch_pre(mt * (2 * BM) + (int)rank * BM + q * 32, nt * TILE_COLS + step0 * 32);
+        fetch_commit();
       }
     }
     if constexpr (SPLIT) {
+      int mt, nt, kb0, kb1;
+      load_bias(locate(first_tile, mt, nt, kb0, kb1), nt);
       if constexpr (F32) {
-        int mt, nt, kb0, kb1;
-        locate(first_tile, mt, nt, kb0, kb1);
         tile_ready = gather(kb0, kb1, acc_phase);
       } else {
         tile_ready = mbar_wait_warp<true>(&tmem_full[0], 0, wc);
@@ -834,13 +878,14 @@ gated_pair_kernel(const __grid_constant__ Problem p) {
       for (int tile = first_tile; tile < p.tiles; tile += tile_step) {
         int mt, nt, kb0, kb1;
         const Sub& u = locate(tile, mt, nt, kb0, kb1);
+        load_bias(u, nt);
         if constexpr (F32) {
           if (!gather(kb0, kb1, acc_phase)) break;
           finish_tile(u, mt, nt, tile + tile_step);
         } else {
           if (!mbar_wait_warp<true>(&tmem_full[acc], acc_phase, wc)) break;
           tc_fence_after();
-          if (!finish_tile(u, mt, nt, tile + tile_step)) break;
+          finish_tile(u, mt, nt, tile + tile_step);
           if (++acc == 2) { acc = 0; acc_phase ^= 1; }
         }
       }
@@ -860,7 +905,7 @@ gated_pair_kernel(const __grid_constant__ Problem p) {
         if (F32 && k >= kParts) break;
         const int st = F32 ? part_step(k) : k;
         const int owner = st * split / kSteps, ls = st - owner * kSteps / split;
-        if (owner == slice || (ls & 1) != half) continue;
+        if (owner == slice || ls % kCols != grp) continue;
         const int part = slice < owner ? slice : slice - 1;
         const uint32_t to = map_to_rank(ring, (uint32_t)owner * 2 + rank) + (q * 32 + lane) * 4;
 #pragma unroll
@@ -968,8 +1013,8 @@ cudaError_t resident_pairs(int* out) {
     const int sms = device_sm_count();
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(sms / 2 * 2);
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = Smem<MODE>::kDynamic;
+    cfg.blockDim = dim3(Smem<MODE, F32>::kThreads);
+    cfg.dynamicSmemBytes = Smem<MODE, F32>::kDynamic;
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeClusterDimension;
     attr.val.clusterDim.x = 2;
@@ -990,7 +1035,7 @@ cudaError_t resident_pairs(int* out) {
 
 template <int MODE, int GATE, bool SPLIT, bool F32>
 cudaError_t launch(Problem& p, cudaStream_t s) {
-  using L = Smem<MODE>;
+  using L = Smem<MODE, F32>;
   auto kern = gated_pair_kernel<MODE, GATE, SPLIT, F32>;
   static PerDeviceOnce configured;
   cudaError_t e = once_per_device(configured, [&] {
@@ -1000,7 +1045,7 @@ cudaError_t launch(Problem& p, cudaStream_t s) {
   const int cluster = 2 * p.split;
   p.wait_limit = wait_limit_cycles();
   cudaLaunchConfig_t cfg = {};
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(L::kThreads);
   cfg.dynamicSmemBytes = L::kDynamic;
   cfg.stream = s;
   cudaLaunchAttribute attr[2];
@@ -1020,9 +1065,9 @@ cudaError_t launch(Problem& p, cudaStream_t s) {
     cfg.gridDim = dim3(2 * (p.tiles < avail ? p.tiles : avail));
     return cudaLaunchKernelEx(&cfg, kern, p);
   }
-  // one cluster per tile; under an SM budget as many launches as keep to it
+  // one cluster per tile from tile0 on; under an SM budget as many launches as keep to it
   const int most = sm_limit() > 0 ? (sm_limit() / cluster > 0 ? sm_limit() / cluster : 1) : p.tiles;
-  for (p.tile0 = 0; p.tile0 < p.tiles; p.tile0 += most) {
+  for (; p.tile0 < p.tiles; p.tile0 += most) {
     const int now = p.tiles - p.tile0 < most ? p.tiles - p.tile0 : most;
     cfg.gridDim = dim3(now * cluster);
     e = cudaLaunchKernelEx(&cfg, kern, p);
@@ -1041,6 +1086,9 @@ int choose_split(int64_t tiles, int blocks) {
   return 1;
 }
 
+// The launch's tiles, shared among pairs where they are few, else whole.  (The 10 tiles of a last round of 380, shared among 40
+// pairs in a launch of their own, took 327 + 42 thousand clocks against 379 and the same time: under the power cap the clock
+// is higher while pairs idle.)
 template <int MODE, int GATE, bool F32 = false>
 cudaError_t launch_either(Problem& p, cudaStream_t s) {
   return p.split > 1 ? launch<MODE, GATE, true, F32>(p, s) : launch<MODE, GATE, false, F32>(p, s);
@@ -1088,11 +1136,9 @@ cudaError_t gated_tc_gradient(const void* dout, int64_t lddo, const void* w_out,
                               cudaStream_t s) {
   Problem p = {};
   Sub& u = p.sub[0];
-  const __nv_bfloat16* g = static_cast<const __nv_bfloat16*>(pre);
   __nv_bfloat16* dg = static_cast<__nv_bfloat16*>(dpre);
   if (!operand_map(&u.a, dout, M, D, lddo, false) || !operand_map(&u.b, w_out, N, D, ldw, true) ||
-      !box_map(&p.l0, g, M, N, ldp) || !box_map(&p.l1, g + N, M, N, ldp) || !box_map(&u.out, dg, M, N, lddp) ||
-      !box_map(&p.o1, dg + N, M, N, lddp))
+      !box_map(&u.out, dg, M, N, lddp) || !box_map(&p.o1, dg + N, M, N, lddp))
     return cudaErrorInvalidValue;
   u.M = (int)M; u.N = (int)N; u.K = (int)D;
   u.order = choose_order(M, N, D, 2 * BM, BN);
@@ -1101,6 +1147,8 @@ cudaError_t gated_tc_gradient(const void* dout, int64_t lddo, const void* w_out,
   if (tiles > (1 << 28)) return cudaErrorInvalidValue;
   p.tiles = (int)tiles;
   p.split = choose_split(tiles, (int)((D + BK - 1) / BK));
+  p.pre = const_cast<void*>(pre);
+  p.ldp = ldp;
   p.sums = sums;
   if (gate == EPD_GATE_SILU) return launch_either<MODE_GATE_GRAD, EPD_GATE_SILU>(p, s);
   if (gate == EPD_GATE_GELU_TANH) return launch_either<MODE_GATE_GRAD, EPD_GATE_GELU_TANH>(p, s);

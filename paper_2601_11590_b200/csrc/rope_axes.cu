@@ -14,6 +14,7 @@
 // so keeps its fraction of a turn to 2^-26.
 #include <math.h>
 
+#include "gated.cuh"
 #include "tcgen05_common.cuh"
 
 namespace epd {
@@ -155,19 +156,6 @@ rope_axes_kernel(const __grid_constant__ AxesPlan plan, const __grid_constant__ 
   }
 }
 
-// Two float operations in one instruction.
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
-  float2 r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t&>(r))
-      : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)));
-  return r;
-}
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-  float2 r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(reinterpret_cast<uint64_t&>(r))
-      : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)), "l"(reinterpret_cast<uint64_t&>(c)));
-  return r;
-}
 __device__ __forceinline__ float2 unpack2(const float* p) { return make_float2(p[0], p[1]); }
 __device__ __forceinline__ float2 unpack2(const __nv_bfloat16* p) {
   return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(p));
