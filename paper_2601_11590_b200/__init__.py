@@ -647,7 +647,8 @@ def _op_type(dtype):
 
 def _expect(name, t, want, device, shape):
     """A tensor of a call: on the call's device, of its element type and shape, rows contiguous."""
-    if t.dtype is want and t.device == device and t.shape == shape and (t.stride(-1) == 1 or shape[-1] <= 1):
+    if t.dtype is want and t.get_device() == device.index and t.shape == shape and \
+            (t.is_contiguous() or t.stride(-1) == 1 or shape[-1] <= 1):
         return
     if not t.is_cuda:
         raise ValueError(f"{name}: not a CUDA tensor (there is no CPU path)")
@@ -699,7 +700,7 @@ def op_gated_linear(dtype, x, w, bias, gate, out=None, pre=None, workspace=None,
     if pre is not None:
         _expect("pre", pre, want, dev, (M, 2 * N))
     if out is None:
-        out = torch.empty((M, N), dtype=want, device=dev)
+        out = x.new_empty((M, N))
     else:
         _expect("out", out, want, dev, (M, N))
     lib = load_library()
@@ -732,15 +733,15 @@ def op_gated_mlp(dtype, x, w_in, b_in, w_out, b_out, gate, out=None, hidden=None
     elif flags & LINEAR_ACCUMULATE:
         raise ValueError("LINEAR_ACCUMULATE adds into `out`: give one")
     else:
-        out = torch.empty((M, D), dtype=out_type, device=dev)
+        out = x.new_empty((M, D), dtype=out_type) if flags else x.new_empty((M, D))
     if hidden is None:
-        hidden = torch.empty((M, N), dtype=want, device=dev)
+        hidden = x.new_empty((M, N))
     else:
         _expect("hidden", hidden, want, dev, (M, N))
     if pre is not None:
         _expect("pre", pre, want, dev, (M, 2 * N))
     elif save:
-        pre = torch.empty((M, 2 * N), dtype=want, device=dev)
+        pre = x.new_empty((M, 2 * N))
     lib = load_library()
     if dtype == DTYPE_F32:
         workspace = _workspace(torch, workspace, lib.epd_gated_mlp_workspace_bytes(dtype, M, N, K, D), dev)
@@ -761,13 +762,13 @@ def op_gated_mlp_backward(dtype, dout, x, w_in, w_out, hidden, pre, gate, bias=T
         _expect(name, t, want, x.device, shape)
     g = {}
     if need_dx:
-        g["dx"] = torch.empty((M, K), dtype=want, device=x.device)
+        g["dx"] = x.new_empty((M, K))
     if need_dw:
-        g["dw_in"] = torch.empty((2 * N, K), dtype=want, device=x.device)
-        g["dw_out"] = torch.empty((D, N), dtype=want, device=x.device)
+        g["dw_in"] = x.new_empty((2 * N, K))
+        g["dw_out"] = x.new_empty((D, N))
     if bias:
-        g["db_in"] = torch.empty(2 * N, dtype=want, device=x.device)
-        g["db_out"] = torch.empty(D, dtype=want, device=x.device)
+        g["db_in"] = x.new_empty(2 * N)
+        g["db_out"] = x.new_empty(D)
     lib = load_library()
     nbytes = lib.epd_gated_mlp_backward_workspace_bytes(dtype, M, N, K, D)
     workspace = _workspace(torch, workspace, nbytes, x.device)
@@ -801,11 +802,11 @@ def op_linear_backward(dtype, dout, x, w, bias=True, need_dx=True, need_dw=True,
         _expect(name, t, want, x.device, shape)
     g = {}
     if need_dx:
-        g["dx"] = torch.empty((M, K), dtype=want, device=x.device)
+        g["dx"] = x.new_empty((M, K))
     if need_dw:
-        g["dw"] = torch.empty((N, K), dtype=want, device=x.device)
+        g["dw"] = x.new_empty((N, K))
     if bias:
-        g["db"] = torch.empty(N, dtype=want, device=x.device)
+        g["db"] = x.new_empty(N)
     lib = load_library()
     workspace = _workspace(torch, workspace, lib.epd_linear_backward_workspace_bytes(dtype, M, N, K), x.device)
     _launch(torch, x.device, stream, lib.epd_op_linear_backward, "epd_op_linear_backward", dtype, _ptr(dout), _ld(dout, N),
@@ -832,7 +833,7 @@ def op_rope_axes(dtype, x, pos, sections, layout, theta, scale=1.0, inverse=Fals
     n = len(sections)
     ps = _check_positions(torch, pos, T, n, dev)
     if out is None:
-        out = torch.empty((T, heads, dh), dtype=want, device=dev)
+        out = x.new_empty((T, heads, dh))
     else:
         _expect("out", out, want, dev, x.shape)
 
@@ -853,7 +854,7 @@ def op_rope_axes_split(dtype, qkv, pos, heads, head_dim, sections, layout, theta
     n = len(sections)
     ps = _check_positions(torch, pos, T, n, qkv.device)
     dhp = (head_dim + 15) // 16 * 16
-    q, k, v = (torch.empty((heads, T, dhp), dtype=want, device=qkv.device) for _ in range(3))
+    q, k, v = (qkv.new_empty((heads, T, dhp)) for _ in range(3))
     _launch(torch, qkv.device, stream, load_library().epd_op_rope_axes_split, "epd_op_rope_axes_split", dtype, _ptr(qkv),
             _ld(qkv, 3 * heads * head_dim), _ptr(pos), ps, _ptr(q), _ptr(k), _ptr(v), T, heads, head_dim,
             (ctypes.c_int32 * n)(*sections), n, layout, theta, q_scale)
@@ -872,7 +873,7 @@ def op_rope_axes_split_backward(dtype, dq, dk, dv, pos, head_dim, sections, layo
             raise ValueError(f"{name} must be contiguous")
     n = len(sections)
     ps = _check_positions(torch, pos, T, n, dq.device)
-    dqkv = torch.empty((T, 3 * heads * head_dim), dtype=want, device=dq.device)
+    dqkv = dq.new_empty((T, 3 * heads * head_dim))
     _launch(torch, dq.device, stream, load_library().epd_op_rope_axes_split_backward, "epd_op_rope_axes_split_backward", dtype,
             _ptr(dq), _ptr(dk), _ptr(dv), _ptr(pos), ps, _ptr(dqkv), 3 * heads * head_dim, T, heads, head_dim,
             (ctypes.c_int32 * n)(*sections), n, layout, theta, q_scale)

@@ -282,6 +282,40 @@ column_sum_partial_kernel(const T* __restrict__ x, int64_t ldx, int64_t M, int64
   }
 }
 
+// Few rows: one launch, 8 threads side by side, 32 along the rows.
+constexpr int kDirectRows = 2048;
+
+template <typename T, int VEC>
+__global__ void __launch_bounds__(256)
+column_sum_direct_kernel(const T* __restrict__ x, int64_t ldx, int M, int64_t N, T* __restrict__ out) {
+  pdl_launch_dependents();
+  pdl_wait();
+  __shared__ float s_sum[32][8 * VEC + 1];
+  const int c = threadIdx.x & 7, r = threadIdx.x >> 3;
+  const int64_t n = ((int64_t)blockIdx.x * 8 + c) * VEC;
+  float acc[VEC] = {};
+  if (n < N) {
+#pragma unroll 8
+    for (int m = r; m < M; m += 32) {
+      alignas(16) T v[VEC];
+      if constexpr (VEC > 1) *reinterpret_cast<uint4*>(v) = *reinterpret_cast<const uint4*>(x + m * ldx + n);
+      else v[0] = x[m * ldx + n];
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) acc[e] += to_float<T>(v[e]);
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) s_sum[r][c * VEC + e] = acc[e];
+  __syncthreads();
+  const int64_t col = (int64_t)blockIdx.x * 8 * VEC + threadIdx.x;
+  if (threadIdx.x < 8 * VEC && col < N) {
+    float s = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 32; ++k) s += s_sum[k][threadIdx.x];
+    out[col] = from_float<T>(s);
+  }
+}
+
 // Second launch, for up to two sums at once: 32 columns by 8 threads along the partial sums.
 struct FinalSum {
   const float* part;
@@ -332,6 +366,20 @@ cudaError_t column_sum_partial(int dtype, const void* x, int64_t ldx, int64_t M,
     return whole ? column_sum_partial_t<float, 4>(x, ldx, M, N, part, s) : column_sum_partial_t<float, 1>(x, ldx, M, N, part, s);
   return whole ? column_sum_partial_t<__nv_bfloat16, 8>(x, ldx, M, N, part, s)
                : column_sum_partial_t<__nv_bfloat16, 1>(x, ldx, M, N, part, s);
+}
+template <typename T, int VEC>
+cudaError_t column_sum_direct_t(const void* x, int64_t ldx, int64_t M, int64_t N, void* out, cudaStream_t s) {
+  return launch_pdl(column_sum_direct_kernel<T, VEC>, dim3((unsigned)((N + 8 * VEC - 1) / (8 * VEC))), dim3(256), 0, s,
+                    static_cast<const T*>(x), ldx, (int)M, N, static_cast<T*>(out));
+}
+// Sums of up to kDirectRows rows.
+cudaError_t column_sum_direct(int dtype, const void* x, int64_t ldx, int64_t M, int64_t N, void* out, cudaStream_t s) {
+  const int vec = dtype == EPD_DTYPE_F32 ? 4 : 8;
+  const bool whole = ((uintptr_t)x & 15) == 0 && ldx % vec == 0 && N % vec == 0;
+  if (dtype == EPD_DTYPE_F32)
+    return whole ? column_sum_direct_t<float, 4>(x, ldx, M, N, out, s) : column_sum_direct_t<float, 1>(x, ldx, M, N, out, s);
+  return whole ? column_sum_direct_t<__nv_bfloat16, 8>(x, ldx, M, N, out, s)
+               : column_sum_direct_t<__nv_bfloat16, 1>(x, ldx, M, N, out, s);
 }
 cudaError_t column_sum_final(int dtype, const FinalSum& a, const FinalSum& b, cudaStream_t s) {
   const int64_t blocks = (a.N + 31) / 32 + (b.N + 31) / 32;
@@ -596,7 +644,9 @@ int epd_op_gated_mlp_backward(int32_t dtype, const void* dout, int64_t lddo, con
   float* part_out = reinterpret_cast<float*>(ws);
   ws += column_sum_bytes(M, D);
   FinalSum sum_in = {}, sum_out = {};
-  if (db_out) {
+  if (db_out && M <= kDirectRows) {
+    EPD_TRY(column_sum_direct(dtype, dout, lddo, M, D, db_out, s));
+  } else if (db_out) {
     EPD_TRY(column_sum_partial(dtype, dout, lddo, M, D, part_out, s));
     sum_out = FinalSum{part_out, sum_groups(M), D, db_out};
   }
@@ -665,8 +715,12 @@ int epd_op_linear_backward(int32_t dtype, const void* dout, int64_t lddo, const 
   }
   if (db) {
     float* part = static_cast<float*>(workspace);
-    EPD_TRY(column_sum_partial(dtype, dout, lddo, M, N, part, s));
-    EPD_TRY(column_sum_final(dtype, FinalSum{part, sum_groups(M), N, db}, FinalSum{}, s));
+    if (M <= kDirectRows) {
+      EPD_TRY(column_sum_direct(dtype, dout, lddo, M, N, db, s));
+    } else {
+      EPD_TRY(column_sum_partial(dtype, dout, lddo, M, N, part, s));
+      EPD_TRY(column_sum_final(dtype, FinalSum{part, sum_groups(M), N, db}, FinalSum{}, s));
+    }
   }
   if (planes) {
     char* ws = static_cast<char*>(workspace) + column_sum_bytes(M, N);

@@ -197,6 +197,12 @@ constexpr int kPasses = 6;
 constexpr int kSumBlocks = 8;  // F32: contraction blocks added up in one accumulator
 __device__ __forceinline__ int plane_a(int pass) { return (0x118 >> (2 * pass)) & 3; }    // 0, 2, 1, 0, 1, 0
 __device__ __forceinline__ int plane_b(int pass) { return (0x052 >> (2 * pass)) & 3; }    // 2, 0, 1, 1, 0, 0
+// GROUP, few rounds: the tiles a pair takes, tile[start[pair]] to tile[start[pair + 1] - 1] in turn.
+constexpr int kMaxPairs = 80, kDealtTiles = 592;
+struct Deal {
+  uint16_t start[kMaxPairs + 1];
+  uint16_t tile[kDealtTiles];
+};
 struct Problem {
   Sub sub[kSubs];              // GROUP: up to three, in the order of the launch's tiles; else the first
   CUtensorMap o1, o2;          // GATE: g, u; GATE_GRAD: out and o1 are dg, du
@@ -214,6 +220,8 @@ struct Problem {
   float* sums;                 // GATE_GRAD: column sums of 32 rows each, [ceil(M / 32), 2N], or NULL
   long long wait_limit;
   int* status;
+  int dealt;                   // GROUP: the tiles are dealt out by `deal`
+  Deal deal;
 };
 
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
@@ -351,8 +359,18 @@ gated_pair_kernel(const __grid_constant__ Problem p) {
   const int slice = SPLIT ? (int)(cta >> 1) : 0;                 // part of the contraction
   const int split = SPLIT ? p.split : 1;
   const WaitCtx wc{abort_flag, map_to_rank(smem_u32(const_cast<int*>(abort_flag)), cta ^ 1u), p.wait_limit};
-  const int first_tile = SPLIT ? p.tile0 + blockIdx.x / (2 * split) : blockIdx.x >> 1;
-  const int tile_step = SPLIT ? p.tiles : gridDim.x >> 1;        // SPLIT: one tile per cluster
+  // This pair's tiles, by number in turn: every gridDim.x / 2-th one, or those it was dealt.  SPLIT: one tile per cluster.
+  auto nth_tile = [&](int n) -> int {
+    if (SPLIT) return n == 0 ? p.tile0 + (int)blockIdx.x / (2 * split) : p.tiles;
+    if constexpr (MODE == MODE_GROUP) {
+      if (p.dealt) {
+        const int pair = blockIdx.x >> 1, at = p.deal.start[pair] + n;
+        return at < p.deal.start[pair + 1] ? p.deal.tile[at] : p.tiles;
+      }
+    }
+    return ((int)blockIdx.x >> 1) + n * ((int)gridDim.x >> 1);
+  };
+  const int first_tile = nth_tile(0);
   uint32_t loads_issued = 0;
 
   // Tile number -> product, place of the tile, part of the contraction (in blocks of BK)
@@ -767,7 +785,7 @@ gated_pair_kernel(const __grid_constant__ Problem p) {
     int stage = 0;
     uint32_t phase = 0;
     bool ok = true;
-    for (int tile = first_tile; tile < p.tiles && ok; tile += tile_step) {
+    for (int n = 0, tile = first_tile; tile < p.tiles && ok; tile = nth_tile(++n)) {
       int mt, nt, kb0, kb1;
       const Sub& u = locate(tile, mt, nt, kb0, kb1);
       const uint64_t pol_a = l2_policy(u.order.by_rows, u.order.stream_normal);
@@ -818,7 +836,7 @@ gated_pair_kernel(const __grid_constant__ Problem p) {
       uint32_t phase = 0;
       uint32_t acc_phase = 0;
       bool ok = true;
-      for (int tile = first_tile; tile < p.tiles && ok; tile += tile_step) {
+      for (int n = 0, tile = first_tile; tile < p.tiles && ok; tile = nth_tile(++n)) {
         int mt, nt, kb0, kb1;
         const Sub& u = locate(tile, mt, nt, kb0, kb1);
         const bool a_mn = MODE == MODE_GROUP && u.a_mn;
@@ -875,17 +893,17 @@ gated_pair_kernel(const __grid_constant__ Problem p) {
         tile_ready = mbar_wait_warp<true>(&tmem_full[0], 0, wc);
       }
     } else {
-      for (int tile = first_tile; tile < p.tiles; tile += tile_step) {
+      for (int n = 0, tile = first_tile; tile < p.tiles; tile = nth_tile(++n)) {
         int mt, nt, kb0, kb1;
         const Sub& u = locate(tile, mt, nt, kb0, kb1);
         load_bias(u, nt);
         if constexpr (F32) {
           if (!gather(kb0, kb1, acc_phase)) break;
-          finish_tile(u, mt, nt, tile + tile_step);
+          finish_tile(u, mt, nt, nth_tile(n + 1));
         } else {
           if (!mbar_wait_warp<true>(&tmem_full[acc], acc_phase, wc)) break;
           tc_fence_after();
-          finish_tile(u, mt, nt, tile + tile_step);
+          finish_tile(u, mt, nt, nth_tile(n + 1));
           if (++acc == 2) { acc = 0; acc_phase ^= 1; }
         }
       }
@@ -1033,6 +1051,54 @@ cudaError_t resident_pairs(int* out) {
   return cudaSuccess;
 }
 
+// Deals the tiles of the products, the longest first, each to a pair that has the least so far, so that tiles dealt one after
+// the other, which share operands, run at about the same time.  The time of the pair that gets the most, in blocks; a tile
+// costs its blocks and about 3 more (the first loads, the epilogue's exposed part).  Many rounds need none of this.
+int64_t deal(const int* tiles, const int* blocks, int n, int pairs, Deal* out) {
+  int64_t load[kMaxPairs] = {};
+  uint8_t owner[kDealtTiles];
+  int count[kMaxPairs] = {}, at = 0;
+  for (int i = 0; i < n; ++i) {
+    for (int left = tiles[i]; left > 0;) {
+      int64_t least = load[0];
+      for (int p = 1; p < pairs; ++p) least = load[p] < least ? load[p] : least;
+      for (int p = 0; p < pairs && left > 0; ++p)
+        if (load[p] == least) { load[p] += blocks[i] + 3; owner[at++] = (uint8_t)p; ++count[p]; --left; }
+    }
+  }
+  int64_t most = 0;
+  for (int p = 0; p < pairs; ++p) most = load[p] > most ? load[p] : most;
+  if (out) {
+    int fill[kMaxPairs];
+    out->start[0] = 0;
+    for (int p = 0; p < pairs; ++p) { fill[p] = out->start[p]; out->start[p + 1] = (uint16_t)(out->start[p] + count[p]); }
+    for (int t = 0; t < at; ++t) out->tile[fill[owner[t]]++] = (uint16_t)t;
+  }
+  return most;
+}
+// For `pairs` pairs, which an SM budget may have made few.
+bool deal_tiles(Problem* p, int pairs) {
+  if (pairs > kMaxPairs || p->tiles > kDealtTiles) return false;
+  int tiles[kSubs], blocks[kSubs];
+  for (int i = 0; i < p->subs; ++i) {
+    const Sub& u = p->sub[i];
+    tiles[i] = (i + 1 < p->subs ? p->sub[i + 1].first : p->tiles) - u.first;
+    blocks[i] = (u.K + BK - 1) / BK * (u.passes ? u.passes : 1);
+  }
+  deal(tiles, blocks, p->subs, pairs, &p->deal);
+  return true;
+}
+// The same time for tiles taken in turn, every pairs-th one: the first pair's.
+int64_t in_turn(const int* tiles, const int* blocks, int n, int pairs) {
+  int64_t cost = 0, at = 0;
+  for (int i = 0; i < n; ++i) {
+    const int64_t from = (pairs - at % pairs) % pairs;
+    if (from < tiles[i]) cost += (tiles[i] - from + pairs - 1) / pairs * (blocks[i] + 3);
+    at += tiles[i];
+  }
+  return cost;
+}
+
 template <int MODE, int GATE, bool SPLIT, bool F32>
 cudaError_t launch(Problem& p, cudaStream_t s) {
   using L = Smem<MODE, F32>;
@@ -1062,6 +1128,7 @@ cudaError_t launch(Problem& p, cudaStream_t s) {
     e = resident_pairs<MODE, GATE, F32>(&pairs);
     if (e != cudaSuccess) return e;
     const int avail = limited_sms(2 * pairs) / 2 > 0 ? limited_sms(2 * pairs) / 2 : 1;
+    if (p.dealt) p.dealt = deal_tiles(&p, p.tiles < avail ? p.tiles : avail) ? 1 : 0;
     cfg.gridDim = dim3(2 * (p.tiles < avail ? p.tiles : avail));
     return cudaLaunchKernelEx(&cfg, kern, p);
   }
@@ -1310,20 +1377,6 @@ namespace {
 
 int blocks_of(const ProductArg& a) { return (int)((a.K + BK - 1) / BK) * (a.planes_a ? kPasses : 1); }
 
-// Time of a launch of whole tiles in contraction blocks, with the products in the given order: the pair that starts with tile 0
-// has the most.  A tile costs its blocks and about 3 more (the first loads, the epilogue's exposed part).
-int64_t rounds_cost(const ProductArg* const* list, int n, int pairs) {
-  int64_t cost = 0, tile = 0;
-  for (int i = 0; i < n; ++i) {
-    const int64_t tiles = tiles_of(list[i]->M, list[i]->N, BN), len = blocks_of(*list[i]) + 3;
-    const int64_t from = (pairs - tile % pairs) % pairs;      // its first tile that falls to the first pair
-    if (from < tiles) cost += ((tiles - from + pairs - 1) / pairs) * len;
-    else if (i + 1 == n && cost == 0) cost = len;
-    tile += tiles;
-  }
-  return cost;
-}
-
 }  // namespace
 
 cudaError_t matmul_tc_group(const ProductArg* list, int n, cudaStream_t s) {
@@ -1336,14 +1389,20 @@ cudaError_t matmul_tc_group(const ProductArg* list, int n, cudaStream_t s) {
   const int pairs = device_sm_count() / 2;
   // One launch for all, or one launch each, which may share tiles among pairs (about 12 blocks' time for a launch).  Products
   // that are not asked for count as well: a result's bits do not depend on what else is formed.
-  int64_t apart = 0;
+  int64_t apart = 0, whole = 0;
+  int counts[kSubs], lens[kSubs];
   for (int i = 0; i < m; ++i) {
     const int64_t tiles = tiles_of(sorted[i]->M, sorted[i]->N, BN);
     const int blocks = blocks_of(*sorted[i]), split = choose_split(tiles, blocks);
-    apart += split > 1 ? blocks / split + 6 : rounds_cost(&sorted[i], 1, pairs);
+    apart += split > 1 ? blocks / split + 16 : (tiles + pairs - 1) / pairs * (blocks + 3);
     if (i > 0) apart += 12;
+    whole += tiles;
+    if (tiles > (1 << 28)) return cudaErrorInvalidValue;
+    counts[i] = (int)tiles;
+    lens[i] = blocks;
   }
-  const bool together = rounds_cost(sorted, m, pairs) <= apart;
+  const bool few = whole <= kDealtTiles && pairs <= kMaxPairs;
+  const bool together = (few ? deal(counts, lens, m, pairs, nullptr) : in_turn(counts, lens, m, pairs)) <= apart;
   for (int first = 0; first < m;) {
     const int count = together ? m : 1;
     Problem p = {};
@@ -1376,6 +1435,7 @@ cudaError_t matmul_tc_group(const ProductArg* list, int n, cudaStream_t s) {
     if (p.subs == 0) continue;
     p.tiles = (int)tiles;
     p.split = choose_split(all_tiles, shortest);
+    p.dealt = few && together && p.split == 1;
     const cudaError_t e = list[0].planes_a ? launch_either<MODE_GROUP, 0, true>(p, s) : launch_either<MODE_GROUP, 0>(p, s);
     if (e != cudaSuccess) return e;
   }
