@@ -196,6 +196,13 @@ rope_axes_staged_kernel(const __grid_constant__ AxesPlan plan, const __grid_cons
   // stretch i of the block -> shared memory, back to back
   const int stretches = g.head_major ? g.copies : ntok;
   const int full = g.copy_pieces, part = g.head_major ? ntok * (g.copy_pieces / g.tok) : g.copy_pieces;
+  const uint32_t s_x0 = (uint32_t)__cvta_generic_to_shared(s_x);
+  if (!g.head_major && a.src_token == g.copy_pieces * VEC) {
+    // the tokens' rows follow one another: one stretch
+    const T* src = static_cast<const T*>(a.src[0]) + j0 * a.src_token;
+    for (int i = threadIdx.x; i < ntok * full; i += blockDim.x)
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(s_x0 + i * 16), "l"(src + (size_t)i * VEC) : "memory");
+  } else
   for (int i = threadIdx.x; i < stretches * part; i += blockDim.x) {
     const int n = i / part, v = i - n * part;
     const T* src;
@@ -205,8 +212,7 @@ rope_axes_staged_kernel(const __grid_constant__ AxesPlan plan, const __grid_cons
     } else {
       src = static_cast<const T*>(a.src[0]) + (j0 + n) * a.src_token;
     }
-    const uint32_t to = (uint32_t)__cvta_generic_to_shared(s_x + ((size_t)n * full + v) * VEC);
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(src + v * VEC) : "memory");
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(s_x0 + (n * full + v) * 16), "l"(src + v * VEC) : "memory");
   }
   asm volatile("cp.async.commit_group;" ::: "memory");
   for (int i = threadIdx.x; i < ntok * plan.pairs; i += blockDim.x) {
