@@ -819,9 +819,9 @@ def op_linear_backward(dtype, dout, x, w, bias=True, need_dx=True, need_dw=True,
 
 def _check_positions(torch, pos, T, n_axes, device) -> int:
     if pos.dtype is not torch.int32 or pos.shape != (n_axes, T) or pos.device != device or \
-            (T > 1 and pos.stride(1) != 1):
-        raise ValueError(f"pos: expected int32 {(n_axes, T)} on {device}, each axis contiguous")
-    return max(T, pos.stride(0)) if n_axes > 1 else T
+            (T > 1 and pos.stride(1) != 1) or (n_axes > 1 and pos.stride(0) < T):
+        raise ValueError(f"pos: expected int32 {(n_axes, T)} on {device}, each axis contiguous, no two sharing memory")
+    return pos.stride(0) if n_axes > 1 else T
 
 
 def op_rope_axes(dtype, x, pos, sections, layout, theta, scale=1.0, inverse=False, out=None, stream=None):

@@ -419,6 +419,26 @@ def test_limited_sms_change_no_result():
     assert all(torch.equal(want[3][n], got[3][n]) for n in want[3])
 
 
+@pytest.mark.parametrize("M,N,K", [(700, 520, 1032), (40, 264, 2056)])   # whole tiles; tiles shared in clusters
+def test_expired_waits_end_and_leave_the_device_usable(M, N, K):
+    """With a wait limit of 1000 cycles ordinary waits (a first tile on its way from memory) run out: the kernels drain and
+    return, their results are undefined.  With the ordinary limit the same calls give the same bits as before."""
+    b = block(91, BF16, M, N, K)
+
+    def step():
+        out, hidden, pre = epd.op_gated_mlp(BF16, b["x"], b["w_in"], b["b_in"], b["w_out"], b["b_out"], epd.GATE_SILU, save=True)
+        g = epd.op_gated_mlp_backward(BF16, b["dout"], b["x"], b["w_in"], b["w_out"], hidden, pre, epd.GATE_SILU)
+        torch.cuda.synchronize()
+        return [out, hidden, pre] + list(g.values())
+    want = step()
+    epd.set_wait_limit(1000)
+    try:
+        step()
+    finally:
+        epd.set_wait_limit(0)
+    assert all(torch.equal(p, q) for p, q in zip(want, step()))
+
+
 def test_binding_refuses_mismatched_tensors():
     b = block(81, BF16, 4, 16, 24)
     ok = (b["x"], b["w_in"], b["b_in"], b["w_out"], b["b_out"])

@@ -257,7 +257,7 @@ def test_streams_and_graphs():
 
 def test_binding_refuses_mismatched_tensors():
     x, pos = normal(1, BF16, 10, 2, 64), positions(1, 2, 10)
-    for bad in (pos.long(), pos[:1], pos[:, :9], pos.cpu(), pos.t().contiguous().t()):
+    for bad in (pos.long(), pos[:1], pos[:, :9], pos.cpu(), pos.t().contiguous().t(), pos[:1].expand(2, 10)):
         with pytest.raises(ValueError):
             epd.op_rope_axes(BF16, x, bad, (16, 16), 0, THETA)
     for sections, layout, theta in (((16, 17), 0, THETA), ((-1, 4), 0, THETA), ((16, 16), 3, THETA),
