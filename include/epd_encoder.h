@@ -417,7 +417,9 @@ enum { EPD_GATE_SILU = 0, EPD_GATE_GELU_TANH = 1, EPD_GATE_GELU_ERF = 2 };   /* 
  * alone), free again once the call's work has run; calls that may overlap on the device need one each.  It is used for large
  * float blocks, whose products then run on the tensor cores with the precision of float (a float as the sum of three bf16
  * numbers; an infinity in an operand gives NaN there); the size is 0 otherwise.  NULL: plain FMAs, with the same precision.
- * M == 0 is valid and launches nothing.  Extents up to 2^28; EPD_EINVAL otherwise. */
+ * In bf16 pre and out are rounded once each, from the float sums.  M == 0 is valid and launches nothing.  Extents up to
+ * 2^28; EPD_EINVAL otherwise.  This call and the gradients below have no status word: a bounded device-side wait that
+ * expires leaves the outputs undefined and is not reported. */
 size_t epd_gated_mlp_workspace_bytes(int32_t dtype, int64_t M, int64_t N, int64_t K, int64_t D);
 int epd_op_gated_linear(int32_t dtype, const void* x, int64_t ldx, const void* w, int64_t ldw, const void* bias, void* out,
                         int64_t ldo, void* pre, int64_t ldp, void* workspace, size_t workspace_bytes, int64_t M, int64_t N,
@@ -530,8 +532,8 @@ int epd_feature_cache_stats(const epd_feature_cache_t* cache, int64_t* hits, int
 
 /* SM budget: the persistent kernels of this library (linear layers, attention) launch at most n_sms CTAs
  * (0 = every SM, the default), leaving the other SMs to kernels of a co-located stage on another stream or
- * in another process.  Process-wide; applies to launches made after the call.  Results do not depend on
- * it (the same tiles are computed, by fewer CTAs).  The short non-persistent kernels (RMSNorm, patchify,
+ * in another process (no fewer than one cluster, of up to 8 CTAs where a linear layer shares its tiles).  Process-wide;
+ * applies to launches made after the call.  Results do not depend on it (the same tiles are computed, by fewer CTAs).  The short non-persistent kernels (RMSNorm, patchify,
  * layout) are not limited. */
 int epd_set_sm_limit(int32_t n_sms);
 int32_t epd_get_sm_limit(void);

@@ -5,6 +5,7 @@
 //   da = dy Wo,  dg = da u act'(g),  du = da act(g),
 //   dx = [dg|du] W,  dW = [dg|du]^T x,  db = sum over rows of [dg|du],  dWo = dy^T a,  dbo = sum over rows of dy
 #include "gated.cuh"
+#include "tcgen05_common.cuh"
 
 namespace epd {
 namespace {
@@ -241,9 +242,13 @@ cudaError_t matmul_fma(int dtype, const FmaArgs& p, cudaStream_t s) {
 }
 
 // =============================================================================================
-// Column sums out[n] = sum_m x[m, n]: float sums of kSumRows rows each, then the sum of those, always in the same order (no
-// atomics).  First launch: 32 threads side by side with a 16-byte piece of the row each, 8 threads along the rows.
-// HBM bound.
+// Column sums out[n] = sum_m x[m, n], always in the same order (no atomics).  HBM bound by themselves; behind products of the
+// same call they run beside them: the products' kernel lets its successor start once everything in front of it is complete, a
+// block of these kernels fits on an SM beside one of it, and there are no more blocks than SMs.  The blocks then wait at their
+// end, so that what follows on the stream follows the products too.  (Gradients of a linear layer
+// 1152 -> 3456 of 6272 tokens: sums in front of the products 83 us, beside them 76, none 75.)
+// Long and narrow: float sums of kSumRows rows each, then the sum of those.  First launch: 32 threads side by side with a
+// 16-byte piece of the row each, 8 threads along the rows.
 // =============================================================================================
 constexpr int kSumRows = 64;
 
@@ -282,38 +287,52 @@ column_sum_partial_kernel(const T* __restrict__ x, int64_t ldx, int64_t M, int64
   }
 }
 
-// Few rows: one launch, 8 threads side by side, 32 along the rows.
+// In one launch: 8 threads side by side, 32 along the rows; 8 rows of a thread are added up before they join its sum.
 constexpr int kDirectRows = 2048;
 
 template <typename T, int VEC>
 __global__ void __launch_bounds__(256)
-column_sum_direct_kernel(const T* __restrict__ x, int64_t ldx, int M, int64_t N, T* __restrict__ out) {
+column_sum_direct_kernel(const T* x, int64_t ldx, int M, int64_t N, T* out, int beside) {
   pdl_launch_dependents();
-  pdl_wait();
+  if (!beside) pdl_wait();
   __shared__ float s_sum[32][8 * VEC + 1];
   const int c = threadIdx.x & 7, r = threadIdx.x >> 3;
-  const int64_t n = ((int64_t)blockIdx.x * 8 + c) * VEC;
-  float acc[VEC] = {};
-  if (n < N) {
-#pragma unroll 8
-    for (int m = r; m < M; m += 32) {
-      alignas(16) T v[VEC];
-      if constexpr (VEC > 1) *reinterpret_cast<uint4*>(v) = *reinterpret_cast<const uint4*>(x + m * ldx + n);
-      else v[0] = x[m * ldx + n];
+  for (int64_t n0 = (int64_t)blockIdx.x * 8 * VEC; n0 < N; n0 += (int64_t)gridDim.x * 8 * VEC) {
+    const int64_t n = n0 + c * VEC;
+    float acc[VEC] = {};
+    if (n < N) {
+      for (int m0 = r; m0 < M; m0 += 256) {
+        alignas(16) T v[8][VEC];
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) acc[e] += to_float<T>(v[e]);
+        for (int i = 0; i < 8; ++i) {
+          const int m = m0 + 32 * i;
+          if constexpr (VEC > 1)
+            *reinterpret_cast<uint4*>(v[i]) =
+                m < M ? __ldcg(reinterpret_cast<const uint4*>(x + m * ldx + n)) : make_uint4(0u, 0u, 0u, 0u);
+          else v[i][0] = m < M ? __ldcg(x + m * ldx + n) : from_float<T>(0.0f);
+        }
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          float sum = 0.0f;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) sum += to_float<T>(v[i][e]);
+          acc[e] += sum;
+        }
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) s_sum[r][c * VEC + e] = acc[e];
+    __syncthreads();
+    const int64_t col = n0 + threadIdx.x;
+    if (threadIdx.x < 8 * VEC && col < N) {
+      float s = 0.0f;
+#pragma unroll
+      for (int k = 0; k < 32; ++k) s += s_sum[k][threadIdx.x];
+      out[col] = from_float<T>(s);
     }
   }
-#pragma unroll
-  for (int e = 0; e < VEC; ++e) s_sum[r][c * VEC + e] = acc[e];
-  __syncthreads();
-  const int64_t col = (int64_t)blockIdx.x * 8 * VEC + threadIdx.x;
-  if (threadIdx.x < 8 * VEC && col < N) {
-    float s = 0.0f;
-#pragma unroll
-    for (int k = 0; k < 32; ++k) s += s_sum[k][threadIdx.x];
-    out[col] = from_float<T>(s);
-  }
+  if (beside) pdl_wait();
 }
 
 // Second launch, for up to two sums at once: 32 columns by 8 threads along the partial sums.
@@ -324,33 +343,43 @@ struct FinalSum {
 };
 template <typename T>
 __global__ void __launch_bounds__(256)
-column_sum_final_kernel(const FinalSum a, const FinalSum b) {
+column_sum_final_kernel(const FinalSum a, const FinalSum b, int beside) {
   pdl_launch_dependents();
-  pdl_wait();
+  if (!beside) pdl_wait();
   __shared__ float s_sum[8][33];
-  const int64_t blocks_a = (a.N + 31) / 32;
-  const bool second = blockIdx.x >= blocks_a;
-  const FinalSum& f = second ? b : a;
+  const int64_t blocks_a = (a.N + 31) / 32, blocks = blocks_a + (b.N + 31) / 32;
   const int c = threadIdx.x & 31, r = threadIdx.x >> 5;
-  const int64_t n = (blockIdx.x - (second ? blocks_a : 0)) * 32 + c;
-  float s = 0.0f;
-  if (n < f.N) {
+  for (int64_t block = blockIdx.x; block < blocks; block += gridDim.x) {
+    const bool second = block >= blocks_a;
+    const FinalSum& f = second ? b : a;
+    const int64_t n = (block - (second ? blocks_a : 0)) * 32 + c;
+    float s = 0.0f;
+    if (n < f.N) {
 #pragma unroll 8
-    for (int64_t g = r; g < f.groups; g += 8) s += f.part[g * f.N + n];
-  }
-  s_sum[r][c] = s;
-  __syncthreads();
-  if (r == 0 && n < f.N) {
-    float t = 0.0f;
+      for (int64_t g = r; g < f.groups; g += 8) s += __ldcg(f.part + g * f.N + n);
+    }
+    __syncthreads();
+    s_sum[r][c] = s;
+    __syncthreads();
+    if (r == 0 && n < f.N) {
+      float t = 0.0f;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) t += s_sum[k][c];
-    static_cast<T*>(f.out)[n] = from_float<T>(t);
+      for (int k = 0; k < 8; ++k) t += s_sum[k][c];
+      static_cast<T*>(f.out)[n] = from_float<T>(t);
+    }
   }
+  if (beside) pdl_wait();
 }
 
 size_t align256(size_t v) { return (v + 255) / 256 * 256; }
 int64_t sum_groups(int64_t M) { return (M + kSumRows - 1) / kSumRows; }
 size_t column_sum_bytes(int64_t M, int64_t N) { return align256((size_t)sum_groups(M) * N * 4); }
+
+// Blocks of a sum: beside other work no more than SMs.
+dim3 sum_grid(int64_t blocks, bool beside) {
+  const int64_t most = beside ? limited_sms(device_sm_count()) : 0x7fffffff;
+  return dim3((unsigned)(blocks < most ? blocks : most));
+}
 
 template <typename T, int VEC>
 cudaError_t column_sum_partial_t(const void* x, int64_t ldx, int64_t M, int64_t N, float* part, cudaStream_t s) {
@@ -368,24 +397,31 @@ cudaError_t column_sum_partial(int dtype, const void* x, int64_t ldx, int64_t M,
                : column_sum_partial_t<__nv_bfloat16, 1>(x, ldx, M, N, part, s);
 }
 template <typename T, int VEC>
-cudaError_t column_sum_direct_t(const void* x, int64_t ldx, int64_t M, int64_t N, void* out, cudaStream_t s) {
-  return launch_pdl(column_sum_direct_kernel<T, VEC>, dim3((unsigned)((N + 8 * VEC - 1) / (8 * VEC))), dim3(256), 0, s,
-                    static_cast<const T*>(x), ldx, (int)M, N, static_cast<T*>(out));
+cudaError_t column_sum_direct_t(const void* x, int64_t ldx, int64_t M, int64_t N, void* out, bool beside, cudaStream_t s) {
+  return launch_pdl(column_sum_direct_kernel<T, VEC>, sum_grid((N + 8 * VEC - 1) / (8 * VEC), beside), dim3(256), 0, s,
+                    static_cast<const T*>(x), ldx, (int)M, N, static_cast<T*>(out), (int)beside);
 }
-// Sums of up to kDirectRows rows.
-cudaError_t column_sum_direct(int dtype, const void* x, int64_t ldx, int64_t M, int64_t N, void* out, cudaStream_t s) {
+cudaError_t column_sum_direct(int dtype, const void* x, int64_t ldx, int64_t M, int64_t N, void* out, bool beside,
+                              cudaStream_t s) {
   const int vec = dtype == EPD_DTYPE_F32 ? 4 : 8;
   const bool whole = ((uintptr_t)x & 15) == 0 && ldx % vec == 0 && N % vec == 0;
   if (dtype == EPD_DTYPE_F32)
-    return whole ? column_sum_direct_t<float, 4>(x, ldx, M, N, out, s) : column_sum_direct_t<float, 1>(x, ldx, M, N, out, s);
-  return whole ? column_sum_direct_t<__nv_bfloat16, 8>(x, ldx, M, N, out, s)
-               : column_sum_direct_t<__nv_bfloat16, 1>(x, ldx, M, N, out, s);
+    return whole ? column_sum_direct_t<float, 4>(x, ldx, M, N, out, beside, s)
+                 : column_sum_direct_t<float, 1>(x, ldx, M, N, out, beside, s);
+  return whole ? column_sum_direct_t<__nv_bfloat16, 8>(x, ldx, M, N, out, beside, s)
+               : column_sum_direct_t<__nv_bfloat16, 1>(x, ldx, M, N, out, beside, s);
 }
-cudaError_t column_sum_final(int dtype, const FinalSum& a, const FinalSum& b, cudaStream_t s) {
+cudaError_t column_sum_final(int dtype, const FinalSum& a, const FinalSum& b, bool beside, cudaStream_t s) {
   const int64_t blocks = (a.N + 31) / 32 + (b.N + 31) / 32;
   if (blocks == 0) return cudaSuccess;
-  if (dtype == EPD_DTYPE_F32) return launch_pdl(column_sum_final_kernel<float>, dim3((unsigned)blocks), dim3(256), 0, s, a, b);
-  return launch_pdl(column_sum_final_kernel<__nv_bfloat16>, dim3((unsigned)blocks), dim3(256), 0, s, a, b);
+  return launch_pdl(dtype == EPD_DTYPE_F32 ? column_sum_final_kernel<float> : column_sum_final_kernel<__nv_bfloat16>,
+                    sum_grid(blocks, beside), dim3(256), 0, s, a, b, (int)beside);
+}
+// One launch: where the rows are few, or where the products of columns x other extent beside it take longer than its blocks, which
+// go through all rows of 64 columns each (about 4 ns a row; two products 3.4 ns a row for every 1024 x 1024).  Float products
+// leave no room beside them.  The choice goes by sizes alone: a result's bits do not depend on what else is formed.
+bool sum_direct(int dtype, int64_t M, int64_t columns, int64_t other) {
+  return M <= kDirectRows || (dtype == EPD_DTYPE_BF16 && other >= 128 && columns * other >= (1 << 20));
 }
 
 // =============================================================================================
@@ -644,12 +680,19 @@ int epd_op_gated_mlp_backward(int32_t dtype, const void* dout, int64_t lddo, con
   float* part_out = reinterpret_cast<float*>(ws);
   ws += column_sum_bytes(M, D);
   FinalSum sum_in = {}, sum_out = {};
-  if (db_out && M <= kDirectRows) {
-    EPD_TRY(column_sum_direct(dtype, dout, lddo, M, D, db_out, s));
-  } else if (db_out) {
+  const bool direct = sum_direct(dtype, M, D, N), beside = dx || dw_in || dw_out;
+  if (db_out && !direct) {
     EPD_TRY(column_sum_partial(dtype, dout, lddo, M, D, part_out, s));
     sum_out = FinalSum{part_out, sum_groups(M), D, db_out};
   }
+  // what is left of the bias gradients once their parts and the products are on the stream
+  auto bias_sums = [&]() -> cudaError_t {
+    if (db_out && direct) {
+      const cudaError_t e = column_sum_direct(dtype, dout, lddo, M, D, db_out, beside, s);
+      if (e != cudaSuccess) return e;
+    }
+    return column_sum_final(dtype, sum_in, sum_out, beside, s);
+  };
   int64_t groups = 0;
   if (dtype == EPD_DTYPE_F32 && float_tc_pays(M, N, K)) {
     const Planes pd = take_planes(&ws, M, 2 * N), py = take_planes(&ws, M, D), px = take_planes(&ws, M, K),
@@ -664,11 +707,11 @@ int epd_op_gated_mlp_backward(int32_t dtype, const void* dout, int64_t lddo, con
       EPD_TRY(gated_f32_gradient(py, po, static_cast<const float*>(pre), ldp, pd, db_in ? part_in : nullptr, M, N, D, gate, s));
       if (db_in) sum_in = FinalSum{part_in, (M + 31) / 32, 2 * N, db_in};
     }
-    EPD_TRY(column_sum_final(dtype, sum_in, sum_out, s));
     const ProductArg list[3] = {input_gradient(pd, pw, dx, lddx, M, 2 * N, K),
                                 weight_gradient(pd, px, dw_in, lddw_in, M, 2 * N, K),
                                 weight_gradient(py, ph, dw_out, lddw_out, M, D, N)};
-    return finish(matmul_tc_group(list, 3, s));
+    EPD_TRY(matmul_tc_group(list, 3, s));
+    return finish(bias_sums());
   }
   void* dpre = ws;
   if (inner) {
@@ -676,12 +719,12 @@ int epd_op_gated_mlp_backward(int32_t dtype, const void* dout, int64_t lddo, con
                           D, gate, s));
     if (db_in) sum_in = FinalSum{part_in, groups, 2 * N, db_in};
   }
-  EPD_TRY(column_sum_final(dtype, sum_in, sum_out, s));
-  return finish(products(dtype,
-                         {input_gradient(dpre, 2 * N, w_in, ldw_in, dx, lddx, M, 2 * N, K),
-                          weight_gradient(dpre, 2 * N, x, ldx, dw_in, lddw_in, M, 2 * N, K),
-                          weight_gradient(dout, lddo, hidden, ldh, dw_out, lddw_out, M, D, N)},
-                         s));
+  EPD_TRY(products(dtype,
+                   {input_gradient(dpre, 2 * N, w_in, ldw_in, dx, lddx, M, 2 * N, K),
+                    weight_gradient(dpre, 2 * N, x, ldx, dw_in, lddw_in, M, 2 * N, K),
+                    weight_gradient(dout, lddo, hidden, ldh, dw_out, lddw_out, M, D, N)},
+                   s));
+  return finish(bias_sums());
 }
 
 size_t epd_linear_backward_workspace_bytes(int32_t dtype, int64_t M, int64_t N, int64_t K) {
@@ -713,15 +756,14 @@ int epd_op_linear_backward(int32_t dtype, const void* dout, int64_t lddo, const 
     if (!workspace || (uintptr_t)workspace % 256) return EPD_EINVAL;
     if (workspace_bytes < epd_linear_backward_workspace_bytes(dtype, M, N, K)) return EPD_ENOMEM;
   }
-  if (db) {
-    float* part = static_cast<float*>(workspace);
-    if (M <= kDirectRows) {
-      EPD_TRY(column_sum_direct(dtype, dout, lddo, M, N, db, s));
-    } else {
-      EPD_TRY(column_sum_partial(dtype, dout, lddo, M, N, part, s));
-      EPD_TRY(column_sum_final(dtype, FinalSum{part, sum_groups(M), N, db}, FinalSum{}, s));
-    }
-  }
+  const bool direct = sum_direct(dtype, M, N, K), beside = dx || dw;
+  float* part = static_cast<float*>(workspace);
+  if (db && !direct) EPD_TRY(column_sum_partial(dtype, dout, lddo, M, N, part, s));
+  auto bias_sum = [&]() -> cudaError_t {      // behind the products
+    if (!db) return cudaSuccess;
+    return direct ? column_sum_direct(dtype, dout, lddo, M, N, db, beside, s)
+                  : column_sum_final(dtype, FinalSum{part, sum_groups(M), N, db}, FinalSum{}, beside, s);
+  };
   if (planes) {
     char* ws = static_cast<char*>(workspace) + column_sum_bytes(M, N);
     const Planes py = take_planes(&ws, M, N), px = take_planes(&ws, M, K), pw = take_planes(&ws, N, K);
@@ -729,12 +771,14 @@ int epd_op_linear_backward(int32_t dtype, const void* dout, int64_t lddo, const 
                           {dw ? static_cast<const float*>(x) : nullptr, ldx, M, px},
                           {dx ? static_cast<const float*>(w) : nullptr, ldw, N, pw}}, s));
     const ProductArg list[2] = {input_gradient(py, pw, dx, lddx, M, N, K), weight_gradient(py, px, dw, lddw, M, N, K)};
-    return finish(matmul_tc_group(list, 2, s));
+    EPD_TRY(matmul_tc_group(list, 2, s));
+    return finish(bias_sum());
   }
-  return finish(products(dtype,
-                         {input_gradient(dout, lddo, w, ldw, dx, lddx, M, N, K),
-                          weight_gradient(dout, lddo, x, ldx, dw, lddw, M, N, K)},
-                         s));
+  EPD_TRY(products(dtype,
+                   {input_gradient(dout, lddo, w, ldw, dx, lddx, M, N, K),
+                    weight_gradient(dout, lddo, x, ldx, dw, lddw, M, N, K)},
+                   s));
+  return finish(bias_sum());
 }
 
 }  // extern "C"

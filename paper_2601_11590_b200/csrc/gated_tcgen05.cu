@@ -219,7 +219,6 @@ struct Problem {
   int64_t planes_ld, planes_rows;   // leading dimension; rows of one plane
   float* sums;                 // GATE_GRAD: column sums of 32 rows each, [ceil(M / 32), 2N], or NULL
   long long wait_limit;
-  int* status;
   int dealt;                   // GROUP: the tiles are dealt out by `deal`
   Deal deal;
 };
@@ -342,7 +341,7 @@ gated_pair_kernel(const __grid_constant__ Problem p) {
   constexpr int kSteps = TILE_COLS / 32;                         // 32-column steps of a tile
   static_assert(MODE != MODE_LINEAR || SPLIT || F32, "whole tiles of a bf16 linear layer run on its own kernel");
 
-  pdl_launch_dependents();
+  if (MODE != MODE_GROUP) pdl_launch_dependents();
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kBarOffset);   // used in the leader only
@@ -405,6 +404,8 @@ gated_pair_kernel(const __grid_constant__ Problem p) {
   tc_fence_after();
   const uint32_t tmem_base = *tmem_base_slot;
   pdl_wait();   // nothing above touches global memory
+  // GROUP: the bias sums behind it run beside it and count on everything in front of it being complete
+  if (MODE == MODE_GROUP) pdl_launch_dependents();
 
   // Epilogue state that lives on past the role's loop in a split launch
   const int q = warp & 3;                          // TMEM lane quarter this warp may read
@@ -959,7 +960,6 @@ gated_pair_kernel(const __grid_constant__ Problem p) {
     // completes by itself and is waited for: the leader's producer waits for the last load of every stage (its barriers
     // count both CTAs' bytes), a commit behind the leader's products reaches both CTAs' drain barriers, the epilogue warps
     // have waited for their stores and fetches; then a fixed pause, and the cluster barrier.
-    if (threadIdx.x == 0 && p.status != nullptr) atomicCAS(p.status, 0, kStatusTimeout);
     if (warp == 0 && lane == 0 && rank == 0) drain_ring<true>(full, STAGES, loads_issued);
     if (warp == 1) {
       if (elect_one()) {
