@@ -39,7 +39,6 @@ struct AxesArgs {
   int rotate[3];
   int n_tensors, heads, dh;
   int pad;                          // elements behind head_dim that the destination rows carry (written), or 0
-  int src_pad;                      // elements behind head_dim that the source rows carry (not used), or 0
   int64_t src_token, src_head, dst_token, dst_head;   // strides in elements
   const int32_t* pos;
   int64_t pos_stride;
@@ -165,24 +164,31 @@ __device__ __forceinline__ void pack2(__nv_bfloat16* p, float2 v) {
   *reinterpret_cast<__nv_bfloat162*>(p) = __floats2bfloat162_rn(v.x, v.y);
 }
 
-// The same through shared memory: a block brings the rows of a few tokens in with 16-byte asynchronous copies, and every
-// thread writes whole 16-byte pieces of the destination, reading its own piece and the partners' elements (PW at a time)
-// from shared memory.  Global memory then sees full pieces in both directions whatever the sections, where the kernel above
-// reads and writes runs of U elements: 81628 tokens of 16 heads x 72 with sections of 12 took it 556 us.  A thread keeps its
-// token and its piece of the head, so the cosines and sines of the piece sit in its registers for all heads and tensors.
-constexpr int kStagedThreads = 320;
+// The same through shared memory: a block brings the rows of a few tokens in with 16-byte asynchronous copies, turns
+// them in place, and sends them out: a token's row in one bulk copy, other rows in 16-byte stores.  Global memory sees whole 16-byte pieces in both directions whatever the sections, where the
+// kernel above reads and writes runs of U elements.  What is not rotated (v) passes through without a thread touching it.
+// A thread keeps its token and PW pairs of the head, so their cosines and sines sit in its registers for all heads.  HBM bound:
+// bf16 81628 tokens of 16 heads x 72 with sections of 12, split 204 us (5.8 TB/s; 556 us in the kernel above), its gradient
+// 188 us (6.0), the rotation alone 125 us; heads of 128 6.2, float 6.4 to 6.7 TB/s.
+constexpr int kStagedThreads = 288;       // 32 rows of nine 16-byte pieces
+enum { STORE_ALL = 0, STORE_TOKENS = 1, STORE_PIECES = 2 };   // bulk copies of the block's tokens or of each; 16-byte stores
 struct Staging {
   int tok;                          // tokens of a block
-  int pieces;                       // 16-byte pieces of a destination row of one head
-  int groups;                       // threads that share a (token, piece) and deal the heads among themselves
-  int head_major;                   // the source holds a head's tokens together
-  int copy_pieces;                  // 16-byte pieces of one contiguous stretch of the source
-  int copies;                       // stretches of a block; row-major: one per token, head-major: one per tensor and head
-  int s_token, s_head, s_tensor;    // strides in shared memory, elements
+  int linear;                       // the source's tokens follow one another, as in shared memory
+  int row_pieces;                   // 16-byte pieces of a destination row of one head, padding included
+  int walks;                        // threads that share a (token, piece) and deal the heads among themselves
+  int slots;                        // threads of a token: units of PW pairs, then units of PW dimensions behind the last pair
+  int groups;                       // threads that share a (token, slot) and deal the heads among themselves
+  int store;
+  int s_token;                      // elements of a token in shared memory: tensors, heads and dimensions back to back
 };
 
+__device__ __forceinline__ void bulk_store(void* dst, uint32_t src, uint32_t bytes) {
+  asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(src), "r"(bytes) : "memory");
+}
+
 template <typename T, int PW>
-__global__ void __launch_bounds__(kStagedThreads, sizeof(T) == 2 && PW == 1 ? 3 : 4)
+__global__ void __launch_bounds__(kStagedThreads, 4)
 rope_axes_staged_kernel(const __grid_constant__ AxesPlan plan, const __grid_constant__ AxesArgs a,
                         const __grid_constant__ Staging g) {
   pdl_launch_dependents();
@@ -190,32 +196,35 @@ rope_axes_staged_kernel(const __grid_constant__ AxesPlan plan, const __grid_cons
   constexpr int VEC = 16 / (int)sizeof(T);
   extern __shared__ __align__(16) uint8_t staged[];
   float2* s_cs = reinterpret_cast<float2*>(staged);
-  T* s_x = reinterpret_cast<T*>(staged + (size_t)g.tok * plan.pairs * sizeof(float2) + (g.tok * plan.pairs % 2) * sizeof(float2));
+  T* s_x = reinterpret_cast<T*>(staged + (size_t)(g.tok * plan.pairs + 1) / 2 * 16);
+  const uint32_t s_x0 = (uint32_t)__cvta_generic_to_shared(s_x);
   const int64_t j0 = (int64_t)blockIdx.x * g.tok;
   const int ntok = (int)min((int64_t)g.tok, a.T - j0);
-  // stretch i of the block -> shared memory, back to back
-  const int stretches = g.head_major ? g.copies : ntok;
-  const int full = g.copy_pieces, part = g.head_major ? ntok * (g.copy_pieces / g.tok) : g.copy_pieces;
-  const uint32_t s_x0 = (uint32_t)__cvta_generic_to_shared(s_x);
-  if (!g.head_major && a.src_token == g.copy_pieces * VEC) {
-    // the tokens' rows follow one another: one stretch
-    const T* src = static_cast<const T*>(a.src[0]) + j0 * a.src_token;
-    for (int i = threadIdx.x; i < ntok * full; i += blockDim.x)
-      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(s_x0 + i * 16), "l"(src + (size_t)i * VEC) : "memory");
-  } else
-  for (int i = threadIdx.x; i < stretches * part; i += blockDim.x) {
-    const int n = i / part, v = i - n * part;
-    const T* src;
-    if (g.head_major) {
-      const int w = n / a.heads, h = n - w * a.heads;
-      src = static_cast<const T*>(w == 0 ? a.src[0] : w == 1 ? a.src[1] : a.src[2]) + h * a.src_head + j0 * a.src_token;
-    } else {
-      src = static_cast<const T*>(a.src[0]) + (j0 + n) * a.src_token;
+  auto source = [&](int w) { return static_cast<const T*>(w == 0 ? a.src[0] : w == 1 ? a.src[1] : a.src[2]); };
+  auto target = [&](int w) { return static_cast<T*>(w == 0 ? a.dst[0] : w == 1 ? a.dst[1] : a.dst[2]); };
+
+  // in and out a thread has one token and one 16-byte piece of the head, and walks tensors and heads with it
+  const int per_walk = g.tok * g.row_pieces, walk = threadIdx.x / per_walk, in_walk = threadIdx.x - walk * per_walk;
+  const int wt = in_walk / g.row_pieces, wd = (in_walk - wt * g.row_pieces) * VEC;
+  const bool walks = walk < g.walks && wt < ntok;
+  const int w_first = wt * g.s_token + walk * a.dh + wd, w_step = g.walks * a.dh;
+  if (g.linear) {
+    // the tokens' rows follow one another in the source: one stretch
+    const T* src = source(0) + j0 * a.src_token;
+    for (int i = threadIdx.x; i < ntok * g.s_token / VEC; i += kStagedThreads)
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(s_x0 + i * 16), "l"(src + i * VEC) : "memory");
+  } else if (walks && wd < a.dh) {
+    const int64_t step = g.walks * a.src_head;
+    for (int w = 0; w < a.n_tensors; ++w) {
+      const T* src = source(w) + (j0 + wt) * a.src_token + walk * a.src_head + wd;
+      uint32_t to = s_x0 + (w * a.heads * a.dh + w_first) * (uint32_t)sizeof(T);
+#pragma unroll 4
+      for (int h = walk; h < a.heads; h += g.walks, src += step, to += w_step * (uint32_t)sizeof(T))
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(src) : "memory");
     }
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(s_x0 + (n * full + v) * 16), "l"(src + v * VEC) : "memory");
   }
   asm volatile("cp.async.commit_group;" ::: "memory");
-  for (int i = threadIdx.x; i < ntok * plan.pairs; i += blockDim.x) {
+  for (int i = threadIdx.x; i < ntok * plan.pairs; i += kStagedThreads) {
     const int t = i / plan.pairs, p = i - t * plan.pairs;
     const int32_t pos = a.pos[plan.axis[p] * a.pos_stride + j0 + t];
     const double turns = (double)pos * plan.turns[p];
@@ -226,84 +235,105 @@ rope_axes_staged_kernel(const __grid_constant__ AxesPlan plan, const __grid_cons
   asm volatile("cp.async.wait_group 0;" ::: "memory");
   __syncthreads();
 
-  const int per_group = g.tok * g.pieces;
-  const int group = threadIdx.x / per_group;
-  const int within = threadIdx.x - group * per_group;
-  const int t = within / g.pieces, d0 = (within - t * g.pieces) * VEC;
-  if (group >= g.groups || t >= ntok) return;
-  int partner[VEC / PW];              // distance to the partners of a group of PW elements; 0: not rotated
-  int angle[VEC / PW];                // where the group's angles begin in s_cs
+  const int per_group = g.tok * g.slots;
+  const int group = threadIdx.x / per_group, within = threadIdx.x - group * per_group;
+  const int t = within / g.slots, slot = within - t * g.slots;
+  if (group < g.groups && t < ntok) {
+    const int units = plan.pairs / PW;
+    const bool turn = slot < units;
+    int d = 2 * plan.pairs + (slot - units) * PW, away = 0, angle = 0;     // first dimension; its partner's distance; angles
+    if (turn) {
+      int r = 0, f = slot * PW;
+      while (f >= plan.run_len[r]) f -= plan.run_len[r++];
+      d = plan.run_base[r] + f;
+      away = plan.run_len[r];
+      angle = t * plan.pairs + plan.run_pair[r] + f;
+    }
+    const int first = t * g.s_token + group * a.dh + d, s_step = g.groups * a.dh;
+    const int rotated = a.n_tensors < 2 ? 1 : 2;
+    for (int w = 0; w < rotated; ++w) {
+      const float sc = w == 0 ? a.scale[0] : a.scale[1];
+      T* s = s_x + w * a.heads * a.dh + first;
+      if constexpr (PW == 1) {
+        const float2 cs = turn ? s_cs[angle] : make_float2(1.0f, 0.0f);
+        const float c = cs.x * sc, sn = cs.y * sc;
+        for (int h = group; h < a.heads; h += g.groups, s += s_step) {
+          const float x = to_float<T>(s[0]);
+          if (turn) {
+            const float y = to_float<T>(s[away]);
+            s[0] = from_float<T>(fmaf(x, c, -y * sn));
+            s[away] = from_float<T>(fmaf(y, c, x * sn));
+          } else {
+            s[0] = from_float<T>(x * sc);
+          }
+        }
+      } else if (turn) {
+        float2 c[PW / 2], sn[PW / 2], neg[PW / 2];
 #pragma unroll
-  for (int u = 0; u < VEC / PW; ++u) {
-    const int d = d0 + u * PW;
-    partner[u] = angle[u] = 0;
-    if (d < 2 * plan.pairs) {
-      int r = 0;
-      while (d >= plan.run_base[r] + 2 * plan.run_len[r]) ++r;
-      const int len = plan.run_len[r], f = d - plan.run_base[r];
-      partner[u] = f < len ? len : -len;
-      angle[u] = t * plan.pairs + plan.run_pair[r] + (f < len ? f : f - len);
+        for (int e = 0; e < PW / 2; ++e) {
+          const float2 p = s_cs[angle + 2 * e], q = s_cs[angle + 2 * e + 1];
+          c[e] = make_float2(p.x * sc, q.x * sc);
+          sn[e] = make_float2(p.y * sc, q.y * sc);
+          neg[e] = make_float2(-sn[e].x, -sn[e].y);
+        }
+#pragma unroll 2
+        for (int h = group; h < a.heads; h += g.groups, s += s_step) {
+          alignas(16) T x[PW], y[PW];
+          load_vec<T, PW>(s, x);
+          load_vec<T, PW>(s + away, y);
+#pragma unroll
+          for (int e = 0; e < PW / 2; ++e) {
+            const float2 p = unpack2(x + 2 * e), q = unpack2(y + 2 * e);
+            pack2(x + 2 * e, fma2(p, c[e], mul2(q, neg[e])));
+            pack2(y + 2 * e, fma2(q, c[e], mul2(p, sn[e])));
+          }
+          store_vec<T, PW>(s, x);
+          store_vec<T, PW>(s + away, y);
+        }
+      } else {
+        for (int h = group; h < a.heads; h += g.groups, s += s_step) {
+          alignas(16) T x[PW];
+          load_vec<T, PW>(s, x);
+#pragma unroll
+          for (int e = 0; e < PW; ++e) x[e] = from_float<T>(to_float<T>(x[e]) * sc);
+          store_vec<T, PW>(s, x);
+        }
+      }
     }
   }
-  const T* sx = s_x + t * g.s_token + d0 + group * g.s_head;
-  const bool padding = d0 >= a.dh;
-  const int s_step = g.groups * g.s_head;
-  const int64_t d_step = g.groups * a.dst_head;
-  for (int w = 0; w < a.n_tensors; ++w, sx += g.s_tensor) {
-    T* dst = static_cast<T*>(w == 0 ? a.dst[0] : w == 1 ? a.dst[1] : a.dst[2]) + (j0 + t) * a.dst_token + group * a.dst_head + d0;
-    const T* s = sx;
-    if (padding) {
-      // column head_dim of v is 1 (the rest of the padding 0): the attention step's P V then yields the row sums
+  if (g.store == STORE_PIECES) {
+    __syncthreads();
+    if (!walks) return;
+    const int64_t step = g.walks * a.dst_head;
+    for (int w = 0; w < a.n_tensors; ++w) {
+      T* dst = target(w) + (j0 + wt) * a.dst_token + walk * a.dst_head + wd;
       alignas(16) T x[VEC];
-      const bool one = w == 2;
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) x[e] = from_float<T>(one && d0 + e == a.dh ? 1.0f : 0.0f);
-      for (int h = group; h < a.heads; h += g.groups, dst += d_step) store_vec<T, VEC>(dst, x);
-    } else if (w == 2) {
-#pragma unroll 2
-      for (int h = group; h < a.heads; h += g.groups, dst += d_step, s += s_step) {
-        alignas(16) T x[VEC];
-        load_vec<T, VEC>(s, x);
-        store_vec<T, VEC>(dst, x);
-      }
-    } else {
-      const float sc = w == 0 ? a.scale[0] : a.scale[1];
-      float2 c2[VEC / 2], s2[VEC / 2];
-#pragma unroll
-      for (int k = 0; k < VEC; ++k) {
-        const int u = k / PW;
-        float2 v = make_float2(1.0f, 0.0f);
-        if (partner[u] != 0) {
-          v = s_cs[angle[u] + k % PW];
-          if (partner[u] > 0) v.y = -v.y;
+      if (wd < a.dh) {
+        const T* from = s_x + w * a.heads * a.dh + w_first;
+#pragma unroll 4
+        for (int h = walk; h < a.heads; h += g.walks, dst += step, from += w_step) {
+          load_vec<T, VEC>(from, x);
+          store_vec<T, VEC>(dst, x);
         }
-        (k & 1 ? c2[k / 2].y : c2[k / 2].x) = v.x * sc;
-        (k & 1 ? s2[k / 2].y : s2[k / 2].x) = v.y * sc;
-      }
-#pragma unroll 2
-      for (int h = group; h < a.heads; h += g.groups, dst += d_step, s += s_step) {
-        alignas(16) T x[VEC], y[VEC];
-        load_vec<T, VEC>(s, x);
+      } else {
+        // column head_dim of v is 1 (the rest of the padding 0): the attention step's P V then yields the row sums
 #pragma unroll
-        for (int u = 0; u < VEC / PW; ++u) {
-          T part[PW];
-          if (partner[u] != 0) {
-            load_vec<T, PW>(s + u * PW + partner[u], part);
-          } else {
-#pragma unroll
-            for (int e = 0; e < PW; ++e) part[e] = from_float<T>(0.0f);
-          }
-#pragma unroll
-          for (int e = 0; e < PW; ++e) y[u * PW + e] = part[e];
-        }
-#pragma unroll
-        for (int e = 0; e < VEC / 2; ++e) {
-          const float2 r = fma2(unpack2(x + 2 * e), c2[e], mul2(unpack2(y + 2 * e), s2[e]));
-          pack2(x + 2 * e, r);
-        }
-        store_vec<T, VEC>(dst, x);
+        for (int e = 0; e < VEC; ++e) x[e] = from_float<T>(w == 2 && wd + e == a.dh ? 1.0f : 0.0f);
+#pragma unroll 4
+        for (int h = walk; h < a.heads; h += g.walks, dst += step) store_vec<T, VEC>(dst, x);
       }
     }
+    return;
+  }
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  __syncthreads();
+  const int copies = g.store == STORE_ALL ? 1 : ntok;
+  const uint32_t elems = (g.store == STORE_ALL ? ntok : 1) * g.s_token;
+  if (threadIdx.x < copies) {
+    bulk_store(target(0) + (j0 + threadIdx.x) * a.dst_token, s_x0 + threadIdx.x * g.s_token * (uint32_t)sizeof(T),
+               elems * (uint32_t)sizeof(T));
+    tc::bulk_commit();
+    tc::bulk_wait_all();
   }
 }
 
@@ -382,50 +412,49 @@ cudaError_t launch(const AxesPlan& p, const AxesArgs& a, cudaStream_t s) {
 
 // Shared memory a block of the staged kernel may take: four blocks on an SM.
 constexpr size_t kStagedBytes = 54 * 1024;
+constexpr size_t kStagedMost = 110 * 1024;      // where one token takes more than that: two blocks
+// Shortest stretch that is worth a bulk copy: as bulk copies, a head's 7 tokens of 160 bytes made the split of 81628 tokens
+// (16 heads x 72) no faster than without them (240 us), a token's row of 6.9 KB its gradient 189 us instead of 247.
+constexpr int kBulkBytes = 2048;
 
-// The staged kernel takes whole 16-byte pieces: every contiguous stretch of the source and every row of the destination
-// starts on a 16-byte boundary and is a multiple of 16 bytes long, and there are tokens enough for a block on every SM
-// (below that the register kernel, which deals heads to blocks, has the shorter latency: one token 3.4 us).
+// The staged kernel takes whole 16-byte pieces: every row of the source and of the destination starts on a 16-byte boundary and
+// is a multiple of 16 bytes long, and there are tokens enough for a block on every SM (below that the register kernel, which
+// deals heads to blocks, has the shorter latency: one token 3.4 us).
 template <typename T>
-bool plan_staging(const AxesArgs& a, const AxesPlan& p, Staging* g, size_t* bytes) {
+bool plan_staging(const AxesArgs& a, const AxesPlan& p, int pw, Staging* g, size_t* bytes) {
   constexpr int VEC = 16 / (int)sizeof(T);
   if (a.dh % VEC || a.pad % VEC || a.src_token % VEC || a.src_head % VEC || a.dst_token % VEC || a.dst_head % VEC) return false;
   for (int i = 0; i < a.n_tensors; ++i)
     if (((uintptr_t)a.src[i] | (uintptr_t)a.dst[i]) & 15) return false;
-  // row-major: a token's tensors and heads lie back to back; head-major: a head's tokens do
-  bool row = a.heads == 1 || a.src_head == a.dh;
-  for (int i = 1; i < a.n_tensors; ++i)
-    row = row && static_cast<const char*>(a.src[i]) ==
-                     static_cast<const char*>(a.src[0]) + (size_t)i * a.heads * a.dh * sizeof(T);
-  const int src_row = a.dh + a.src_pad;
-  if (!row && a.src_token != src_row) return false;
-  g->head_major = !row;
-  const int row_elems = row ? a.dh : src_row;
-  const int64_t token_bytes = (int64_t)a.n_tensors * a.heads * row_elems * (int)sizeof(T) + p.pairs * 8;
-  if (token_bytes > (int64_t)kStagedBytes) return false;
+  const int row = a.dh + a.pad;
+  const int64_t token_bytes = (int64_t)a.n_tensors * a.heads * a.dh * (int)sizeof(T) + p.pairs * 8;
+  if (token_bytes > (int64_t)kStagedMost - 64) return false;
+  g->slots = p.pairs / pw + (a.scale[0] != 1.0f ? (a.dh - 2 * p.pairs) / pw : 0);
+  if (g->slots == 0) g->slots = 1;          // nothing turns: one idle slot
   int tok = (int)(kStagedBytes / token_bytes);
-  tok = tok > kMaxTokens ? kMaxTokens : tok;
-  while (tok > 1 && a.T < (int64_t)tok * 2 * 148) --tok;
+  tok = tok > kMaxTokens ? kMaxTokens : tok < 1 ? 1 : tok;
+  while (tok > 1 && (a.T < (int64_t)tok * 2 * 148 || tok * g->slots > kStagedThreads || tok * (row / VEC) > kStagedThreads)) --tok;
   if (a.T < (int64_t)tok * 148) return false;
   g->tok = tok;
-  g->pieces = (a.dh + a.pad) / VEC;
-  const int per_group = tok * g->pieces;
-  const int most = kStagedThreads / per_group > 0 ? kStagedThreads / per_group : 1;
-  const int rounds = (a.heads + most - 1) / most;
-  g->groups = (a.heads + rounds - 1) / rounds;      // no more than the rounds need
-  if (row) {
-    g->copies = tok;
-    g->copy_pieces = a.n_tensors * a.heads * a.dh / VEC;
-    g->s_token = a.n_tensors * a.heads * a.dh;
-    g->s_head = a.dh;
-    g->s_tensor = a.heads * a.dh;
-  } else {
-    g->copies = a.n_tensors * a.heads;
-    g->copy_pieces = tok * src_row / VEC;
-    g->s_token = src_row;
-    g->s_head = tok * src_row;
-    g->s_tensor = a.heads * tok * src_row;
-  }
+  auto deal_heads = [&](int threads) {              // groups of threads, no more than the rounds need
+    const int most = kStagedThreads / threads > 0 ? kStagedThreads / threads : 1, rounds = (a.heads + most - 1) / most;
+    return (a.heads + rounds - 1) / rounds;
+  };
+  g->groups = deal_heads(tok * g->slots);
+  g->row_pieces = row / VEC;
+  g->walks = deal_heads(tok * g->row_pieces);
+  g->s_token = a.n_tensors * a.heads * a.dh;
+  // whether a token's tensors and heads lie back to back
+  auto packed = [&](const auto* ptr, int64_t head) {
+    bool back_to_back = a.heads == 1 || head == a.dh;
+    for (int i = 1; i < a.n_tensors; ++i)
+      back_to_back = back_to_back && (const char*)ptr[i] == (const char*)ptr[0] + (size_t)i * a.heads * a.dh * sizeof(T);
+    return back_to_back;
+  };
+  g->linear = packed(a.src, a.src_head) && a.src_token == g->s_token;
+  g->store = a.pad || !packed(a.dst, a.dst_head) || g->s_token * (int)sizeof(T) < kBulkBytes ? STORE_PIECES
+             : a.dst_token == g->s_token                                                     ? STORE_ALL
+                                                                                             : STORE_TOKENS;
   *bytes = (size_t)tok * (size_t)token_bytes + 16;
   return true;
 }
@@ -435,34 +464,27 @@ cudaError_t launch_staged(const AxesPlan& p, const AxesArgs& a, const Staging& g
   auto kern = rope_axes_staged_kernel<T, PW>;
   static PerDeviceOnce configured;
   cudaError_t e = once_per_device(configured, [&] {
-    return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kStagedBytes + 64);
+    return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kStagedMost);
   });
   if (e != cudaSuccess) return e;
   const int64_t blocks = (a.T + g.tok - 1) / g.tok;
-  const int threads = (g.tok * g.pieces * g.groups + 31) / 32 * 32;
-  return launch_pdl(kern, dim3((unsigned)blocks), dim3(threads), bytes, s, p, a, g);
+  return launch_pdl(kern, dim3((unsigned)blocks), dim3(kStagedThreads), bytes, s, p, a, g);
 }
 
 // Widest vector that every run, every stride and every pointer allows.
 cudaError_t dispatch(int dtype, const AxesPlan& p, const AxesArgs& a, cudaStream_t s) {
   if (a.T == 0) return cudaSuccess;
   const int es = dtype == EPD_DTYPE_F32 ? 4 : 2;
-  // elements that share a run and its partners' run: the width of a partner access
-  int pw = 16 / es;
+  // pairs of a thread in shared memory: with 4 or 8 (accesses of 8 or 16 bytes) a thread has more angles to set up and fewer heads
+  // to use them on, and bf16 heads of 128 took 80 or 109 us for 77 (12543 tokens of 25 heads); heads of 72 the same
+  int pw = 2;
   for (int r = 0; r < p.n_runs; ++r)
-    while (p.run_len[r] % pw || p.run_base[r] % pw) pw >>= 1;
+    if (p.run_len[r] % 2 || p.run_base[r] % 2) pw = 1;
   Staging g;
   size_t bytes = 0;
-  if (dtype == EPD_DTYPE_F32 ? plan_staging<float>(a, p, &g, &bytes) : plan_staging<__nv_bfloat16>(a, p, &g, &bytes)) {
-    if (dtype == EPD_DTYPE_F32) {
-      if (pw == 4) return launch_staged<float, 4>(p, a, g, bytes, s);
-      if (pw == 2) return launch_staged<float, 2>(p, a, g, bytes, s);
-      return launch_staged<float, 1>(p, a, g, bytes, s);
-    }
-    if (pw == 8) return launch_staged<__nv_bfloat16, 8>(p, a, g, bytes, s);
-    if (pw == 4) return launch_staged<__nv_bfloat16, 4>(p, a, g, bytes, s);
-    if (pw == 2) return launch_staged<__nv_bfloat16, 2>(p, a, g, bytes, s);
-    return launch_staged<__nv_bfloat16, 1>(p, a, g, bytes, s);
+  if (dtype == EPD_DTYPE_F32 ? plan_staging<float>(a, p, pw, &g, &bytes) : plan_staging<__nv_bfloat16>(a, p, pw, &g, &bytes)) {
+    if (dtype == EPD_DTYPE_F32) return pw == 2 ? launch_staged<float, 2>(p, a, g, bytes, s) : launch_staged<float, 1>(p, a, g, bytes, s);
+    return pw == 2 ? launch_staged<__nv_bfloat16, 2>(p, a, g, bytes, s) : launch_staged<__nv_bfloat16, 1>(p, a, g, bytes, s);
   }
   int u = 16 / es;
   auto fits = [&](int w) {
@@ -604,7 +626,6 @@ int epd_op_rope_axes_split_backward(int32_t dtype, const void* dq, const void* d
   a.n_tensors = 3;
   a.heads = heads;
   a.dh = head_dim;
-  a.src_pad = dhp - head_dim;
   a.src_token = dhp;
   a.src_head = T * dhp;
   a.dst_token = lddqkv;

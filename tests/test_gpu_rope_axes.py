@@ -134,6 +134,50 @@ def test_strided_views(dtype, offset):
         assert bool(torch.isnan(big).all())
 
 
+@pytest.mark.parametrize("dtype,heads,dh,sections", [(BF16, 20, 128, (16, 24, 24)), (F32, 20, 72, (11, 7, 12)),
+                                                     (BF16, 9, 96, (6, 5, 3)), (F32, 124, 128, (20, 20)),
+                                                     (BF16, 16, 72, (12, 12, 12)), (F32, 3, 64, (0, 0))])
+def test_many_tokens_in_every_arrangement(dtype, heads, dh, sections):
+    """Enough tokens for whole blocks of them: rows back to back, gaps behind tokens or heads, head-major rows, on either side;
+    a last block with fewer tokens; NaN in dimensions that do not turn stays where it is."""
+    T = 1333
+    dt = torch.float32 if dtype == F32 else torch.bfloat16
+    pos = positions(5, len(sections), T)
+    x = normal(6, dtype, T, heads, dh)
+    R = sum(sections)
+    if 2 * R < dh:
+        x[1::3, :, 2 * R] = float("nan")
+
+    def empty(kind):
+        if kind == "packed":
+            return torch.full((T, heads, dh), float("nan"), dtype=dt, device="cuda"), None
+        if kind == "token gap":
+            big = torch.full((T, heads * dh + 24), 7.0, dtype=dt, device="cuda")
+            return big[:, :heads * dh].unflatten(1, (heads, dh)), big[:, heads * dh:]
+        if kind == "head gap":
+            big = torch.full((T, heads, dh + 8), 7.0, dtype=dt, device="cuda")
+            return big[:, :, :dh], big[:, :, dh:]
+        big = torch.full((heads, T, dh), 7.0, dtype=dt, device="cuda")
+        return big.transpose(0, 1), None
+    for n, layout in enumerate(LAYOUTS):
+        ref = rotate(x.double(), pos, sections, layout) * 0.37
+        known = torch.isfinite(ref)
+        for kind in ("packed", "token gap", "head gap", "head-major"):
+            src, _ = empty(kind)
+            src.copy_(x)
+            for into in ("packed", "token gap", "head gap", "head-major"):
+                if n and into != kind:
+                    continue
+                out, gap = empty(into)
+                epd.op_rope_axes(dtype, src, pos, sections, layout, THETA, scale=0.37, out=out)
+                parity(torch.where(known, out, torch.zeros_like(out)), torch.where(known, ref, torch.zeros_like(ref)), TOL[dtype],
+                       f"{kind} -> {into}")
+                assert torch.equal(torch.isnan(out), torch.isnan(ref))
+                assert gap is None or bool((gap == 7.0).all())
+            epd.op_rope_axes(dtype, src, pos, sections, layout, THETA, scale=0.37, out=src)     # in place
+            assert torch.equal(src[known], epd.op_rope_axes(dtype, x, pos, sections, layout, THETA, scale=0.37)[known])
+
+
 def split_reference(qkv, pos, heads, dh, sections, layout, q_scale):
     T = qkv.shape[0]
     x = qkv.double().view(T, 3, heads, dh)
