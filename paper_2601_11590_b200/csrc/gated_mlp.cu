@@ -16,8 +16,10 @@ namespace {
 // thread in two groups of rows by two groups of columns (the gated product keeps a column's gate in the first group and its
 // up projection in the second), two outputs per instruction (fma.rn.f32x2), the next block of the contraction fetched into
 // registers while the present one is multiplied out of one of two buffers.  Bound by the FMA pipe.
-// Where the tiles are fewer than the SMs, the 2, 4 or 8 CTAs of a cluster share a tile, each with a part of the contraction;
+// A 64 x 64 tile has two groups of threads, each with half of every block's steps.  Where the tiles are fewer than the SMs, the 2, 4 or 8 CTAs of a cluster share a tile, each with a part of the contraction;
 // each then adds up some of the rows from all parts, in order, out of the others' shared memory.
+// A kernel lets its successor start once everything in front of itself is complete.  One that needs nothing of its predecessor
+// (`beside`: a second and third product of the same inputs) runs along with it and waits for it at its end.
 // =============================================================================================
 constexpr int FK = 16;
 
@@ -38,6 +40,7 @@ struct FmaArgs {
   void* dpre;                // GATE_GRAD: dg|du [M, 2N]
   int64_t lddp;
   int gate;
+  int beside;
 };
 
 __device__ __forceinline__ uint64_t pair_of(float a) {
@@ -56,11 +59,13 @@ struct FmaTile {
   static_assert(kFloats >= TM * TN || TM > 64, "a shared tile's sums take the place of its buffers");
 };
 
-template <typename T, int TM, int TN, int RM, int RN, bool A_MN, bool B_MN, int EPI>
-__global__ void __launch_bounds__((TM / RM) * (TN / RN))
+template <typename T, int TM, int TN, int RM, int RN, int G, int WIDTH, bool A_MN, bool B_MN, int EPI>
+__global__ void __launch_bounds__(G * (TM / RM) * (TN / RN), 256 / TM < 2 ? 1 : 2)
 matmul_fma_kernel(const FmaArgs p, const int split) {
+  if (!p.beside) pdl_wait();
+  pdl_launch_dependents();
   using L = FmaTile<TM, TN>;
-  constexpr int kThreads = (TM / RM) * (TN / RN);
+  constexpr int kGroup = (TM / RM) * (TN / RN), kThreads = G * kGroup;
   constexpr int LA = TM * FK / kThreads, LB = TN * FK / kThreads;
   constexpr int COLS = EPI == EPI_GATE ? TN / 2 : TN;     // output columns of a tile
   __shared__ __align__(16) float smem[L::kFloats];
@@ -68,72 +73,110 @@ matmul_fma_kernel(const FmaArgs p, const int split) {
   float* const sb = smem + 2 * FK * L::kPadM;
   const T* A = static_cast<const T*>(p.a);
   const T* B = static_cast<const T*>(p.b);
-  const int tx = threadIdx.x % (TN / RN), ty = threadIdx.x / (TN / RN);
+  const int group = threadIdx.x / kGroup, in_group = threadIdx.x % kGroup;
+  const int tx = in_group % (TN / RN), ty = in_group / (TN / RN);
   const int part = blockIdx.x % split;
   const int64_t m0 = (int64_t)(blockIdx.x / split) * TM, n0 = (int64_t)blockIdx.y * COLS;
   const int64_t blocks = (p.K + FK - 1) / FK;
   const int64_t b0 = part * blocks / split, b1 = (part + 1) * blocks / split;
-  float ra[LA], rb[LB];
-  auto fetch = [&](int64_t k0) {
+  // A thread's elements of a block, WIDTH next to one another in memory: its place in the tile (row, step), whether its row exists,
+  // and where it is in the first block.
+  constexpr int VA = LA / WIDTH, VB = LB / WIDTH;
+  alignas(16) float ra[LA], rb[LB];
+  auto place = [&](bool mn, int extent, int i, int& r, int& k) {
+    const int e = (threadIdx.x + kThreads * i) * WIDTH;
+    r = mn ? e % extent : e / FK;
+    k = mn ? e / extent : e % FK;
+  };
+  const T* at_a[VA];
+  const T* at_b[VB];
 #pragma unroll
-    for (int i = 0; i < LA; ++i) {
-      const int e = threadIdx.x + kThreads * i;
-      const int r = A_MN ? e % TM : e / FK, kk = A_MN ? e / TM : e % FK;
-      const int64_t m = m0 + r, k = k0 + kk;
-      ra[i] = (m < p.M && k < p.K) ? to_float<T>(A_MN ? A[k * p.lda + m] : A[m * p.lda + k]) : 0.0f;
+  for (int i = 0; i < VA; ++i) {
+    int r, k;
+    place(A_MN, TM, i, r, k);
+    at_a[i] = m0 + r < p.M ? A + (A_MN ? (b0 * FK + k) * p.lda + m0 + r : (m0 + r) * p.lda + b0 * FK + k) : nullptr;
+  }
+#pragma unroll
+  for (int i = 0; i < VB; ++i) {
+    int r, k;
+    place(B_MN, TN, i, r, k);
+    // gated: the tile's second half of columns is the up projection of the first half's
+    const int64_t c = n0 + (EPI == EPI_GATE ? r % COLS : r), n = EPI == EPI_GATE && r >= COLS ? p.N + c : c;
+    at_b[i] = c < p.N ? B + (B_MN ? (b0 * FK + k) * p.ldb + n : n * p.ldb + b0 * FK + k) : nullptr;
+  }
+  auto take = [&](const T* from, bool in, float* to) {
+    if constexpr (WIDTH == 4) *reinterpret_cast<float4*>(to) = in ? *reinterpret_cast<const float4*>(from) : make_float4(0.f, 0.f, 0.f, 0.f);
+    else *to = in ? to_float<T>(*from) : 0.0f;
+  };
+  auto fetch = [&](int64_t block) {       // and on to the next block
+    const int64_t left = p.K - block * FK;
+#pragma unroll
+    for (int i = 0; i < VA; ++i) {
+      int r, k;
+      place(A_MN, TM, i, r, k);
+      take(at_a[i], at_a[i] != nullptr && k < left, ra + i * WIDTH);
+      if (at_a[i]) at_a[i] += A_MN ? FK * p.lda : FK;
     }
 #pragma unroll
-    for (int i = 0; i < LB; ++i) {
-      const int e = threadIdx.x + kThreads * i;
-      const int r = B_MN ? e % TN : e / FK, kk = B_MN ? e / TN : e % FK;
-      // gated: the tile's second half of columns is the up projection of the first half's
-      const int64_t c = n0 + (EPI == EPI_GATE ? r % COLS : r), k = k0 + kk;
-      const int64_t n = EPI == EPI_GATE && r >= COLS ? p.N + c : c;
-      rb[i] = (c < p.N && k < p.K) ? to_float<T>(B_MN ? B[k * p.ldb + n] : B[n * p.ldb + k]) : 0.0f;
+    for (int i = 0; i < VB; ++i) {
+      int r, k;
+      place(B_MN, TN, i, r, k);
+      take(at_b[i], at_b[i] != nullptr && k < left, rb + i * WIDTH);
+      if (at_b[i]) at_b[i] += B_MN ? FK * p.ldb : FK;
+    }
+  };
+  auto put_one = [&](bool mn, const float* v, float* tile, int pad, int r, int k) {
+    if (WIDTH == 4 && mn) {
+      *reinterpret_cast<float4*>(tile + k * pad + r) = *reinterpret_cast<const float4*>(v);
+    } else {
+#pragma unroll
+      for (int e = 0; e < WIDTH; ++e) tile[(k + e) * pad + r] = v[e];
     }
   };
   auto put = [&](int buf) {
 #pragma unroll
-    for (int i = 0; i < LA; ++i) {
-      const int e = threadIdx.x + kThreads * i;
-      sa[(buf * FK + (A_MN ? e / TM : e % FK)) * L::kPadM + (A_MN ? e % TM : e / FK)] = ra[i];
+    for (int i = 0; i < VA; ++i) {
+      int r, k;
+      place(A_MN, TM, i, r, k);
+      put_one(A_MN, ra + i * WIDTH, sa + buf * FK * L::kPadM, L::kPadM, r, k);
     }
 #pragma unroll
-    for (int i = 0; i < LB; ++i) {
-      const int e = threadIdx.x + kThreads * i;
-      sb[(buf * FK + (B_MN ? e / TN : e % FK)) * L::kPadN + (B_MN ? e % TN : e / FK)] = rb[i];
+    for (int i = 0; i < VB; ++i) {
+      int r, k;
+      place(B_MN, TN, i, r, k);
+      put_one(B_MN, rb + i * WIDTH, sb + buf * FK * L::kPadN, L::kPadN, r, k);
     }
   };
-  uint64_t acc2[RM][RN / 2] = {};
+  uint64_t acc2[RM / 2][RN] = {};      // pairs of rows
   if (b0 < b1) {
-    fetch(b0 * FK);
+    fetch(b0);
     put(0);
   }
   __syncthreads();
   int buf = 0;
   for (int64_t b = b0; b < b1; ++b, buf ^= 1) {
-    if (b + 1 < b1) fetch((b + 1) * FK);
+    if (b + 1 < b1) fetch(b + 1);
 #pragma unroll
-    for (int kk = 0; kk < FK; ++kk) {
-      const float* ka = sa + (buf * FK + kk) * L::kPadM + ty * (RM / 2);
-      const float* kb = sb + (buf * FK + kk) * L::kPadN + tx * (RN / 2);
-      alignas(16) float a[RM];
-      alignas(16) uint64_t bv[RN / 2];
+    for (int kk = 0; kk < FK / G; ++kk) {
+      const float* ka = sa + (buf * FK + group * (FK / G) + kk) * L::kPadM + ty * (RM / 2);
+      const float* kb = sb + (buf * FK + group * (FK / G) + kk) * L::kPadN + tx * (RN / 2);
       static_assert(RM == 8, "rows in two groups of four");
-      *reinterpret_cast<float4*>(a) = *reinterpret_cast<const float4*>(ka);
-      *reinterpret_cast<float4*>(a + 4) = *reinterpret_cast<const float4*>(ka + TM / 2);
+      alignas(16) uint64_t av[RM / 2];
+      alignas(16) float bv[RN];
+      *reinterpret_cast<float4*>(av) = *reinterpret_cast<const float4*>(ka);
+      *reinterpret_cast<float4*>(av + 2) = *reinterpret_cast<const float4*>(ka + TM / 2);
       if constexpr (RN == 8) {
         *reinterpret_cast<float4*>(bv) = *reinterpret_cast<const float4*>(kb);
-        *reinterpret_cast<float4*>(bv + 2) = *reinterpret_cast<const float4*>(kb + TN / 2);
+        *reinterpret_cast<float4*>(bv + 4) = *reinterpret_cast<const float4*>(kb + TN / 2);
       } else {
-        bv[0] = *reinterpret_cast<const uint64_t*>(kb);
-        bv[1] = *reinterpret_cast<const uint64_t*>(kb + TN / 2);
+        *reinterpret_cast<float2*>(bv) = *reinterpret_cast<const float2*>(kb);
+        *reinterpret_cast<float2*>(bv + 2) = *reinterpret_cast<const float2*>(kb + TN / 2);
       }
 #pragma unroll
-      for (int i = 0; i < RM; ++i) {
-        const uint64_t av = pair_of(a[i]);
+      for (int j = 0; j < RN; ++j) {
+        const uint64_t b2 = pair_of(bv[j]);
 #pragma unroll
-        for (int j = 0; j < RN / 2; ++j) fma_pair(acc2[i][j], av, bv[j]);
+        for (int i = 0; i < RM / 2; ++i) fma_pair(acc2[i][j], av[i], b2);
       }
     }
     if (b + 1 < b1) put(buf ^ 1);
@@ -141,22 +184,42 @@ matmul_fma_kernel(const FmaArgs p, const int split) {
   }
   float acc[RM][RN];
 #pragma unroll
-  for (int i = 0; i < RM; ++i)
+  for (int i = 0; i < RM / 2; ++i)
 #pragma unroll
-    for (int j = 0; j < RN / 2; ++j)
-      asm("mov.b64 {%0, %1}, %2;" : "=f"(acc[i][2 * j]), "=f"(acc[i][2 * j + 1]) : "l"(acc2[i][j]));
-  int i0 = 0, i1 = RM;          // rows of acc this CTA finishes
-  if constexpr (TM <= 64) {
+    for (int j = 0; j < RN; ++j) asm("mov.b64 {%0, %1}, %2;" : "=f"(acc[2 * i][j]), "=f"(acc[2 * i + 1][j]) : "l"(acc2[i][j]));
+  int i0 = 0, i1 = RM;          // rows of acc this thread finishes
+  if constexpr (G == 2) {
+    // each group finishes half of the rows and gives its sums of the others away
+    constexpr int H = RM / 2;
+#pragma unroll
+    for (int i = 0; i < H; ++i)
+#pragma unroll
+      for (int j = 0; j < RN; ++j)
+        smem[((i * RN + j) * 2 + group) * kGroup + in_group] = group ? acc[i][j] : acc[i + H][j];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < H; ++i)
+#pragma unroll
+      for (int j = 0; j < RN; ++j) {
+        const float other = smem[((i * RN + j) * 2 + (group ^ 1)) * kGroup + in_group];
+        if (group) acc[i + H][j] += other;
+        else acc[i][j] += other;
+      }
+    i0 = group * H;
+    i1 = i0 + H;
     if (split > 1) {
       // sums by (row, column) of the thread, then by thread
+      __syncthreads();
 #pragma unroll
-      for (int i = 0; i < RM; ++i)
+      for (int i = 0; i < RM; ++i) {
+        if (i < i0 || i >= i1) continue;
 #pragma unroll
-        for (int j = 0; j < RN; ++j) smem[(i * RN + j) * kThreads + threadIdx.x] = acc[i][j];
+        for (int j = 0; j < RN; ++j) smem[(i * RN + j) * kGroup + in_group] = acc[i][j];
+      }
       asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-      i0 = part * RM / split;
-      i1 = (part + 1) * RM / split;
-      const uint32_t own = (uint32_t)__cvta_generic_to_shared(smem + threadIdx.x);
+      i1 = i0 + (part + 1) * H / split;
+      i0 += part * H / split;
+      const uint32_t own = (uint32_t)__cvta_generic_to_shared(smem + in_group);
 #pragma unroll
       for (int i = 0; i < RM; ++i) {
         if (i < i0 || i >= i1) continue;
@@ -168,7 +231,7 @@ matmul_fma_kernel(const FmaArgs p, const int split) {
 #pragma unroll
           for (int j = 0; j < RN; ++j) {
             float v;
-            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at + (uint32_t)((i * RN + j) * kThreads * 4)));
+            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at + (uint32_t)((i * RN + j) * kGroup * 4)));
             acc[i][j] += v;
           }
         }
@@ -208,25 +271,29 @@ matmul_fma_kernel(const FmaArgs p, const int split) {
       }
     }
   }
+  if (p.beside) pdl_wait();
 }
 
-template <typename T, int TILE, int RN, bool A_MN, bool B_MN, int EPI>
+template <typename T, int TILE, int RN, int WIDTH, bool A_MN, bool B_MN, int EPI>
 cudaError_t matmul_fma_t(const FmaArgs& p, int split, cudaStream_t s) {
   const int64_t cols = EPI == EPI_GATE ? TILE / 2 : TILE;
   const int64_t gx = (p.M + TILE - 1) / TILE * split, gy = (p.N + cols - 1) / cols;
   if (gx > 0x7fffffff || gy > 65535) return cudaErrorInvalidValue;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)gx, (unsigned)gy);
-  cfg.blockDim = dim3((TILE / 8) * (TILE / RN));
+  constexpr int G = TILE == 64 ? 2 : 1;
+  cfg.blockDim = dim3(G * (TILE / 8) * (TILE / RN));
   cfg.stream = s;
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = split;
-  attr.val.clusterDim.y = 1;
-  attr.val.clusterDim.z = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = split > 1 ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, matmul_fma_kernel<T, TILE, TILE, 8, RN, A_MN, B_MN, EPI>, p, split);
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = split;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = split > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, matmul_fma_kernel<T, TILE, TILE, 8, RN, G, WIDTH, A_MN, B_MN, EPI>, p, split);
 }
 // 128 x 128 tiles where they fill the SMs, else 64 x 64, and as many CTAs per tile as fill the SMs twice and leave each at least
 // 4 blocks of the contraction.
@@ -234,11 +301,15 @@ template <bool A_MN, bool B_MN, int EPI>
 cudaError_t matmul_fma(int dtype, const FmaArgs& p, cudaStream_t s) {
   const int64_t n = EPI == EPI_GATE ? 2 * p.N : p.N;
   const int64_t large = ((p.M + 127) / 128) * ((n + 127) / 128), small = ((p.M + 63) / 64) * ((n + 63) / 64);
-  if (large >= 148 && dtype == EPD_DTYPE_F32) return matmul_fma_t<float, 128, 8, A_MN, B_MN, EPI>(p, 1, s);
+  // 16-byte loads: where every row of both operands, and the end of what lies contiguous in them, allows
+  const bool wide = dtype == EPD_DTYPE_F32 && (((uintptr_t)p.a | (uintptr_t)p.b) & 15) == 0 && p.lda % 4 == 0 && p.ldb % 4 == 0 &&
+                    (A_MN ? p.M : p.K) % 4 == 0 && (B_MN ? p.N : p.K) % 4 == 0;
+  if (large >= 148 && dtype == EPD_DTYPE_F32)
+    return wide ? matmul_fma_t<float, 128, 8, 4, A_MN, B_MN, EPI>(p, 1, s) : matmul_fma_t<float, 128, 8, 1, A_MN, B_MN, EPI>(p, 1, s);
   int split = 1;
   while (split < 8 && small * split * 2 <= 2 * 148 && (p.K + FK - 1) / FK >= 8 * split) split *= 2;
-  return dtype == EPD_DTYPE_F32 ? matmul_fma_t<float, 64, 4, A_MN, B_MN, EPI>(p, split, s)
-                                : matmul_fma_t<__nv_bfloat16, 64, 4, A_MN, B_MN, EPI>(p, split, s);
+  if (dtype == EPD_DTYPE_BF16) return matmul_fma_t<__nv_bfloat16, 64, 4, 1, A_MN, B_MN, EPI>(p, split, s);
+  return wide ? matmul_fma_t<float, 64, 4, 4, A_MN, B_MN, EPI>(p, split, s) : matmul_fma_t<float, 64, 4, 1, A_MN, B_MN, EPI>(p, split, s);
 }
 
 // =============================================================================================
@@ -465,7 +536,7 @@ cudaError_t gated_linear(int dtype, const void* x, int64_t ldx, const void* w, i
 }
 
 // dpre[M, 2N] from dout[M, D], w_out[D, N] and pre[M, 2N]; its column sums in groups of rows into part (NULL: not formed),
-// the number of groups into *groups.
+// the number of groups into *groups: 0 where the few rows of dpre are to be added up directly.
 cudaError_t gate_gradient(int dtype, const void* dout, int64_t lddo, const void* w_out, int64_t ldw, const void* pre,
                           int64_t ldp, void* dpre, int64_t lddp, float* part, int64_t* groups, int64_t M, int64_t N,
                           int64_t D, int gate, cudaStream_t s) {
@@ -481,8 +552,8 @@ cudaError_t gate_gradient(int dtype, const void* dout, int64_t lddo, const void*
   p.M = M; p.N = N; p.K = D;
   p.gate = gate;
   const cudaError_t e = matmul_fma<false, true, EPI_GATE_GRAD>(dtype, p, s);
-  *groups = sum_groups(M);
-  return e != cudaSuccess || !part ? e : column_sum_partial(dtype, dpre, lddp, M, 2 * N, part, s);
+  *groups = M <= kDirectRows ? 0 : sum_groups(M);
+  return e != cudaSuccess || !part || *groups == 0 ? e : column_sum_partial(dtype, dpre, lddp, M, 2 * N, part, s);
 }
 
 // dx[M, K] = dout[M, N] . w[N, K]
@@ -507,7 +578,7 @@ ProductArg weight_gradient(const Planes& dout, const Planes& x, void* dw, int64_
 // The products of the list (those with an output): together on the tensor cores where they can take them, else on FMAs.
 cudaError_t products(int dtype, std::initializer_list<ProductArg> list, cudaStream_t s) {
   ProductArg tc[3];
-  int n = 0;
+  int n = 0, fma = 0;
   for (const ProductArg& a : list) {
     // what lies contiguous in memory comes in pieces of 8: A's rows or its contraction, and the columns
     if (dtype == EPD_DTYPE_BF16 &&
@@ -521,6 +592,7 @@ cudaError_t products(int dtype, std::initializer_list<ProductArg> list, cudaStre
     p.b = a.b; p.ldb = a.ldb;
     p.out = a.out; p.ldo = a.ldo;
     p.M = a.M; p.N = a.N; p.K = a.K;
+    p.beside = fma++ > 0;      // the products do not depend on one another
     const cudaError_t e = a.a_mn ? matmul_fma<true, true, EPI_PLAIN>(dtype, p, s) : matmul_fma<false, true, EPI_PLAIN>(dtype, p, s);
     if (e != cudaSuccess) return e;
   }
@@ -685,12 +757,13 @@ int epd_op_gated_mlp_backward(int32_t dtype, const void* dout, int64_t lddo, con
     EPD_TRY(column_sum_partial(dtype, dout, lddo, M, D, part_out, s));
     sum_out = FinalSum{part_out, sum_groups(M), D, db_out};
   }
+  const void* dpre_rows = nullptr;     // added up directly
   // what is left of the bias gradients once their parts and the products are on the stream
   auto bias_sums = [&]() -> cudaError_t {
-    if (db_out && direct) {
-      const cudaError_t e = column_sum_direct(dtype, dout, lddo, M, D, db_out, beside, s);
-      if (e != cudaSuccess) return e;
-    }
+    cudaError_t e = cudaSuccess;
+    if (dpre_rows) e = column_sum_direct(dtype, dpre_rows, 2 * N, M, 2 * N, db_in, beside, s);
+    if (e == cudaSuccess && db_out && direct) e = column_sum_direct(dtype, dout, lddo, M, D, db_out, beside, s);
+    if (e != cudaSuccess) return e;
     return column_sum_final(dtype, sum_in, sum_out, beside, s);
   };
   int64_t groups = 0;
@@ -717,7 +790,8 @@ int epd_op_gated_mlp_backward(int32_t dtype, const void* dout, int64_t lddo, con
   if (inner) {
     EPD_TRY(gate_gradient(dtype, dout, lddo, w_out, ldw_out, pre, ldp, dpre, 2 * N, db_in ? part_in : nullptr, &groups, M, N,
                           D, gate, s));
-    if (db_in) sum_in = FinalSum{part_in, groups, 2 * N, db_in};
+    if (db_in && groups > 0) sum_in = FinalSum{part_in, groups, 2 * N, db_in};
+    else if (db_in) dpre_rows = dpre;
   }
   EPD_TRY(products(dtype,
                    {input_gradient(dpre, 2 * N, w_in, ldw_in, dx, lddx, M, 2 * N, K),

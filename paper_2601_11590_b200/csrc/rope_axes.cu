@@ -164,10 +164,10 @@ __device__ __forceinline__ void pack2(__nv_bfloat16* p, float2 v) {
   *reinterpret_cast<__nv_bfloat162*>(p) = __floats2bfloat162_rn(v.x, v.y);
 }
 
-// The same through shared memory: a block brings the rows of a few tokens in with 16-byte asynchronous copies, turns
-// them in place, and sends them out: a token's row in one bulk copy, other rows in 16-byte stores.  Global memory sees whole 16-byte pieces in both directions whatever the sections, where the
-// kernel above reads and writes runs of U elements.  What is not rotated (v) passes through without a thread touching it.
-// A thread keeps its token and PW pairs of the head, so their cosines and sines sit in its registers for all heads.  HBM bound:
+// The same through shared memory: a block brings the rows of a few tokens in with 16-byte asynchronous copies, turns them in
+// place, and sends them out: a token's row in one bulk copy, other rows in 16-byte stores.  Global memory sees whole 16-byte
+// pieces in both directions whatever the sections, where the kernel above reads and writes runs of U elements.  A thread keeps
+// its token and PW pairs of the head, so their cosines and sines sit in its registers for all heads.  HBM bound:
 // bf16 81628 tokens of 16 heads x 72 with sections of 12, split 204 us (5.8 TB/s; 556 us in the kernel above), its gradient
 // 188 us (6.0), the rotation alone 125 us; heads of 128 6.2, float 6.4 to 6.7 TB/s.
 constexpr int kStagedThreads = 288;       // 32 rows of nine 16-byte pieces
