@@ -272,4 +272,120 @@ cudaError_t linear_few_rows(const void* x, int64_t ldx, const void* w, int64_t l
   return launch_linear(p, s);
 }
 
+// ---- float ----------------------------------------------------------------------------------
+// Plain multiply-adds, bound by reading the weights once as well.  A warp has four weight rows (gated: the gate and up rows of
+// two columns); its lanes take every 32nd 16-byte piece of the contraction, of which 1, 2, 4 or 8 warps of the block have a
+// share each, and the lanes' sums are added by shuffles, the warps' in shared memory, always in the same order.
+// One token of a 1152 x 4304 block 91 -> 21 us (the plain-FMA tiles compute 64 rows whatever there is), 16 tokens 92 -> 46.
+namespace {
+
+constexpr int kRowsF32 = 4;
+
+struct FewRowsF32 {
+  const float *x, *w, *bias;
+  int64_t ldx, ldw;
+  int M, N, K;
+  float *out, *pre;
+  int64_t ldo, ldp;
+  int gate, accumulate;
+  int shares;               // warps that share a contraction
+};
+
+template <int TOKENS, bool GATED>
+__global__ void __launch_bounds__(32 * kWarps) few_rows_f32_kernel(const FewRowsF32 p) {
+  pdl_wait();
+  pdl_launch_dependents();
+  constexpr int COLS = GATED ? kRowsF32 / 2 : kRowsF32;      // output columns of a warp's rows
+  __shared__ float part[kWarps][kRowsF32][TOKENS];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int share = warp % p.shares, groups = kWarps / p.shares;
+  const int64_t n0 = ((int64_t)blockIdx.x * groups + warp / p.shares) * COLS;
+  const float* w[kRowsF32];
+#pragma unroll
+  for (int r = 0; r < kRowsF32; ++r) {
+    const int64_t n = min(n0 + r % COLS, (int64_t)p.N - 1);
+    w[r] = p.w + (GATED && r >= COLS ? p.N + n : n) * p.ldw;
+  }
+  const float* x[TOKENS];
+#pragma unroll
+  for (int m = 0; m < TOKENS; ++m) x[m] = p.x + (m < p.M ? m : 0) * p.ldx;
+  float acc[kRowsF32][TOKENS] = {};
+  const int step = 128 * p.shares;
+#pragma unroll (TOKENS <= 8 ? 2 : 1)
+  for (int k = 128 * share + 4 * lane; k < p.K; k += step) {
+    float4 a[kRowsF32];
+#pragma unroll
+    for (int r = 0; r < kRowsF32; ++r) a[r] = __ldcs(reinterpret_cast<const float4*>(w[r] + k));
+#pragma unroll
+    for (int m = 0; m < TOKENS; ++m) {
+      const float4 b = *reinterpret_cast<const float4*>(x[m] + k);
+#pragma unroll
+      for (int r = 0; r < kRowsF32; ++r)
+        acc[r][m] = fmaf(a[r].x, b.x, fmaf(a[r].y, b.y, fmaf(a[r].z, b.z, fmaf(a[r].w, b.w, acc[r][m]))));
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < kRowsF32; ++r)
+#pragma unroll
+    for (int m = 0; m < TOKENS; ++m) {
+      float v = acc[r][m];
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+      if (lane == 0) part[warp][r][m] = v;
+    }
+  __syncthreads();
+  for (int i = threadIdx.x; i < groups * COLS * TOKENS; i += 32 * kWarps) {
+    const int c = i % COLS, m = i / COLS % TOKENS, group = i / (COLS * TOKENS);
+    const int64_t n = ((int64_t)blockIdx.x * groups + group) * COLS + c;
+    if (m >= p.M || n >= p.N) continue;
+    float s = 0.0f, u = 0.0f;
+    for (int k = 0; k < p.shares; ++k) {
+      s += part[group * p.shares + k][c][m];
+      if (GATED) u += part[group * p.shares + k][COLS + c][m];
+    }
+    if (p.bias) s += p.bias[n];
+    if constexpr (GATED) {
+      if (p.bias) u += p.bias[p.N + n];
+      p.out[m * p.ldo + n] = gate_act(p.gate, s) * u;
+      if (p.pre) {
+        p.pre[m * p.ldp + n] = s;
+        p.pre[m * p.ldp + p.N + n] = u;
+      }
+    } else {
+      float* o = p.out + m * p.ldo + n;
+      *o = p.accumulate ? *o + s : s;
+    }
+  }
+}
+
+template <bool GATED>
+cudaError_t launch_f32(FewRowsF32& p, cudaStream_t s) {
+  // as many warps to a contraction as fill the SMs twice, each with a whole step at least
+  const int64_t warps = (p.N + (GATED ? 1 : 3)) / (GATED ? 2 : 4);
+  p.shares = 1;
+  while (p.shares < kWarps && warps * p.shares < 2 * 148 * kWarps && p.K >= 256 * p.shares) p.shares *= 2;
+  const int64_t blocks = (warps * p.shares + kWarps - 1) / kWarps;
+  const dim3 grid((unsigned)blocks), block(32 * kWarps);
+  if (p.M == 1) return launch_pdl(few_rows_f32_kernel<1, GATED>, grid, block, 0, s, p);
+  if (p.M <= 4) return launch_pdl(few_rows_f32_kernel<4, GATED>, grid, block, 0, s, p);
+  if (p.M <= 8) return launch_pdl(few_rows_f32_kernel<8, GATED>, grid, block, 0, s, p);
+  return launch_pdl(few_rows_f32_kernel<16, GATED>, grid, block, 0, s, p);
+}
+
+}  // namespace
+
+cudaError_t few_rows_float(const void* x, int64_t ldx, const void* w, int64_t ldw, const void* bias, void* out, int64_t ldo,
+                           void* pre, int64_t ldp, int64_t M, int64_t N, int64_t K, int gate, bool accumulate, cudaStream_t s) {
+  FewRowsF32 p = {};
+  p.x = static_cast<const float*>(x); p.ldx = ldx;
+  p.w = static_cast<const float*>(w); p.ldw = ldw;
+  p.bias = static_cast<const float*>(bias);
+  p.M = (int)M; p.N = (int)N; p.K = (int)K;
+  p.out = static_cast<float*>(out); p.ldo = ldo;
+  p.pre = static_cast<float*>(pre); p.ldp = ldp;
+  p.gate = gate;
+  p.accumulate = accumulate;
+  return gate >= 0 ? launch_f32<true>(p, s) : launch_f32<false>(p, s);
+}
+
 }  // namespace epd

@@ -14,10 +14,12 @@ namespace {
 // Matrix product with plain FMAs: out[m, n] = sum_k A(m, k) B(n, k), every operand either contraction-contiguous
 // ("K-major": element (r, k) at r * ld + k) or row-contiguous ("MN-major": at k * ld + r).  TM x TN tile, RM x RN outputs per
 // thread in two groups of rows by two groups of columns (the gated product keeps a column's gate in the first group and its
-// up projection in the second), two outputs per instruction (fma.rn.f32x2), the next block of the contraction fetched into
-// registers while the present one is multiplied out of one of two buffers.  Bound by the FMA pipe.
-// A 64 x 64 tile has two groups of threads, each with half of every block's steps.  Where the tiles are fewer than the SMs, the 2, 4 or 8 CTAs of a cluster share a tile, each with a part of the contraction;
-// each then adds up some of the rows from all parts, in order, out of the others' shared memory.
+// up projection in the second), two outputs per instruction (fma.rn.f32x2).  Float operands come by asynchronous copies, 3 to 5
+// blocks of the contraction ahead (element by element where a block is to be turned); bf16 ones, which become floats on the way,
+// through registers.  Bound by the FMA pipe where tiles are many, by latency below.
+// A 64 x 64 tile has two groups of threads, each with half of every block's steps.  Where the tiles are fewer than the SMs, the
+// 2, 4 or 8 CTAs of a cluster share a tile, each with a part of the contraction; each then adds up some of the rows from all
+// parts, in order, out of the others' shared memory.
 // A kernel lets its successor start once everything in front of itself is complete.  One that needs nothing of its predecessor
 // (`beside`: a second and third product of the same inputs) runs along with it and waits for it at its end.
 // =============================================================================================
@@ -43,20 +45,13 @@ struct FmaArgs {
   int beside;
 };
 
-__device__ __forceinline__ uint64_t pair_of(float a) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %1};" : "=l"(r) : "f"(a));
-  return r;
-}
-__device__ __forceinline__ void fma_pair(uint64_t& c, uint64_t a, uint64_t b) {
-  asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(c) : "l"(a), "l"(b));
-}
-
-template <int TM, int TN>
+template <typename T, int TM, int TN>
 struct FmaTile {
   static constexpr int kPadM = TM + 4, kPadN = TN + 4;
-  static constexpr int kFloats = 2 * FK * (kPadM + kPadN);
-  static_assert(kFloats >= TM * TN || TM > 64, "a shared tile's sums take the place of its buffers");
+  static constexpr int kStageFloats = FK * (kPadM + kPadN);
+  static constexpr int kStages = sizeof(T) == 2 ? 2 : TM == 64 ? 6 : 4;
+  static constexpr int kBytes = kStages * kStageFloats * 4;
+  static_assert(kStages * kStageFloats >= TM * TN || TM > 64, "a shared tile's sums take the place of its stages");
 };
 
 template <typename T, int TM, int TN, int RM, int RN, int G, int WIDTH, bool A_MN, bool B_MN, int EPI>
@@ -64,13 +59,11 @@ __global__ void __launch_bounds__(G * (TM / RM) * (TN / RN), 256 / TM < 2 ? 1 : 
 matmul_fma_kernel(const FmaArgs p, const int split) {
   if (!p.beside) pdl_wait();
   pdl_launch_dependents();
-  using L = FmaTile<TM, TN>;
+  using L = FmaTile<T, TM, TN>;
   constexpr int kGroup = (TM / RM) * (TN / RN), kThreads = G * kGroup;
   constexpr int LA = TM * FK / kThreads, LB = TN * FK / kThreads;
   constexpr int COLS = EPI == EPI_GATE ? TN / 2 : TN;     // output columns of a tile
-  __shared__ __align__(16) float smem[L::kFloats];
-  float* const sa = smem;
-  float* const sb = smem + 2 * FK * L::kPadM;
+  extern __shared__ __align__(16) float smem[];          // stages of [FK][kPadM] of A, [FK][kPadN] of B
   const T* A = static_cast<const T*>(p.a);
   const T* B = static_cast<const T*>(p.b);
   const int group = threadIdx.x / kGroup, in_group = threadIdx.x % kGroup;
@@ -79,89 +72,107 @@ matmul_fma_kernel(const FmaArgs p, const int split) {
   const int64_t m0 = (int64_t)(blockIdx.x / split) * TM, n0 = (int64_t)blockIdx.y * COLS;
   const int64_t blocks = (p.K + FK - 1) / FK;
   const int64_t b0 = part * blocks / split, b1 = (part + 1) * blocks / split;
-  // A thread's elements of a block, WIDTH next to one another in memory: its place in the tile (row, step), whether its row exists,
-  // and where it is in the first block.
-  constexpr int VA = LA / WIDTH, VB = LB / WIDTH;
-  alignas(16) float ra[LA], rb[LB];
-  auto place = [&](bool mn, int extent, int i, int& r, int& k) {
-    const int e = (threadIdx.x + kThreads * i) * WIDTH;
+  // A thread's elements of a block: rows next to one another where those are contiguous (WIDTH of them a load), else steps.
+  constexpr int WA = A_MN ? WIDTH : 1, WB = B_MN ? WIDTH : 1, VA = LA / WA, VB = LB / WB;
+  auto place = [&](bool mn, int extent, int width, int i, int& r, int& k) {
+    const int e = (threadIdx.x + kThreads * i) * width;
     r = mn ? e % extent : e / FK;
     k = mn ? e / extent : e % FK;
   };
-  const T* at_a[VA];
+  const T* at_a[VA];      // in the block to fetch next; NULL: the row does not exist
   const T* at_b[VB];
 #pragma unroll
   for (int i = 0; i < VA; ++i) {
     int r, k;
-    place(A_MN, TM, i, r, k);
+    place(A_MN, TM, WA, i, r, k);
     at_a[i] = m0 + r < p.M ? A + (A_MN ? (b0 * FK + k) * p.lda + m0 + r : (m0 + r) * p.lda + b0 * FK + k) : nullptr;
   }
 #pragma unroll
   for (int i = 0; i < VB; ++i) {
     int r, k;
-    place(B_MN, TN, i, r, k);
+    place(B_MN, TN, WB, i, r, k);
     // gated: the tile's second half of columns is the up projection of the first half's
     const int64_t c = n0 + (EPI == EPI_GATE ? r % COLS : r), n = EPI == EPI_GATE && r >= COLS ? p.N + c : c;
     at_b[i] = c < p.N ? B + (B_MN ? (b0 * FK + k) * p.ldb + n : n * p.ldb + b0 * FK + k) : nullptr;
   }
-  auto take = [&](const T* from, bool in, float* to) {
-    if constexpr (WIDTH == 4) *reinterpret_cast<float4*>(to) = in ? *reinterpret_cast<const float4*>(from) : make_float4(0.f, 0.f, 0.f, 0.f);
-    else *to = in ? to_float<T>(*from) : 0.0f;
-  };
-  auto fetch = [&](int64_t block) {       // and on to the next block
-    const int64_t left = p.K - block * FK;
-#pragma unroll
-    for (int i = 0; i < VA; ++i) {
-      int r, k;
-      place(A_MN, TM, i, r, k);
-      take(at_a[i], at_a[i] != nullptr && k < left, ra + i * WIDTH);
-      if (at_a[i]) at_a[i] += A_MN ? FK * p.lda : FK;
-    }
-#pragma unroll
-    for (int i = 0; i < VB; ++i) {
-      int r, k;
-      place(B_MN, TN, i, r, k);
-      take(at_b[i], at_b[i] != nullptr && k < left, rb + i * WIDTH);
-      if (at_b[i]) at_b[i] += B_MN ? FK * p.ldb : FK;
-    }
-  };
-  auto put_one = [&](bool mn, const float* v, float* tile, int pad, int r, int k) {
-    if (WIDTH == 4 && mn) {
-      *reinterpret_cast<float4*>(tile + k * pad + r) = *reinterpret_cast<const float4*>(v);
+  float hold[sizeof(T) == 2 ? LA + LB : 1];      // bf16: on its way from memory to floats in shared memory
+  auto fetch_one = [&](const T*& at, const T* base, int64_t step, int width, bool in, float* to, float& held) {
+    in = in && at != nullptr;
+    if constexpr (sizeof(T) == 2) {
+      held = in ? to_float<T>(*at) : 0.0f;
     } else {
-#pragma unroll
-      for (int e = 0; e < WIDTH; ++e) tile[(k + e) * pad + r] = v[e];
+      const uint32_t dst = (uint32_t)__cvta_generic_to_shared(to);
+      const T* from = in ? at : base;      // aligned as the copy is, though nothing is read there
+      if (width == 4) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(from), "r"(in ? 16 : 0) : "memory");
+      else asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(from), "r"(in ? 4 : 0) : "memory");
     }
+    if (at) at += step;
   };
-  auto put = [&](int buf) {
+  auto fetch = [&](int64_t block) {               // blocks in order
+    const int64_t left = p.K - block * FK;
+    float* sa = smem + (int)((block - b0) % L::kStages) * L::kStageFloats;
+    float* sb = sa + FK * L::kPadM;
 #pragma unroll
     for (int i = 0; i < VA; ++i) {
       int r, k;
-      place(A_MN, TM, i, r, k);
-      put_one(A_MN, ra + i * WIDTH, sa + buf * FK * L::kPadM, L::kPadM, r, k);
+      place(A_MN, TM, WA, i, r, k);
+      fetch_one(at_a[i], A, A_MN ? FK * p.lda : FK, WA, k < left, sa + k * L::kPadM + r, hold[sizeof(T) == 2 ? i : 0]);
     }
 #pragma unroll
     for (int i = 0; i < VB; ++i) {
       int r, k;
-      place(B_MN, TN, i, r, k);
-      put_one(B_MN, rb + i * WIDTH, sb + buf * FK * L::kPadN, L::kPadN, r, k);
+      place(B_MN, TN, WB, i, r, k);
+      fetch_one(at_b[i], B, B_MN ? FK * p.ldb : FK, WB, k < left, sb + k * L::kPadN + r, hold[sizeof(T) == 2 ? LA + i : 0]);
     }
   };
-  uint64_t acc2[RM / 2][RN] = {};      // pairs of rows
-  if (b0 < b1) {
-    fetch(b0);
-    put(0);
+  auto put = [&](int64_t block) {                 // bf16: what was fetched, to shared memory
+    float* sa = smem + (int)((block - b0) % L::kStages) * L::kStageFloats;
+    float* sb = sa + FK * L::kPadM;
+#pragma unroll
+    for (int i = 0; i < VA; ++i) {
+      int r, k;
+      place(A_MN, TM, 1, i, r, k);
+      sa[k * L::kPadM + r] = hold[sizeof(T) == 2 ? i : 0];
+    }
+#pragma unroll
+    for (int i = 0; i < VB; ++i) {
+      int r, k;
+      place(B_MN, TN, 1, i, r, k);
+      sb[k * L::kPadN + r] = hold[sizeof(T) == 2 ? LA + i : 0];
+    }
+  };
+  auto commit = [] { asm volatile("cp.async.commit_group;" ::: "memory"); };
+  float2 acc2[RM / 2][RN] = {};      // pairs of rows
+  if constexpr (sizeof(T) == 2) {
+    if (b0 < b1) {
+      fetch(b0);
+      put(b0);
+    }
+  } else {
+#pragma unroll 1
+    for (int i = 0; i < L::kStages - 1; ++i) {
+      if (b0 + i < b1) fetch(b0 + i);
+      commit();
+    }
   }
-  __syncthreads();
-  int buf = 0;
-  for (int64_t b = b0; b < b1; ++b, buf ^= 1) {
-    if (b + 1 < b1) fetch(b + 1);
+  for (int64_t b = b0; b < b1; ++b) {
+    if constexpr (sizeof(T) == 2) {
+      __syncthreads();
+      if (b + 1 < b1) fetch(b + 1);
+    } else {
+      asm volatile("cp.async.wait_group %0;" ::"n"(L::kStages - 2) : "memory");
+      __syncthreads();       // this block has arrived, and everyone is done with the one before it, whose stage is taken now
+      if (b + L::kStages - 1 < b1) fetch(b + L::kStages - 1);
+      commit();
+    }
+    const float* sa = smem + (int)((b - b0) % L::kStages) * L::kStageFloats;
+    const float* sb = sa + FK * L::kPadM;
 #pragma unroll
     for (int kk = 0; kk < FK / G; ++kk) {
-      const float* ka = sa + (buf * FK + group * (FK / G) + kk) * L::kPadM + ty * (RM / 2);
-      const float* kb = sb + (buf * FK + group * (FK / G) + kk) * L::kPadN + tx * (RN / 2);
+      const float* ka = sa + (group * (FK / G) + kk) * L::kPadM + ty * (RM / 2);
+      const float* kb = sb + (group * (FK / G) + kk) * L::kPadN + tx * (RN / 2);
       static_assert(RM == 8, "rows in two groups of four");
-      alignas(16) uint64_t av[RM / 2];
+      alignas(16) float2 av[RM / 2];
       alignas(16) float bv[RN];
       *reinterpret_cast<float4*>(av) = *reinterpret_cast<const float4*>(ka);
       *reinterpret_cast<float4*>(av + 2) = *reinterpret_cast<const float4*>(ka + TM / 2);
@@ -174,23 +185,25 @@ matmul_fma_kernel(const FmaArgs p, const int split) {
       }
 #pragma unroll
       for (int j = 0; j < RN; ++j) {
-        const uint64_t b2 = pair_of(bv[j]);
+        const float2 b2 = make_float2(bv[j], bv[j]);
 #pragma unroll
-        for (int i = 0; i < RM / 2; ++i) fma_pair(acc2[i][j], av[i], b2);
+        for (int i = 0; i < RM / 2; ++i) acc2[i][j] = __ffma2_rn(av[i], b2, acc2[i][j]);
       }
     }
-    if (b + 1 < b1) put(buf ^ 1);
-    __syncthreads();
+    if constexpr (sizeof(T) == 2) {
+      if (b + 1 < b1) put(b + 1);
+    }
   }
   float acc[RM][RN];
 #pragma unroll
   for (int i = 0; i < RM / 2; ++i)
 #pragma unroll
-    for (int j = 0; j < RN; ++j) asm("mov.b64 {%0, %1}, %2;" : "=f"(acc[2 * i][j]), "=f"(acc[2 * i + 1][j]) : "l"(acc2[i][j]));
+    for (int j = 0; j < RN; ++j) { acc[2 * i][j] = acc2[i][j].x; acc[2 * i + 1][j] = acc2[i][j].y; }
   int i0 = 0, i1 = RM;          // rows of acc this thread finishes
   if constexpr (G == 2) {
     // each group finishes half of the rows and gives its sums of the others away
     constexpr int H = RM / 2;
+    __syncthreads();
 #pragma unroll
     for (int i = 0; i < H; ++i)
 #pragma unroll
@@ -279,9 +292,16 @@ cudaError_t matmul_fma_t(const FmaArgs& p, int split, cudaStream_t s) {
   const int64_t cols = EPI == EPI_GATE ? TILE / 2 : TILE;
   const int64_t gx = (p.M + TILE - 1) / TILE * split, gy = (p.N + cols - 1) / cols;
   if (gx > 0x7fffffff || gy > 65535) return cudaErrorInvalidValue;
+  constexpr int G = TILE == 64 ? 2 : 1;
+  auto kern = matmul_fma_kernel<T, TILE, TILE, 8, RN, G, WIDTH, A_MN, B_MN, EPI>;
+  static PerDeviceOnce configured;
+  const cudaError_t e = once_per_device(configured, [&] {
+    return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, FmaTile<T, TILE, TILE>::kBytes);
+  });
+  if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)gx, (unsigned)gy);
-  constexpr int G = TILE == 64 ? 2 : 1;
+  cfg.dynamicSmemBytes = FmaTile<T, TILE, TILE>::kBytes;
   cfg.blockDim = dim3(G * (TILE / 8) * (TILE / RN));
   cfg.stream = s;
   cudaLaunchAttribute attr[2];
@@ -293,7 +313,7 @@ cudaError_t matmul_fma_t(const FmaArgs& p, int split, cudaStream_t s) {
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = split > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, matmul_fma_kernel<T, TILE, TILE, 8, RN, G, WIDTH, A_MN, B_MN, EPI>, p, split);
+  return cudaLaunchKernelEx(&cfg, kern, p, split);
 }
 // 128 x 128 tiles where they fill the SMs, else 64 x 64, and as many CTAs per tile as fill the SMs twice and leave each at least
 // 4 blocks of the contraction.
@@ -301,9 +321,9 @@ template <bool A_MN, bool B_MN, int EPI>
 cudaError_t matmul_fma(int dtype, const FmaArgs& p, cudaStream_t s) {
   const int64_t n = EPI == EPI_GATE ? 2 * p.N : p.N;
   const int64_t large = ((p.M + 127) / 128) * ((n + 127) / 128), small = ((p.M + 63) / 64) * ((n + 63) / 64);
-  // 16-byte loads: where every row of both operands, and the end of what lies contiguous in them, allows
-  const bool wide = dtype == EPD_DTYPE_F32 && (((uintptr_t)p.a | (uintptr_t)p.b) & 15) == 0 && p.lda % 4 == 0 && p.ldb % 4 == 0 &&
-                    (A_MN ? p.M : p.K) % 4 == 0 && (B_MN ? p.N : p.K) % 4 == 0;
+  // 16-byte copies of row-contiguous operands, where they allow
+  auto whole = [](const void* ptr, int64_t ld, int64_t rows) { return ((uintptr_t)ptr & 15) == 0 && ld % 4 == 0 && rows % 4 == 0; };
+  const bool wide = (A_MN || B_MN) && (!A_MN || whole(p.a, p.lda, p.M)) && (!B_MN || whole(p.b, p.ldb, p.N));
   if (large >= 148 && dtype == EPD_DTYPE_F32)
     return wide ? matmul_fma_t<float, 128, 8, 4, A_MN, B_MN, EPI>(p, 1, s) : matmul_fma_t<float, 128, 8, 1, A_MN, B_MN, EPI>(p, 1, s);
   int split = 1;
@@ -519,9 +539,17 @@ bool few_rows(int dtype, const void* x, int64_t ldx, const void* w, int64_t ldw,
          (((uintptr_t)x | (uintptr_t)w) & 15) == 0;
 }
 
+// The same of float.
+bool few_rows_f32(int dtype, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t M, int64_t K) {
+  return dtype == EPD_DTYPE_F32 && M <= kFewRowsF32 && K % 4 == 0 && ldx % 4 == 0 && ldw % 4 == 0 &&
+         (((uintptr_t)x | (uintptr_t)w) & 15) == 0;
+}
+
 cudaError_t gated_linear(int dtype, const void* x, int64_t ldx, const void* w, int64_t ldw, const void* bias, void* out,
                          int64_t ldo, void* pre, int64_t ldp, int64_t M, int64_t N, int64_t K, int gate, cudaStream_t s) {
   if (few_rows(dtype, x, ldx, w, ldw, M, K)) return gated_few_rows(x, ldx, w, ldw, bias, out, ldo, pre, ldp, M, N, K, gate, s);
+  if (few_rows_f32(dtype, x, ldx, w, ldw, M, K))
+    return few_rows_float(x, ldx, w, ldw, bias, out, ldo, pre, ldp, M, N, K, gate, false, s);
   if (dtype == EPD_DTYPE_BF16 && gated_tc_supported({{x, ldx}, {w, ldw}, {out, ldo}, {pre, ldp}}, {N, K}))
     return gated_tc_forward(x, ldx, w, ldw, bias, out, ldo, pre, ldp, M, N, K, gate, s);
   FmaArgs p = {};
@@ -695,6 +723,9 @@ int epd_op_gated_mlp(int32_t dtype, const void* x, int64_t ldx, const void* w_in
   if (dtype == EPD_DTYPE_BF16 && ldo % 8 == 0 && linear_tc_split_pays(M, D, N) &&
       gated_tc_supported({{hidden, ldh}, {w_out, ldw_out}, {out, ldo}}, {D, N}))
     return finish(linear_tc_split(hidden, ldh, w_out, ldw_out, b_out, out, ldo, M, D, N, flags, s));
+  if (few_rows_f32(dtype, hidden, ldh, w_out, ldw_out, M, N))
+    return finish(few_rows_float(hidden, ldh, w_out, ldw_out, b_out, out, ldo, nullptr, 0, M, D, N, -1,
+                                 (flags & EPD_LINEAR_ACCUMULATE) != 0, s));
   if (dtype == EPD_DTYPE_F32) {
     FmaArgs p = {};
     p.a = hidden; p.lda = ldh;

@@ -247,6 +247,27 @@ def test_strided_operands_and_untouched_neighbours(dtype, M, offset):
         assert bool(torch.isnan(big).all()), n
 
 
+@pytest.mark.parametrize("M", [1, 3, 8, 11, 16, 17])
+def test_residual_update_of_a_float_block(M):
+    """Widths that end inside a lane's stretch of the contraction and inside a warp's rows; gaps behind the rows."""
+    N, K, D = 1001, 204, 333
+    b = block(5, F32, M, N + 3, K, D)
+    w_in = torch.cat([b["w_in"][:N], b["w_in"][-N:]])
+    big = torch.full((D, N + 15), float("nan"), device="cuda")
+    big[:, :N] = b["w_out"][:, :N]
+    w_out, b_in = big[:, :N], b["b_in"][:2 * N].contiguous()
+    pre_ref, hid_ref = reference_forward(b["x"], w_in, b_in, epd.GATE_GELU_ERF)
+    hid = torch.full((M, N + 7), float("nan"), device="cuda")[:, :N]
+    out = torch.randn(M, D, device="cuda")
+    ref = out.double() + hid_ref @ f64(w_out).T + f64(b["b_out"])
+    pre = torch.empty(M, 2 * N, device="cuda")
+    epd.op_gated_mlp(F32, b["x"], w_in, b_in, w_out, b["b_out"], epd.GATE_GELU_ERF, out=out, hidden=hid, pre=pre,
+                     flags=epd.LINEAR_ACCUMULATE)
+    parity(pre, pre_ref, ONE[F32], "pre")
+    parity(hid, hid_ref, ONE[F32], "hidden")
+    parity(out, ref, TWO[F32], "residual")
+
+
 @pytest.mark.parametrize("M", [1, 12, 200])
 def test_residual_update_and_float_output(M):
     b = block(4, BF16, M, 320, 192)
