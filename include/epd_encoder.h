@@ -530,11 +530,11 @@ int epd_feature_cache_stats(const epd_feature_cache_t* cache, int64_t* hits, int
  * prefetch)
  * ---------------------------------------------------------------------------------------- */
 
-/* SM budget: the persistent kernels of this library (linear layers, attention) launch at most n_sms CTAs
- * (0 = every SM, the default), leaving the other SMs to kernels of a co-located stage on another stream or
- * in another process (no fewer than one cluster, of up to 8 CTAs where a linear layer shares its tiles).  Process-wide;
- * applies to launches made after the call.  Results do not depend on it (the same tiles are computed, by fewer CTAs).  The short non-persistent kernels (RMSNorm, patchify,
- * layout) are not limited. */
+/* SM budget: the persistent kernels of this library (linear layers, gated blocks and gradients in bf16, attention) launch at
+ * most n_sms CTAs (0 = every SM, the default; no fewer than one cluster, which is up to 8 CTAs where a gated block shares a
+ * tile), leaving the other SMs to kernels of a co-located stage on another stream or in another process.  Process-wide;
+ * applies to launches made after the call.  Results do not depend on it (the same tiles are computed, by fewer CTAs).  The
+ * non-persistent kernels (RMSNorm, patchify, layout, rotary steps, plain-FMA products) are not limited. */
 int epd_set_sm_limit(int32_t n_sms);
 int32_t epd_get_sm_limit(void);
 
