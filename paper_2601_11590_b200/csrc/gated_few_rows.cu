@@ -20,7 +20,11 @@ namespace {
 constexpr int kWarps = 8;
 constexpr int kChunk = 32;          // contraction steps of a warp's piece: 64 bytes of a row
 
-enum { KIND_GATED = 0, KIND_16 = 1, KIND_8 = 2 };     // a 16-row tile: 8 gate + 8 up rows; 16 rows; 8 rows and nothing
+// The 16 rows of a tile: 8 gate + 8 up rows; 16 rows; 8 rows and nothing; 16 in the first and 8 in the second of two tiles.
+enum { KIND_GATED = 0, KIND_16 = 1, KIND_8 = 2, KIND_24 = 3 };
+template <int KIND, int TILES> constexpr int kColumns = KIND == KIND_24 ? 24 : KIND == KIND_16 ? 16 * TILES : 8 * TILES;
+// Whether tile i has rows in its second half.
+__host__ __device__ constexpr bool whole_tile(int kind, int i) { return kind == KIND_24 ? i == 0 : kind != KIND_8; }
 
 struct FewRows {
   const __nv_bfloat16 *x, *w, *bias;
@@ -56,7 +60,7 @@ __device__ __forceinline__ uint4 load_slot(uint32_t slot) {
 // TILES 16-row tiles of weights and NT groups of 8 tokens to a step.
 template <int KIND, int NT, int TILES>
 struct Ring {
-  static constexpr int kWeights = KIND == KIND_8 ? 1 : 2 * TILES;           // pieces of weights per step and thread
+  static constexpr int kWeights = KIND == KIND_8 ? 1 : KIND == KIND_24 ? 3 : 2 * TILES;    // pieces of weights per step and thread
   static constexpr int kPieces = kWeights + NT;
   static constexpr int kBlocksPerSm = NT * TILES >= 8 ? 1 : NT * TILES >= 4 ? 2 : 3;
   static constexpr int kPieceBytes = 32 * kWarps * 16;
@@ -66,14 +70,14 @@ struct Ring {
   static constexpr int kRingBytes = kDepth * kPieces * kPieceBytes;
   static constexpr int kBytes = kRingBytes + kPartBytes;
   static_assert(kDepth >= 3 && kBlocksPerSm * (kBytes + 1024) <= 233472, "the blocks of an SM");
-  static_assert(KIND != KIND_8 || TILES == 1, "half a tile");
+  static_assert(KIND == KIND_8 ? TILES == 1 : KIND != KIND_24 || TILES == 2, "half a tile; one and a half");
 };
 
 template <int KIND, int NT, int TILES>
 __global__ void __launch_bounds__(32 * kWarps, Ring<KIND, NT, TILES>::kBlocksPerSm)
 few_rows_kernel(const FewRows p) {
   using R = Ring<KIND, NT, TILES>;
-  constexpr int COLS = KIND == KIND_16 ? 16 * TILES : 8 * TILES;       // output columns of a group
+  constexpr int COLS = kColumns<KIND, TILES>;       // output columns of a group
   extern __shared__ __align__(16) uint8_t smem[];
   float* part = reinterpret_cast<float*>(smem + R::kRingBytes);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -108,11 +112,11 @@ few_rows_kernel(const FewRows p) {
     const bool in = c.k + 8 * t < p.K;
     const __nv_bfloat16* w = p.w + (in ? c.k + 8 * t : 0);
 #pragma unroll
-    for (int i = 0; i < (KIND == KIND_8 ? 1 : TILES); ++i) {
-      const int n0 = c.group * COLS + i * (KIND == KIND_16 ? 16 : 8);
+    for (int i = 0; i < TILES; ++i) {
+      const int n0 = c.group * COLS + i * (KIND == KIND_GATED ? 8 : 16);
       const int64_t r0 = min(n0 + g, p.N - 1);
       copy16(slot(depth, 2 * i), w + r0 * p.ldw, in);
-      if constexpr (KIND != KIND_8) {
+      if (whole_tile(KIND, i)) {
         const int64_t r1 = KIND == KIND_GATED ? p.N + r0 : min(n0 + g + 8, p.N - 1);
         copy16(slot(depth, 2 * i + 1), w + r1 * p.ldw, in);
       }
@@ -153,7 +157,7 @@ few_rows_kernel(const FewRows p) {
       for (int i = 0; i < TILES; ++i) {
         const uint4 u = load_slot(slot(depth, 2 * i));
         uint4 v = make_uint4(0u, 0u, 0u, 0u);
-        if constexpr (KIND != KIND_8) v = load_slot(slot(depth, 2 * i + 1));
+        if (whole_tile(KIND, i)) v = load_slot(slot(depth, 2 * i + 1));
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
           mma_16816(acc[i][j], u.x, v.x, u.y, v.y, b[j].x, b[j].y);
@@ -220,7 +224,7 @@ cudaError_t launch_tokens(const FewRows& p, cudaStream_t s) {
     return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, R::kBytes);
   });
   if (e != cudaSuccess) return e;
-  constexpr int COLS = KIND == KIND_16 ? 16 * TILES : 8 * TILES;
+  constexpr int COLS = kColumns<KIND, TILES>;
   const int groups = (p.N + COLS - 1) / COLS, most = R::kBlocksPerSm * limited_sms(device_sm_count());
   return launch_pdl(kern, dim3((unsigned)(groups < most ? groups : most)), dim3(32 * kWarps), R::kBytes, s, p);
 }
@@ -235,11 +239,21 @@ cudaError_t launch_gated(const FewRows& p, cudaStream_t s) {
   if (p.M <= 16) return wide ? launch_tokens<KIND_GATED, 2, 2>(p, s) : launch_tokens<KIND_GATED, 2, 1>(p, s);
   return wide ? launch_tokens<KIND_GATED, 4, 2>(p, s) : launch_tokens<KIND_GATED, 4, 1>(p, s);
 }
+// More than 8 tokens, columns enough for groups of 16 on every SM: the width with the fewest 16-byte pieces, of weights and tokens,
+// on the SM that has most of them.  (12800 -> 3200, both products of the block: 24 columns a group, 134 groups, 55.9 us, 32
+// columns, 100 groups, 58.7 for 16 tokens; 65.4 and 67.1 for 32.)
+template <int NT>
+cudaError_t launch_linear_many(const FewRows& p, cudaStream_t s) {
+  if (p.N / 16 < 148) return launch_tokens<KIND_8, NT, 1>(p, s);
+  auto busiest = [&](int64_t columns) {      // of 148 SMs, whatever an SM budget says: the same call always takes the same way
+    return ((p.N + columns - 1) / columns + 147) / 148 * (columns / 8 + NT);
+  };
+  if (busiest(24) < busiest(32) && busiest(24) < busiest(16)) return launch_tokens<KIND_24, NT, 2>(p, s);
+  return busiest(16) < busiest(32) ? launch_tokens<KIND_16, NT, 1>(p, s) : launch_tokens<KIND_16, NT, 2>(p, s);
+}
 cudaError_t launch_linear(const FewRows& p, cudaStream_t s) {
   if (p.M <= 8) return p.N / 16 >= 296 ? launch_tokens<KIND_16, 1, 1>(p, s) : launch_tokens<KIND_8, 1, 1>(p, s);
-  if (p.N / 32 >= 100) return p.M <= 16 ? launch_tokens<KIND_16, 2, 2>(p, s) : launch_tokens<KIND_16, 4, 2>(p, s);
-  if (p.N / 16 >= 148) return p.M <= 16 ? launch_tokens<KIND_16, 2, 1>(p, s) : launch_tokens<KIND_16, 4, 1>(p, s);
-  return p.M <= 16 ? launch_tokens<KIND_8, 2, 1>(p, s) : launch_tokens<KIND_8, 4, 1>(p, s);
+  return p.M <= 16 ? launch_linear_many<2>(p, s) : launch_linear_many<4>(p, s);
 }
 
 }  // namespace

@@ -268,6 +268,49 @@ def test_residual_update_of_a_float_block(M):
     parity(out, ref, TWO[F32], "residual")
 
 
+@pytest.mark.parametrize("D", [2371, 2500, 3200, 3600, 4800])      # groups of 24, 32 and 16 columns; a last group cut short
+@pytest.mark.parametrize("M", [9, 16, 25])
+def test_few_tokens_wide_output(M, D):
+    b = block(6, BF16, M, 264, 72, D)
+    _, hid_ref = reference_forward(b["x"], b["w_in"], b["b_in"], epd.GATE_SILU)
+    ref = hid_ref @ f64(b["w_out"]).T + f64(b["b_out"])
+    args = (BF16, b["x"], b["w_in"], b["b_in"], b["w_out"], b["b_out"], epd.GATE_SILU)
+    big = torch.full((M + 1, D + 5), float("nan"), dtype=torch.bfloat16, device="cuda")
+    parity(epd.op_gated_mlp(*args, out=big[:M, :D]), ref, TWO[BF16], "out")
+    big[:M, :D] = float("nan")
+    assert bool(torch.isnan(big).all())
+    x = torch.randn(M, D, device="cuda")
+    want = ref + x.double()
+    epd.op_gated_mlp(*args, out=x, flags=epd.LINEAR_ACCUMULATE)
+    parity(x, want, ONE[BF16], "residual")
+
+
+@pytest.mark.parametrize("dtype,M,N,K", [(BF16, 3000, 1152, 1152), (BF16, 500, 136, 72), (F32, 900, 100, 60),
+                                         (F32, 700, 640, 640), (BF16, 300, 33, 15)])
+def test_gradients_follow_what_is_in_front_of_them(dtype, M, N, K):
+    """The bias sums run beside the products and must still see what the stream did in front of the call, whoever wrote it: a copy,
+    or another step of this library, whose successors may start early."""
+    n = Draw(77, dtype)
+    x, w = n(1.0, M, K), n(K ** -0.5, N, K)
+    sources = [n(1.0, M, N) for _ in range(6)]
+    want = [epd.op_linear_backward(dtype, s, x, w) for s in sources]
+    torch.cuda.synchronize()
+    ws = torch.empty(epd.load_library().epd_linear_backward_workspace_bytes(dtype, M, N, K), dtype=torch.uint8, device="cuda")
+    pos = torch.zeros(1, M * N, dtype=torch.int32, device="cuda")
+    dout = torch.empty_like(sources[0])
+    got = []
+    for rep in range(3):
+        for i, s in enumerate(sources):
+            if (i + rep) % 2:
+                dout.copy_(s)
+            else:      # position 0 turns nothing: a copy by one of this library's kernels
+                epd.op_rope_axes(dtype, s.view(M * N, 1, 1), pos, (0,), epd.ROPE_BLOCKS, 10000.0, out=dout.view(M * N, 1, 1))
+            got.append(epd.op_linear_backward(dtype, dout, x, w, workspace=ws))
+    for i, g in enumerate(got):
+        for name in g:
+            assert torch.equal(g[name], want[i % len(sources)][name]), (i, name)
+
+
 @pytest.mark.parametrize("M", [1, 12, 200])
 def test_residual_update_and_float_output(M):
     b = block(4, BF16, M, 320, 192)
