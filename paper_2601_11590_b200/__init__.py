@@ -684,7 +684,7 @@ def _launch(torch, device, stream, fn, what, *args):
 
 def _ld(t, cols) -> int:
     """Leading dimension of a matrix; one row may have any stride."""
-    return cols if t is None or t.shape[0] <= 1 else t.stride(0)
+    return cols if t is None or t.size(0) <= 1 else t.stride(0)
 
 
 def op_gated_linear(dtype, x, w, bias, gate, out=None, pre=None, workspace=None, stream=None):
@@ -745,9 +745,13 @@ def op_gated_mlp(dtype, x, w_in, b_in, w_out, b_out, gate, out=None, hidden=None
     lib = load_library()
     if dtype == DTYPE_F32:
         workspace = _workspace(torch, workspace, lib.epd_gated_mlp_workspace_bytes(dtype, M, N, K, D), dev)
-    _launch(torch, dev, stream, lib.epd_op_gated_mlp, "epd_op_gated_mlp", dtype, _ptr(x), _ld(x, K), _ptr(w_in),
-            _ld(w_in, K), _ptr(b_in), _ptr(w_out), _ld(w_out, N), _ptr(b_out), _ptr(hidden), _ld(hidden, N), _ptr(pre),
-            _ld(pre, 2 * N), _ptr(out), _ld(out, D), _ptr(workspace), _bytes(workspace), M, N, K, D, gate, flags)
+    if M > 1:
+        ldx, ldh, ldo, ldp = x.stride(0), hidden.stride(0), out.stride(0), _ld(pre, 2 * N)
+    else:                               # one row may have any stride: see _ld()
+        ldx, ldh, ldo, ldp = K, N, D, 2 * N
+    _launch(torch, dev, stream, lib.epd_op_gated_mlp, "epd_op_gated_mlp", dtype, x.data_ptr(), ldx, w_in.data_ptr(),
+            _ld(w_in, K), _ptr(b_in), w_out.data_ptr(), _ld(w_out, N), _ptr(b_out), hidden.data_ptr(), ldh, _ptr(pre), ldp,
+            out.data_ptr(), ldo, _ptr(workspace), _bytes(workspace), M, N, K, D, gate, flags)
     return (out, hidden, pre) if save else out
 
 
@@ -838,8 +842,8 @@ def op_rope_axes(dtype, x, pos, sections, layout, theta, scale=1.0, inverse=Fals
         _expect("out", out, want, dev, x.shape)
 
     def strides(t):                     # one token or one head may have any stride
-        head = t.stride(1) if heads > 1 else dh
-        return (t.stride(0) if T > 1 else 0), head
+        s = t.stride()
+        return (s[0] if T > 1 else 0), (s[1] if heads > 1 else dh)
     (xt, xh), (ot, oh) = strides(x), strides(out)
     _launch(torch, dev, stream, load_library().epd_op_rope_axes, "epd_op_rope_axes", dtype, _ptr(x), xt, xh, _ptr(pos), ps,
             _ptr(out), ot, oh, T, heads, dh, (ctypes.c_int32 * n)(*sections), n, layout, theta, scale, int(inverse))
