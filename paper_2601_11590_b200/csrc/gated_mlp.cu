@@ -98,8 +98,9 @@ matmul_fma_kernel(const FmaArgs p, const int split) {
     at_b[i] = c < p.N ? B + (B_MN ? (b0 * FK + k) * p.ldb + n : n * p.ldb + b0 * FK + k) : nullptr;
   }
   float hold[sizeof(T) == 2 ? LA + LB : 1];      // bf16: on its way from memory to floats in shared memory
-  auto fetch_one = [&](const T*& at, const T* base, int64_t step, int width, bool in, float* to, float& held) {
-    in = in && at != nullptr;
+  const bool whole_tile = m0 + TM <= p.M && n0 + COLS <= p.N;
+  auto fetch_one = [&](const T*& at, const T* base, int64_t step, int width, bool whole, bool in, float* to, float& held) {
+    in = whole || (in && at != nullptr);
     if constexpr (sizeof(T) == 2) {
       held = in ? to_float<T>(*at) : 0.0f;
     } else {
@@ -108,27 +109,29 @@ matmul_fma_kernel(const FmaArgs p, const int split) {
       if (width == 4) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(from), "r"(in ? 16 : 0) : "memory");
       else asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(from), "r"(in ? 4 : 0) : "memory");
     }
-    if (at) at += step;
+    if (whole || at != nullptr) at += step;
   };
-  auto fetch = [&](int64_t block) {               // blocks in order
-    const int64_t left = p.K - block * FK;
-    float* sa = smem + (int)((block - b0) % L::kStages) * L::kStageFloats;
+  auto fetch_block = [&](int64_t block, float* sa, bool whole) {
+    const int left = (int)min(p.K - block * FK, (int64_t)FK);
     float* sb = sa + FK * L::kPadM;
 #pragma unroll
     for (int i = 0; i < VA; ++i) {
       int r, k;
       place(A_MN, TM, WA, i, r, k);
-      fetch_one(at_a[i], A, A_MN ? FK * p.lda : FK, WA, k < left, sa + k * L::kPadM + r, hold[sizeof(T) == 2 ? i : 0]);
+      fetch_one(at_a[i], A, A_MN ? FK * p.lda : FK, WA, whole, k < left, sa + k * L::kPadM + r, hold[sizeof(T) == 2 ? i : 0]);
     }
 #pragma unroll
     for (int i = 0; i < VB; ++i) {
       int r, k;
       place(B_MN, TN, WB, i, r, k);
-      fetch_one(at_b[i], B, B_MN ? FK * p.ldb : FK, WB, k < left, sb + k * L::kPadN + r, hold[sizeof(T) == 2 ? LA + i : 0]);
+      fetch_one(at_b[i], B, B_MN ? FK * p.ldb : FK, WB, whole, k < left, sb + k * L::kPadN + r, hold[sizeof(T) == 2 ? LA + i : 0]);
     }
   };
-  auto put = [&](int64_t block) {                 // bf16: what was fetched, to shared memory
-    float* sa = smem + (int)((block - b0) % L::kStages) * L::kStageFloats;
+  auto fetch = [&](int64_t block, float* sa) {    // blocks in order; inside the matrices without a test for every element
+    if (whole_tile && (block + 1) * FK <= p.K) fetch_block(block, sa, true);
+    else fetch_block(block, sa, false);
+  };
+  auto put = [&](float* sa) {                     // bf16: what was fetched, to shared memory
     float* sb = sa + FK * L::kPadM;
 #pragma unroll
     for (int i = 0; i < VA; ++i) {
@@ -145,29 +148,39 @@ matmul_fma_kernel(const FmaArgs p, const int split) {
   };
   auto commit = [] { asm volatile("cp.async.commit_group;" ::: "memory"); };
   float2 acc2[RM / 2][RN] = {};      // pairs of rows
+  int fill = 0, stage = 0;                        // stages of the next fetch and of the next product
+  auto filled = [&] {
+    float* at = smem + fill * L::kStageFloats;
+    if (++fill == L::kStages) fill = 0;
+    return at;
+  };
   if constexpr (sizeof(T) == 2) {
     if (b0 < b1) {
-      fetch(b0);
-      put(b0);
+      fetch(b0, nullptr);
+      put(filled());
     }
   } else {
 #pragma unroll 1
     for (int i = 0; i < L::kStages - 1; ++i) {
-      if (b0 + i < b1) fetch(b0 + i);
+      float* at = filled();
+      if (b0 + i < b1) fetch(b0 + i, at);
       commit();
     }
   }
+#pragma unroll 1
   for (int64_t b = b0; b < b1; ++b) {
     if constexpr (sizeof(T) == 2) {
       __syncthreads();
-      if (b + 1 < b1) fetch(b + 1);
+      if (b + 1 < b1) fetch(b + 1, nullptr);
     } else {
       asm volatile("cp.async.wait_group %0;" ::"n"(L::kStages - 2) : "memory");
       __syncthreads();       // this block has arrived, and everyone is done with the one before it, whose stage is taken now
-      if (b + L::kStages - 1 < b1) fetch(b + L::kStages - 1);
+      float* at = filled();
+      if (b + L::kStages - 1 < b1) fetch(b + L::kStages - 1, at);
       commit();
     }
-    const float* sa = smem + (int)((b - b0) % L::kStages) * L::kStageFloats;
+    const float* sa = smem + stage * L::kStageFloats;
+    if (++stage == L::kStages) stage = 0;
     const float* sb = sa + FK * L::kPadM;
 #pragma unroll
     for (int kk = 0; kk < FK / G; ++kk) {
@@ -193,7 +206,7 @@ matmul_fma_kernel(const FmaArgs p, const int split) {
       }
     }
     if constexpr (sizeof(T) == 2) {
-      if (b + 1 < b1) put(b + 1);
+      if (b + 1 < b1) put(filled());
     }
   }
   float acc[RM][RN];
