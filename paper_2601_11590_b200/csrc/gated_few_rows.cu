@@ -287,13 +287,14 @@ cudaError_t linear_few_rows(const void* x, int64_t ldx, const void* w, int64_t l
 }
 
 // ---- float ----------------------------------------------------------------------------------
-// Plain multiply-adds, bound by reading the weights once as well.  A warp has four weight rows (gated: the gate and up rows of
-// two columns); its lanes take every 32nd 16-byte piece of the contraction, of which 1, 2, 4 or 8 warps of the block have a
-// share each, and the lanes' sums are added by shuffles, the warps' in shared memory, always in the same order.
-// One token of a 1152 x 4304 block 91 -> 21 us (the plain-FMA tiles compute 64 rows whatever there is), 16 tokens 92 -> 46.
+// Plain multiply-adds, bound by reading the weights as well.  A warp has four weight rows (gated: the gate and up rows of two
+// columns) and one or four tokens; its lanes take every 32nd 16-byte piece of the contraction, of which 1, 2, 4 or 8 warps of the
+// block have a share each, and the lanes' sums are added by shuffles, the warps' in shared memory, always in the same order.
+// More tokens are other blocks next to this one, which find the weights in L2 (in one block, with 8 or 16 tokens in registers,
+// 8 tokens of a 3200 x 12800 block took 157 us for 129, 16 tokens 293 for 230).  One token of a 1152 x 4304 block takes 16 us
+// (91 as plain-FMA tiles, which compute 64 rows whatever there is), 16 tokens 44 (92); of 3200 x 12800, 491 MB, 4 tokens 85.
 namespace {
 
-constexpr int kRowsF32 = 4;
 
 struct FewRowsF32 {
   const float *x, *w, *bias;
@@ -303,7 +304,10 @@ struct FewRowsF32 {
   int64_t ldo, ldp;
   int gate, accumulate;
   int shares;               // warps that share a contraction
+  int token_groups;         // blocks side by side that have the same weights for other tokens
 };
+
+constexpr int kRowsF32 = 4;
 
 template <int TOKENS, bool GATED>
 __global__ void __launch_bounds__(32 * kWarps) few_rows_f32_kernel(const FewRowsF32 p) {
@@ -313,7 +317,9 @@ __global__ void __launch_bounds__(32 * kWarps) few_rows_f32_kernel(const FewRows
   __shared__ float part[kWarps][kRowsF32][TOKENS];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int share = warp % p.shares, groups = kWarps / p.shares;
-  const int64_t n0 = ((int64_t)blockIdx.x * groups + warp / p.shares) * COLS;
+  const int64_t block = blockIdx.x / p.token_groups;
+  const int m0 = (int)(blockIdx.x % p.token_groups) * TOKENS, M = min(p.M - m0, TOKENS);
+  const int64_t n0 = (block * groups + warp / p.shares) * COLS;
   const float* w[kRowsF32];
 #pragma unroll
   for (int r = 0; r < kRowsF32; ++r) {
@@ -322,10 +328,10 @@ __global__ void __launch_bounds__(32 * kWarps) few_rows_f32_kernel(const FewRows
   }
   const float* x[TOKENS];
 #pragma unroll
-  for (int m = 0; m < TOKENS; ++m) x[m] = p.x + (m < p.M ? m : 0) * p.ldx;
+  for (int m = 0; m < TOKENS; ++m) x[m] = p.x + (m0 + (m < M ? m : 0)) * p.ldx;
   float acc[kRowsF32][TOKENS] = {};
   const int step = 128 * p.shares;
-#pragma unroll (TOKENS <= 8 ? 2 : 1)
+#pragma unroll (TOKENS == 1 ? 4 : 2)
   for (int k = 128 * share + 4 * lane; k < p.K; k += step) {
     float4 a[kRowsF32];
 #pragma unroll
@@ -350,8 +356,8 @@ __global__ void __launch_bounds__(32 * kWarps) few_rows_f32_kernel(const FewRows
   __syncthreads();
   for (int i = threadIdx.x; i < groups * COLS * TOKENS; i += 32 * kWarps) {
     const int c = i % COLS, m = i / COLS % TOKENS, group = i / (COLS * TOKENS);
-    const int64_t n = ((int64_t)blockIdx.x * groups + group) * COLS + c;
-    if (m >= p.M || n >= p.N) continue;
+    const int64_t n = (block * groups + group) * COLS + c, row = m0 + m;
+    if (m >= M || n >= p.N) continue;
     float s = 0.0f, u = 0.0f;
     for (int k = 0; k < p.shares; ++k) {
       s += part[group * p.shares + k][c][m];
@@ -360,30 +366,33 @@ __global__ void __launch_bounds__(32 * kWarps) few_rows_f32_kernel(const FewRows
     if (p.bias) s += p.bias[n];
     if constexpr (GATED) {
       if (p.bias) u += p.bias[p.N + n];
-      p.out[m * p.ldo + n] = gate_act(p.gate, s) * u;
+      p.out[row * p.ldo + n] = gate_act(p.gate, s) * u;
       if (p.pre) {
-        p.pre[m * p.ldp + n] = s;
-        p.pre[m * p.ldp + p.N + n] = u;
+        p.pre[row * p.ldp + n] = s;
+        p.pre[row * p.ldp + p.N + n] = u;
       }
     } else {
-      float* o = p.out + m * p.ldo + n;
+      float* o = p.out + row * p.ldo + n;
       *o = p.accumulate ? *o + s : s;
     }
   }
 }
 
-template <bool GATED>
+template <int TOKENS, bool GATED>
 cudaError_t launch_f32(FewRowsF32& p, cudaStream_t s) {
+  constexpr int COLS = GATED ? kRowsF32 / 2 : kRowsF32;
   // as many warps to a contraction as fill the SMs twice, each with a whole step at least
-  const int64_t warps = (p.N + (GATED ? 1 : 3)) / (GATED ? 2 : 4);
+  const int64_t warps = (p.N + COLS - 1) / COLS;
+  p.token_groups = (p.M + TOKENS - 1) / TOKENS;
   p.shares = 1;
   while (p.shares < kWarps && warps * p.shares < 2 * 148 * kWarps && p.K >= 256 * p.shares) p.shares *= 2;
-  const int64_t blocks = (warps * p.shares + kWarps - 1) / kWarps;
-  const dim3 grid((unsigned)blocks), block(32 * kWarps);
-  if (p.M == 1) return launch_pdl(few_rows_f32_kernel<1, GATED>, grid, block, 0, s, p);
-  if (p.M <= 4) return launch_pdl(few_rows_f32_kernel<4, GATED>, grid, block, 0, s, p);
-  if (p.M <= 8) return launch_pdl(few_rows_f32_kernel<8, GATED>, grid, block, 0, s, p);
-  return launch_pdl(few_rows_f32_kernel<16, GATED>, grid, block, 0, s, p);
+  const int64_t blocks = (warps * p.shares + kWarps - 1) / kWarps * p.token_groups;
+  return launch_pdl(few_rows_f32_kernel<TOKENS, GATED>, dim3((unsigned)blocks), dim3(32 * kWarps), 0, s, p);
+}
+template <bool GATED>
+cudaError_t launch_f32(FewRowsF32& p, cudaStream_t s) {
+  if (p.M == 1) return launch_f32<1, GATED>(p, s);
+  return launch_f32<4, GATED>(p, s);
 }
 
 }  // namespace

@@ -330,7 +330,7 @@ cudaError_t matmul_fma_t(const FmaArgs& p, int split, cudaStream_t s) {
   cfg.numAttrs = split > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kern, p, split);
 }
-// 128 x 128 tiles where they fill the SMs, else 64 x 64, and as many CTAs per tile as fill the SMs twice and leave each at least
+// 128 x 128 tiles where they fill the SMs and are more than half full, else 64 x 64, and as many CTAs per tile as fill the SMs twice and leave each at least
 // 4 blocks of the contraction.
 template <bool A_MN, bool B_MN, int EPI>
 cudaError_t matmul_fma(int dtype, const FmaArgs& p, cudaStream_t s) {
@@ -339,7 +339,7 @@ cudaError_t matmul_fma(int dtype, const FmaArgs& p, cudaStream_t s) {
   // 16-byte copies of row-contiguous operands, where they allow
   auto whole = [](const void* ptr, int64_t ld, int64_t rows) { return ((uintptr_t)ptr & 15) == 0 && ld % 4 == 0 && rows % 4 == 0; };
   const bool wide = (A_MN || B_MN) && (!A_MN || whole(p.a, p.lda, p.M)) && (!B_MN || whole(p.b, p.ldb, p.N));
-  if (large >= 148 && dtype == EPD_DTYPE_F32)
+  if (large >= 148 && p.M > 64 && n > 64 && dtype == EPD_DTYPE_F32)
     return wide ? matmul_fma_t<float, 128, 8, 4, A_MN, B_MN, EPI>(p, 1, s) : matmul_fma_t<float, 128, 8, 1, A_MN, B_MN, EPI>(p, 1, s);
   int split = 1;
   while (split < 8 && small * split * 2 <= 2 * 148 && (p.K + FK - 1) / FK >= 8 * split) split *= 2;
