@@ -26,7 +26,7 @@ namespace {
 constexpr int FK = 16;
 
 // Multiply-adds of one projection from which a float block runs on the tensor cores.  Training steps in us, tensor cores / FMAs:
-// 512 x 256 x 1024 169 / 113, 512 x 512 x 1024 (this limit) 161 / 185, 128 x 1024 x 4096 326 / 312, 1024 x 512 x 2048 262 / 554,
+// 512 x 256 x 1024 169 / 106, 512 x 512 x 1024 (this limit) 161 / 185, 128 x 1024 x 4096 326 / 312, 1024 x 512 x 2048 262 / 554,
 // 800 x 1152 x 4304 709 / 1974.
 constexpr double kFloatTensorCoreWork = 256.0 * 1024 * 1024;
 

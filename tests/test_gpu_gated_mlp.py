@@ -470,6 +470,39 @@ def test_repeated_calls_streams_and_graphs_give_the_same_bits(M):
     assert all(torch.equal(p, q) for p, q in zip(want, captured))
 
 
+@pytest.mark.parametrize("dtype,M,N,K", [(BF16, 2500, 1152, 1024), (BF16, 90, 33, 20), (F32, 300, 256, 128), (F32, 700, 640, 640)])
+def test_captured_training_steps_back_to_back(dtype, M, N, K):
+    """A graph with a copy in front of a training step, replayed over other inputs without a pause: launches that run beside one
+    another in the graph see what it copied."""
+    sets = [block(80 + i, dtype, M, N, K) for i in range(3)]
+    b = {k: v.clone() for k, v in sets[0].items()}
+
+    def step():
+        out, hidden, pre = epd.op_gated_mlp(dtype, b["x"], b["w_in"], b["b_in"], b["w_out"], b["b_out"], epd.GATE_GELU_TANH, save=True)
+        g = epd.op_gated_mlp_backward(dtype, b["dout"], b["x"], b["w_in"], b["w_out"], hidden, pre, epd.GATE_GELU_TANH)
+        return [out] + list(g.values())
+    want = []
+    for s in sets:
+        for k in b:
+            b[k].copy_(s[k])
+        want.append(step())
+    source = {k: v.clone() for k, v in sets[0].items()}
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for k in b:
+            b[k].copy_(source[k])
+        captured = step()
+    got = []
+    for i in (1, 2, 0, 2, 1):
+        for k in b:
+            source[k].copy_(sets[i][k])
+        graph.replay()
+        got.append((i, [t.clone() for t in captured]))
+    torch.cuda.synchronize()
+    for i, r in got:
+        assert all(torch.equal(p, q) for p, q in zip(want[i], r)), i
+
+
 def test_limited_sms_change_no_result():
     b = block(71, BF16, 700, 520, 264)
     want = check_block(BF16, b, epd.GATE_SILU)
